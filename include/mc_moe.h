@@ -276,7 +276,7 @@ mc_status mc_stack_workspace(int T, int E, int k, int d, int ffn, size_t *bytes)
 
 /* A stack of n_layers MoE layers joined by residual connections: the expert
  * half of Mixtral-style decoder blocks, each with its pre-MoE RMSNorm (unit
- * gain, eps = 1e-5); attention is not part of this library.
+ * gain, eps = 1e-5); attention has its own calls (mc_attn_decode and others).
  *   h_0 = x;  for l = 0 .. n_layers-1:
  *     xn_l    = bf16(h_l / sqrt(mean_j h_l[j]^2 + 1e-5))   (per token; the
  *               sum of squares and the quotient in fp64, one rounding),
@@ -377,6 +377,157 @@ mc_status mc_pmq_expert_error(const float *w_gate, const float *w_up, const floa
                               int ffn, int group, const uint16_t *x_bf16, const mc_routing *r,
                               double *eps_host, void *workspace, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------- attention --
+ * The attention half of the decoder blocks that the MoE layers belong to, over
+ * a paged key-value cache.
+ *
+ * Cache layout (normative).  A page holds `page` consecutive tokens of one
+ * sequence for every key-value head, in blocks of 16 tokens made of 16-byte
+ * units of U elements (U = 8 for bf16, 16 for e4m3): element (token t, head h,
+ * dimension i) of page p lies at
+ *   k + p*page_stride + e * (((h*page/16 + t/16)*(D/U) + i/U)*16*U + (t%16)*U + i%U)
+ *   v + p*page_stride + e * (((h*page/16 + t/16)*(16/U) + (t%16)/U)*D*U + i*U + t%U)
+ * bytes, e the element size: a unit runs along D for keys and along the tokens
+ * for values, which is how the matrix instructions take them, so no kernel
+ * transposes anything it reads.  e4m3 is the OCP format (no infinities, NaN =
+ * 0x7f and 0xff); the value of a code is code * scale[h].
+ *
+ * Batch.  S sequences; sequence s has kv_len[s] tokens in the cache, the last
+ * q_start[s+1] - q_start[s] of them new in this call; the new tokens' rows
+ * q_start[s] .. q_start[s+1]-1 of q, k, v and the outputs hold them in order,
+ * so that row r of sequence s is at position
+ *   pos = kv_len[s] - (q_start[s+1] - q_start[s]) + (r - q_start[s]).
+ * Position j lies on page page_table[s][j / page].  Sequences without new
+ * tokens are allowed; rows before q_start[0] and from q_start[S] on are
+ * padding: their outputs are left as they were.  The device arrays are not
+ * checked on the host: page numbers outside [0, n_pages) or lengths above
+ * max_pages*page give wrong values (mc_kv_append skips such tokens) but never
+ * an access outside a buffer. */
+#define MC_KV_BF16 0
+#define MC_KV_E4M3 1
+
+typedef struct mc_kv_cache {
+  int n_pages;             /* pages in k and in v */
+  int page;                /* tokens a page: 16, 32, 64, 128 or 256 */
+  int Hkv;                 /* key-value heads, 1 .. 256 */
+  int D;                   /* head size, 64 or 128 (other values: MC_EUNSUPPORTED) */
+  int dtype;               /* MC_KV_BF16 or MC_KV_E4M3 */
+  void *k, *v;             /* device, 16-byte aligned */
+  size_t page_stride;      /* bytes between pages, a multiple of 16; mc_kv_page_bytes
+                              or more (layers may share an allocation) */
+  size_t k_bytes, v_bytes; /* from k and from v to the end of the last page */
+  const float *k_scale, *v_scale;  /* device [Hkv], positive; e4m3 only */
+} mc_kv_cache;
+
+typedef struct mc_kv_batch {
+  int S, T;                  /* sequences; rows of q, k, v and the outputs */
+  int max_pages;             /* row length of page_table */
+  int max_len;               /* host: a length that few sequences exceed, as a hint
+                                for how the work is split; 0 = max_pages*page.
+                                Results do not depend on it beyond rounding */
+  const int32_t *q_start;    /* device [S+1], ascending (mc_attn_decode: ignored) */
+  const int32_t *kv_len;     /* device [S] */
+  const int32_t *page_table; /* device [S][max_pages] */
+} mc_kv_batch;
+
+/* Bytes of one page of k (and of v).  Errors: MC_EINVAL, MC_EUNSUPPORTED. */
+mc_status mc_kv_page_bytes(int page, int Hkv, int D, int dtype, size_t *bytes);
+
+/* What mc_kv_append does to queries and keys: an RMSNorm, then a rotation of
+ * the first `rot` dimensions of each head.  NULL weights: no norm. */
+typedef struct mc_qk_prep {
+  const uint16_t *q_norm, *k_norm; /* device bf16 [D], or [Hq*D] and [Hkv*D] with
+                                      norm_row; both or neither; 16-byte aligned */
+  int norm_row;              /* 0: a norm for each head; 1: one over the whole row */
+  float eps;                 /* >= 0 */
+  int rot;                   /* rotated dimensions: 0 (none) or a multiple of 16 up to D */
+  int rope_pairs;            /* 0: dimension i turns with i + rot/2; 1: 2i with 2i+1 */
+  const float *rope;         /* device [n_pos][rot/2][2]: cosine, sine; 16-byte aligned */
+  int n_pos;                 /* positions in rope */
+} mc_qk_prep;
+
+/* Norms and rotates the new tokens' queries and keys and appends keys and
+ * values to the cache.  For every row of the batch and every head of q and k:
+ *   y = x * w / sqrt(mean(x^2) + eps)          (over D, or over the row)
+ *   (y_a, y_b) <- (y_a cos - y_b sin, y_a sin + y_b cos)   (each rotated pair)
+ * in fp32, rounded once: queries to bf16 into q_out, keys to the cache's type;
+ * values are stored as they are.  An e4m3 code is the nearest one (ties to even)
+ * of y / scale[h] clamped to +-448; NaN stays NaN.
+ * q [T][Hq*D], k and v [T][Hkv*D] bf16 with the given elements between rows
+ * (multiples of 8, so that slices of one fused projection serve); q_out
+ * likewise, and it may be q itself (same stride).  q and q_out may both be
+ * NULL: only the cache is written.  prep may be NULL: neither norm nor rotation.
+ * A token is skipped, its q_out row and its place in the cache left as they
+ * were, where its position is negative, not below kv_len or max_pages*page or
+ * (with rot) n_pos, or its page outside [0, n_pages).  Two rows must not share a
+ * place of the cache.  Limits: 1 <= Hq, Hkv <= 256; T and S at most MC_MAX_TOKENS.
+ * Errors: MC_EINVAL (shape, stride, NULL or misaligned pointer), MC_ENOSPACE
+ * (cache arrays too short), MC_EUNSUPPORTED, MC_EHIP. */
+mc_status mc_kv_append(const uint16_t *q, size_t q_stride, const uint16_t *k, size_t k_stride,
+                       const uint16_t *v, size_t v_stride, int Hq, const mc_qk_prep *prep,
+                       const mc_kv_batch *b, const mc_kv_cache *c, uint16_t *q_out, size_t out_stride,
+                       void *stream);
+
+/* Scores and masks of the attention calls.  For the query at position i and
+ * the key at position j of the same sequence
+ *   s = cap(scale * q.k) + slope[h] * (j - i),   cap(x) = softcap * tanh(x / softcap)
+ * and j is visible where j <= i and (window = 0 or j > i - window), or
+ * j < prefix[s] (and j < kv_len[s]).  Query head h reads key-value head
+ * h / (Hq / Hkv). */
+typedef struct mc_attention {
+  int Hq;                    /* query heads, a multiple of Hkv, up to 256 */
+  float scale;               /* finite */
+  float softcap;             /* 0: none; else positive */
+  int window;                /* 0: none; else positive */
+  const float *slopes;       /* device [Hq] or NULL */
+  const int32_t *prefix;     /* device [S] or NULL */
+} mc_attention;
+
+/* Workspace bytes of mc_attn_decode (T = its S) and mc_attn_prefill; they
+ * serve every smaller T too.  Errors: MC_EINVAL, MC_EUNSUPPORTED. */
+mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t *bytes);
+
+/* Attention of one new token a sequence: row s of q at position kv_len[s] - 1
+ * (b->T is ignored), after its key and value are in the cache.
+ *   o = sum_j exp(s_j - lse) v_j,   lse = ln sum_j exp(s_j)   over visible j
+ * Scores, sums and statistics in fp32; the weights exp(s - max) are rounded to
+ * bf16 for the product with the values.  A row that sees no key (kv_len 0), or
+ * only scores of -infinity, gets o = 0 and lse = -infinity.  What the cache
+ * holds at positions a row does not see has no effect on it, NaN included.
+ * q [S][Hq*D] bf16 and o likewise with their elements between rows (multiples
+ * of 8); lse [S][Hq] fp32 or NULL.  The cache is split over its length where
+ * the batch is small, the parts joined in a fixed order (deterministic).
+ * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
+mc_status mc_attn_decode(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
+                         const mc_attention *a, uint16_t *o, size_t o_stride, float *lse, void *workspace,
+                         size_t ws_bytes, void *stream);
+
+/* The same for every new token of a ragged batch (prompts, chunks of prompts
+ * over what the cache holds already, several tokens of a decoding sequence):
+ * q, o [T][Hq*D] and lse [T][Hq] in the batch's rows; rows at a negative
+ * position see no key.  Errors as mc_attn_decode. */
+mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
+                          const mc_attention *a, uint16_t *o, size_t o_stride, float *lse, void *workspace,
+                          size_t ws_bytes, void *stream);
+
+/* mc_token_importance without an attention map: the probabilities of Eq. 6 are
+ * recomputed as exp(s - lse) from the prompt's queries, its cached keys and the
+ * lse that mc_attn_prefill returned:
+ *   I_j = ||x_j||_1 * (1/Hq) * sum_h sum_{i=j}^{L-1} exp(s_hij - lse[i][h]) / (L - j)
+ * (0 for a pair that the window hides), fp32 sums in a fixed order, and
+ * important[j] = 1 for the floor(rho*L + 1/2) largest I_j (equal values: lower j
+ * first).  One sequence a call: b->S = 1, L = b->T its tokens, at positions
+ * 0 .. L-1 of page_table[0] (q_start and kv_len are ignored; rows 0 .. L-1 of
+ * q and lse).  a->prefix must be NULL (Eq. 6 is of causal attention).  x [L][d]
+ * bf16; importance [L] fp32 may be NULL.  Workspace: mc_attn_importance_workspace.
+ * Errors: MC_EINVAL (shape, rho outside [0, 1], NULL or misaligned pointer),
+ * MC_ENOSPACE, MC_EUNSUPPORTED (prefix, L above MC_MAX_TOKENS), MC_EHIP. */
+mc_status mc_attn_importance_workspace(int Hq, int L, size_t *bytes);
+mc_status mc_attn_importance(const uint16_t *q, size_t q_stride, const float *lse, const mc_kv_batch *b,
+                             const mc_kv_cache *c, const mc_attention *a, const uint16_t *x_bf16, int d,
+                             float rho, float *importance, uint8_t *important, void *workspace,
+                             size_t ws_bytes, void *stream);
+
 /* Instrumentation.  mc_timing_enable(1) clears the record and brackets every
  * kernel launch made afterwards by two HIP events on the launch stream;
  * mc_timing_enable(0) stops recording.  mc_timing_read waits for the recorded
@@ -387,7 +538,8 @@ mc_status mc_pmq_expert_error(const float *w_gate, const float *w_up, const floa
  * GEMMs' preparation, that launch, and none as prefill_prep), route_select,
  * route_lists, prefill_prep, gateup, down, combine, importance_colsum,
  * importance_finish, importance_select, rmsnorm, router, gptq_hessian,
- * gptq_factor, gptq_quantize (each a whole call).
+ * gptq_factor, gptq_quantize (each a whole call), kv_append, attn_decode,
+ * attn_prefill, attn_join, attn_colsum, attn_finish.
  * Errors: MC_EINVAL (unknown name, NULL pointer), MC_EHIP. */
 mc_status mc_timing_enable(int on);
 mc_status mc_timing_read(const char *kernel, double *total_ms, int *launches);

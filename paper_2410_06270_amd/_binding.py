@@ -43,6 +43,29 @@ class _Routing(ctypes.Structure):
                 ("pair_pos", ctypes.c_void_p), ("n_pruned", ctypes.c_void_p)]
 
 
+class _KVCache(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("page_stride", ctypes.c_size_t), ("k_bytes", ctypes.c_size_t), ("v_bytes", ctypes.c_size_t),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _KVBatch(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int), ("T", ctypes.c_int), ("max_pages", ctypes.c_int), ("max_len", ctypes.c_int),
+                ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class _QKPrep(ctypes.Structure):
+    _fields_ = [("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("norm_row", ctypes.c_int),
+                ("eps", ctypes.c_float), ("rot", ctypes.c_int), ("rope_pairs", ctypes.c_int),
+                ("rope", ctypes.c_void_p), ("n_pos", ctypes.c_int)]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("window", ctypes.c_int), ("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -111,6 +134,20 @@ def load():
         lib.mc_pmq_error_workspace.argtypes = [I, I, I, I, I, I, ctypes.POINTER(S)]
         lib.mc_pmq_expert_error.restype = st
         lib.mc_pmq_expert_error.argtypes = [P, P, P, I, I, I, I, P, ctypes.POINTER(_Routing), P, P, S, P]
+        KC, KB, AT = (ctypes.POINTER(t) for t in (_KVCache, _KVBatch, _Attention))
+        lib.mc_kv_page_bytes.restype = st
+        lib.mc_kv_page_bytes.argtypes = [I, I, I, I, ctypes.POINTER(S)]
+        lib.mc_kv_append.restype = st
+        lib.mc_kv_append.argtypes = [P, S, P, S, P, S, I, ctypes.POINTER(_QKPrep), KB, KC, P, S, P]
+        lib.mc_attn_workspace.restype = st
+        lib.mc_attn_workspace.argtypes = [I, I, I, I, ctypes.POINTER(S)]
+        for f in (lib.mc_attn_decode, lib.mc_attn_prefill):
+            f.restype = st
+            f.argtypes = [P, S, KB, KC, AT, P, S, P, P, S, P]
+        lib.mc_attn_importance_workspace.restype = st
+        lib.mc_attn_importance_workspace.argtypes = [I, I, ctypes.POINTER(S)]
+        lib.mc_attn_importance.restype = st
+        lib.mc_attn_importance.argtypes = [P, S, P, KB, KC, AT, P, I, ctypes.c_float, P, P, P, S, P]
         lib.mc_timing_enable.restype = st
         lib.mc_timing_enable.argtypes = [I]
         lib.mc_timing_read.restype = st
@@ -390,6 +427,181 @@ def pmq_expert_error(w_gate, w_up, w_down, x, routing: Routing, group: int, work
                                       _ptr(workspace), workspace.numel() * workspace.element_size(),
                                       _stream(stream)))
     return eps
+
+
+def kv_page_bytes(page: int, Hkv: int, D: int, dtype=torch.bfloat16) -> int:
+    b = ctypes.c_size_t()
+    _check(load().mc_kv_page_bytes(page, Hkv, D, _kv_dtype(dtype), ctypes.byref(b)))
+    return b.value
+
+
+def _kv_dtype(dtype) -> int:
+    assert dtype in (torch.bfloat16, torch.float8_e4m3fn), "a cache holds bfloat16 or float8_e4m3fn"
+    return 1 if dtype == torch.float8_e4m3fn else 0
+
+
+def _here(*tensors):
+    """The tensors (None aside) are on the current device, on which the kernels run."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device.index == dev), "tensors must be on the current device"
+
+
+class KVCache:
+    """Device buffers + descriptor of a paged cache (torch-allocated, or the
+    given k and v: [n_pages][..] with contiguous pages, which may be slices of
+    an allocation that layers share).  k_scale, v_scale: float32 [Hkv], for
+    float8_e4m3fn caches."""
+
+    def __init__(self, n_pages: int, page: int, Hkv: int, D: int, dtype=torch.bfloat16, k=None, v=None,
+                 k_scale=None, v_scale=None, device=None):
+        kind = _kv_dtype(dtype)
+        per = kv_page_bytes(page, Hkv, D, dtype)
+        e = 1 if kind else 2
+        device = device or torch.device("cuda")
+        if k is None:
+            k = torch.zeros((n_pages, per // e), dtype=dtype, device=device)
+        if v is None:
+            v = torch.zeros((n_pages, per // e), dtype=dtype, device=device)
+        for t in (k, v):
+            assert t.element_size() == e and t.is_cuda and t.shape[0] == n_pages
+            assert t.numel() * e == n_pages * per and t[0].is_contiguous()
+        stride = k.stride(0) * e if n_pages > 1 else per
+        assert n_pages == 1 or v.stride(0) * e == stride, "k and v differ in their page stride"
+        if kind:
+            for t in (k_scale, v_scale):
+                assert t is not None and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == Hkv
+        self.n_pages, self.page, self.Hkv, self.D, self.dtype = n_pages, page, Hkv, D, dtype
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        nb = (n_pages - 1) * stride + per
+        self.desc = _KVCache(n_pages, page, Hkv, D, kind, k.data_ptr(), v.data_ptr(), stride, nb, nb,
+                             k_scale.data_ptr() if k_scale is not None else None,
+                             v_scale.data_ptr() if v_scale is not None else None)
+
+
+class KVBatch:
+    """Descriptor over a batch's device arrays (int32): kv_len [S], page_table
+    [S][max_pages] and, for calls on several new tokens a sequence, q_start
+    [S + 1] with T rows.  max_len: a length that few sequences exceed."""
+
+    def __init__(self, kv_len, page_table, q_start=None, T=None, max_len: int = 0):
+        S, max_pages = page_table.shape
+        for t in (kv_len, page_table) + (() if q_start is None else (q_start,)):
+            assert t.dtype == torch.int32 and t.is_contiguous() and t.is_cuda
+        assert kv_len.numel() == S and (q_start is None or q_start.numel() == S + 1)
+        assert q_start is None or T is not None, "q_start comes with T, the number of rows"
+        self.S, self.T, self.max_pages = S, S if T is None else int(T), max_pages
+        self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
+        self.desc = _KVBatch(S, self.T, max_pages, int(max_len), None if q_start is None else q_start.data_ptr(),
+                             kv_len.data_ptr(), page_table.data_ptr())
+
+
+class QKPrep:
+    """Norm and rotation of kv_append.  rope: float32 [n_pos][rot/2][2] (cosine,
+    sine); q_norm, k_norm: bfloat16 weights of a head, or with norm_row of the
+    whole row."""
+
+    def __init__(self, rope=None, rope_pairs: bool = False, q_norm=None, k_norm=None, norm_row: bool = False,
+                 eps: float = 1e-5):
+        if rope is not None:
+            assert rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2
+        for t in (q_norm, k_norm):
+            assert t is None or (t.element_size() == 2 and t.is_contiguous())
+        self.rope, self.q_norm, self.k_norm, self.norm_row = rope, q_norm, k_norm, bool(norm_row)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.desc = _QKPrep(ptr(q_norm), ptr(k_norm), int(norm_row), float(eps),
+                            0 if rope is None else 2 * rope.shape[1], int(rope_pairs), ptr(rope),
+                            0 if rope is None else rope.shape[0])
+
+
+class Attention:
+    """Scores and masks of the attention calls.  slopes: float32 [Hq]; prefix:
+    int32 [S]."""
+
+    def __init__(self, Hq: int, scale: float, softcap: float = 0.0, window: int = 0, slopes=None, prefix=None):
+        assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_contiguous() and slopes.numel() == Hq)
+        assert prefix is None or (prefix.dtype == torch.int32 and prefix.is_contiguous())
+        self.Hq, self.slopes, self.prefix = Hq, slopes, prefix
+        self.desc = _Attention(Hq, float(scale), float(softcap), int(window),
+                               None if slopes is None else slopes.data_ptr(),
+                               None if prefix is None else prefix.data_ptr())
+
+
+def _row_matrix(t, rows: int, width: int):
+    """(pointer, elements between rows) of a bf16 matrix with contiguous rows."""
+    assert t.element_size() == 2 and t.dim() == 2 and tuple(t.shape) == (rows, width)
+    assert t.stride(1) == 1 or width == 1
+    return _ptr(t), max(width, t.stride(0)) if rows > 1 else (width + 7) // 8 * 8
+
+
+def kv_append(q, k, v, prep, batch: KVBatch, cache: KVCache, q_out, stream=None, Hq=None):
+    """q [T][Hq*D], k and v [T][Hkv*D], q_out [T][Hq*D]: bf16, rows may be slices
+    of wider ones; q and q_out may be None.  prep: QKPrep or None."""
+    _here(q, k, v, q_out, cache.k, batch.kv_len)
+    T, D = batch.T, cache.D
+    assert batch.q_start is not None
+    if q is not None:
+        Hq = q.shape[1] // D
+    qp, qs = (None, 0) if q is None else _row_matrix(q, T, Hq * D)
+    op, os_ = (None, 0) if q_out is None else _row_matrix(q_out, T, Hq * D)
+    kp, ks = _row_matrix(k, T, cache.Hkv * D)
+    vp, vs = _row_matrix(v, T, cache.Hkv * D)
+    if prep is not None and prep.q_norm is not None and prep.k_norm is not None:
+        assert prep.k_norm.numel() == (cache.Hkv * D if prep.norm_row else D)
+        assert q is None or prep.q_norm.numel() == (Hq * D if prep.norm_row else D)
+    _check(load().mc_kv_append(qp, qs, kp, ks, vp, vs, Hq or 1, None if prep is None else ctypes.byref(prep.desc),
+                               ctypes.byref(batch.desc), ctypes.byref(cache.desc), op, os_, _stream(stream)))
+
+
+def attn_workspace(T: int, Hq: int, Hkv: int, D: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load().mc_attn_workspace(T, Hq, Hkv, D, ctypes.byref(b)))
+    return b.value
+
+
+def _attn(fn, rows, q, batch, cache, attn, o, workspace, lse, stream):
+    _here(q, o, lse, workspace, cache.k, batch.kv_len)
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * attn.Hq)
+    assert attn.prefix is None or attn.prefix.numel() == batch.S
+    qp, qs = _row_matrix(q, rows, attn.Hq * cache.D)
+    op, os_ = _row_matrix(o, rows, attn.Hq * cache.D)
+    _check(fn(qp, qs, ctypes.byref(batch.desc), ctypes.byref(cache.desc), ctypes.byref(attn.desc), op, os_, _ptr(lse),
+              _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def attn_decode(q, batch: KVBatch, cache: KVCache, attn: Attention, o, workspace, lse=None, stream=None):
+    """q, o [S][Hq*D] bf16 (rows may be slices of wider ones); lse [S][Hq] float32."""
+    _attn(load().mc_attn_decode, batch.S, q, batch, cache, attn, o, workspace, lse, stream)
+
+
+def attn_prefill(q, batch: KVBatch, cache: KVCache, attn: Attention, o, workspace, lse=None, stream=None):
+    """q, o [T][Hq*D] bf16 (rows may be slices of wider ones); lse [T][Hq] float32."""
+    assert batch.q_start is not None
+    _attn(load().mc_attn_prefill, batch.T, q, batch, cache, attn, o, workspace, lse, stream)
+
+
+def attn_importance_workspace(Hq: int, L: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load().mc_attn_importance_workspace(Hq, L, ctypes.byref(b)))
+    return b.value
+
+
+def attn_importance(q, lse, batch: KVBatch, cache: KVCache, attn: Attention, x, rho: float, important, workspace,
+                    importance=None, stream=None):
+    """q [L][Hq*D] bf16, lse [L][Hq] float32 (as attn_prefill wrote it), x [L][d] bf16;
+    writes the protected mask (uint8 [L]) and, if given, the importance (float32 [L])."""
+    _here(q, lse, x, important, importance, workspace, cache.k)
+    L = batch.T
+    assert x.dim() == 2 and x.shape[0] == L and x.is_contiguous() and x.element_size() == 2
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == L * attn.Hq
+    assert important.dtype == torch.uint8 and important.is_contiguous() and important.numel() == L
+    assert importance is None or (importance.dtype == torch.float32 and importance.is_contiguous()
+                                  and importance.numel() == L)
+    qp, qs = _row_matrix(q, L, attn.Hq * cache.D)
+    _check(load().mc_attn_importance(qp, qs, _ptr(lse), ctypes.byref(batch.desc), ctypes.byref(cache.desc),
+                                     ctypes.byref(attn.desc), _ptr(x), x.shape[1], ctypes.c_float(rho),
+                                     _ptr(importance), _ptr(important), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def timing_enable(on: bool = True):

@@ -8,7 +8,7 @@
 #include <mutex>
 #include <vector>
 
-#include "mc_internal.hpp"
+#include "attn.hpp"
 
 // Workspace of mc_moe_forward_noalloc: a file-scope device array, one copy
 // on every GPU the library runs on, held until the process ends.  Host code
@@ -712,6 +712,233 @@ mc_status mc_timing_read(const char* kernel, double* total_ms, int* launches) {
   const int site = mc::timing_site(kernel);
   if (site < 0) return fail(MC_EINVAL, "unknown kernel name '%s'", kernel);
   return hip_status(mc::timing_read(site, total_ms, launches), "mc_timing_read");
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------- attention --
+namespace {
+
+bool misaligned(const void* p, size_t to = 16) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+mc_status check_kv_shape(int page, int Hkv, int D, int dtype) {
+  if (page < 16 || page > 256 || (page & (page - 1)))
+    return fail(MC_EINVAL, "page=%d: 16, 32, 64, 128 or 256 tokens", page);
+  if (Hkv < 1 || Hkv > 256) return fail(MC_EINVAL, "Hkv=%d outside [1, 256]", Hkv);
+  if (D != 64 && D != 128)
+    return fail(D > 0 && D % 16 == 0 ? MC_EUNSUPPORTED : MC_EINVAL, "head size %d: this build supports 64 and 128", D);
+  if (dtype != MC_KV_BF16 && dtype != MC_KV_E4M3) return fail(MC_EINVAL, "cache dtype %d", dtype);
+  return MC_OK;
+}
+
+size_t kv_page_bytes(int page, int Hkv, int D, int dtype) {
+  return (size_t)page * Hkv * D * (dtype == MC_KV_E4M3 ? 1 : 2);
+}
+
+mc_status check_cache(const mc_kv_cache* c) {
+  if (!c) return fail(MC_EINVAL, "cache descriptor is NULL");
+  mc_status s = check_kv_shape(c->page, c->Hkv, c->D, c->dtype);
+  if (s != MC_OK) return s;
+  if (c->n_pages < 1) return fail(MC_EINVAL, "n_pages=%d must be >= 1", c->n_pages);
+  if (!c->k || !c->v) return fail(MC_EINVAL, "cache k or v is NULL");
+  if (misaligned(c->k) || misaligned(c->v)) return fail(MC_EINVAL, "cache k or v is not 16-byte aligned");
+  if ((c->dtype == MC_KV_E4M3) != (c->k_scale != nullptr) || (c->dtype == MC_KV_E4M3) != (c->v_scale != nullptr))
+    return fail(MC_EINVAL, "k_scale and v_scale belong to e4m3 caches, and to those only");
+  const size_t need = kv_page_bytes(c->page, c->Hkv, c->D, c->dtype);
+  if (c->page_stride % 16 || c->page_stride < need)
+    return fail(MC_EINVAL, "page_stride %zu: a multiple of 16, at least %zu", c->page_stride, need);
+  const size_t n = (size_t)c->n_pages - 1;
+  if (c->page_stride > ((size_t)1 << 40) || n * c->page_stride + need > c->k_bytes ||
+      n * c->page_stride + need > c->v_bytes)
+    return fail(MC_ENOSPACE, "cache arrays hold %zu/%zu bytes, need %zu", c->k_bytes, c->v_bytes,
+                n * c->page_stride + need);
+  return MC_OK;
+}
+
+mc_status check_batch(const mc_kv_batch* b, bool ragged) {
+  if (!b) return fail(MC_EINVAL, "batch descriptor is NULL");
+  if (b->S < 1 || (ragged && b->T < 1)) return fail(MC_EINVAL, "S=%d and T=%d must be >= 1", b->S, b->T);
+  if (b->S > MC_MAX_TOKENS || (ragged && b->T > MC_MAX_TOKENS))
+    return fail(MC_EUNSUPPORTED, "S=%d or T=%d above %d", b->S, b->T, MC_MAX_TOKENS);
+  if (b->max_pages < 1 || b->max_len < 0)
+    return fail(MC_EINVAL, "max_pages=%d must be >= 1 and max_len=%d >= 0", b->max_pages, b->max_len);
+  if (!b->kv_len || !b->page_table || (ragged && !b->q_start))
+    return fail(MC_EINVAL, "q_start, kv_len or page_table is NULL");
+  return MC_OK;
+}
+
+mc_status check_attention(const mc_attention* a, const mc_kv_cache* c) {
+  if (!a) return fail(MC_EINVAL, "attention descriptor is NULL");
+  if (a->Hq < 1 || a->Hq > 256 || a->Hq % c->Hkv)
+    return fail(MC_EINVAL, "Hq=%d: a multiple of Hkv=%d up to 256", a->Hq, c->Hkv);
+  if (!std::isfinite(a->scale) || !(a->softcap >= 0.0f) || !std::isfinite(a->softcap))
+    return fail(MC_EINVAL, "scale %g and softcap %g: finite, softcap >= 0", (double)a->scale, (double)a->softcap);
+  if (a->window < 0) return fail(MC_EINVAL, "window=%d must be >= 0", a->window);
+  return MC_OK;
+}
+
+mc_status check_rows(const char* what, const void* p, size_t stride, size_t width) {
+  if (!p) return fail(MC_EINVAL, "%s is NULL", what);
+  if (misaligned(p)) return fail(MC_EINVAL, "%s is not 16-byte aligned", what);
+  if (stride % 8 || stride < width || stride > ((size_t)1 << 32))
+    return fail(MC_EINVAL, "%s: %zu elements between rows: a multiple of 8, at least %zu", what, stride, width);
+  return MC_OK;
+}
+
+mc::KvArgs kv_args(const mc_kv_cache* c) {
+  int lb = 0;
+  while ((16 << lb) < c->page) ++lb;
+  return {static_cast<char*>(c->k), static_cast<char*>(c->v), c->page_stride, c->n_pages, c->Hkv, lb,
+          c->k_scale, c->v_scale};
+}
+
+mc::BatchArgs batch_args(const mc_kv_batch* b) {
+  return {b->q_start, b->kv_len, b->page_table, b->S, b->T, b->max_pages};
+}
+
+mc::ScoreArgs score_args(const mc_attention* a, const mc_kv_cache* c) {
+  return {a->Hq, a->Hq / c->Hkv, a->scale, a->softcap, a->window, a->slopes, a->prefix};
+}
+
+int longest(const mc_kv_batch* b, const mc_kv_cache* c) {
+  const long long most = (long long)b->max_pages * c->page;
+  if (b->max_len > 0 && b->max_len < most) return b->max_len;
+  return (int)std::min<long long>(most, 0x7fffffff);
+}
+
+mc_status check_attn_call(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
+                          const mc_attention* a, const uint16_t* o, size_t o_stride, const void* ws, size_t ws_bytes,
+                          bool ragged) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_batch(b, ragged);
+  if (s == MC_OK) s = check_attention(a, c);
+  if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
+  if (s == MC_OK) s = check_rows("o", o, o_stride, (size_t)a->Hq * c->D);
+  if (s != MC_OK) return s;
+  if (!ws || misaligned(ws)) return fail(MC_EINVAL, "workspace is NULL or not 16-byte aligned");
+  const size_t need = mc::attn_workspace_bytes(ragged ? b->T : b->S, a->Hq, c->Hkv, c->D);
+  if (ws_bytes < need) return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+  return MC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+mc_status mc_kv_page_bytes(int page, int Hkv, int D, int dtype, size_t* bytes) {
+  if (!bytes) return fail(MC_EINVAL, "bytes is NULL");
+  mc_status s = check_kv_shape(page, Hkv, D, dtype);
+  if (s != MC_OK) return s;
+  *bytes = kv_page_bytes(page, Hkv, D, dtype);
+  return MC_OK;
+}
+
+mc_status mc_kv_append(const uint16_t* q, size_t q_stride, const uint16_t* k, size_t k_stride, const uint16_t* v,
+                       size_t v_stride, int Hq, const mc_qk_prep* prep, const mc_kv_batch* b, const mc_kv_cache* c,
+                       uint16_t* q_out, size_t out_stride, void* stream) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_batch(b, true);
+  if (s != MC_OK) return s;
+  if (Hq < 1 || Hq > 256) return fail(MC_EINVAL, "Hq=%d outside [1, 256]", Hq);
+  if (!q != !q_out) return fail(MC_EINVAL, "q and q_out: both or neither");
+  if (q) {
+    s = check_rows("q", q, q_stride, (size_t)Hq * c->D);
+    if (s == MC_OK) s = check_rows("q_out", q_out, out_stride, (size_t)Hq * c->D);
+    if (s == MC_OK && q == q_out && q_stride != out_stride)
+      s = fail(MC_EINVAL, "q_out is q with another stride");
+  }
+  if (s == MC_OK) s = check_rows("k", k, k_stride, (size_t)c->Hkv * c->D);
+  if (s == MC_OK) s = check_rows("v", v, v_stride, (size_t)c->Hkv * c->D);
+  if (s != MC_OK) return s;
+  mc::QkPrepArgs p = {nullptr, nullptr, 0, 0.0f, 0, 0, nullptr, 0x7fffffff};
+  if (prep) {
+    if (!prep->q_norm != !prep->k_norm) return fail(MC_EINVAL, "q_norm and k_norm: both or neither");
+    if (misaligned(prep->q_norm) || misaligned(prep->k_norm))
+      return fail(MC_EINVAL, "q_norm or k_norm is not 16-byte aligned");
+    if (!(prep->eps >= 0.0f) || !std::isfinite(prep->eps))
+      return fail(MC_EINVAL, "eps %g must be finite and >= 0", (double)prep->eps);
+    if (prep->rot < 0 || prep->rot > c->D || prep->rot % 16)
+      return fail(MC_EINVAL, "rot=%d: 0 or a multiple of 16 up to %d", prep->rot, c->D);
+    if (prep->rot && (!prep->rope || misaligned(prep->rope) || prep->n_pos < 1))
+      return fail(MC_EINVAL, "rope is NULL or not 16-byte aligned, or n_pos=%d < 1", prep->n_pos);
+    p = {prep->q_norm, prep->k_norm, prep->norm_row != 0, prep->eps, prep->rot, prep->rope_pairs != 0,
+         prep->rope, prep->rot ? prep->n_pos : 0x7fffffff};
+  }
+  (void)hipGetLastError();
+  return hip_status(mc::launch_kv_append({q, q_stride}, {k, k_stride}, {v, v_stride}, Hq, c->D, p, batch_args(b),
+                                         kv_args(c), {q_out, out_stride}, static_cast<hipStream_t>(stream)),
+                    "mc_kv_append launch");
+}
+
+mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t* bytes) {
+  if (!bytes) return fail(MC_EINVAL, "bytes is NULL");
+  mc_status s = check_kv_shape(16, Hkv, D, MC_KV_BF16);
+  if (s != MC_OK) return s;
+  if (T < 1 || Hq < 1 || Hq > 256 || Hq % Hkv) return fail(MC_EINVAL, "bad shape T=%d Hq=%d Hkv=%d", T, Hq, Hkv);
+  if (T > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "T=%d above %d", T, MC_MAX_TOKENS);
+  *bytes = mc::attn_workspace_bytes(T, Hq, Hkv, D);
+  return MC_OK;
+}
+
+mc_status mc_attn_decode(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
+                         const mc_attention* a, uint16_t* o, size_t o_stride, float* lse, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  mc_status s = check_attn_call(q, q_stride, b, c, a, o, o_stride, workspace, ws_bytes, false);
+  if (s != MC_OK) return s;
+  (void)hipGetLastError();
+  return hip_status(mc::launch_attn_decode({q, q_stride}, c->D, batch_args(b), kv_args(c), score_args(a, c),
+                                           {o, o_stride}, lse, longest(b, c), workspace,
+                                           static_cast<hipStream_t>(stream)),
+                    "mc_attn_decode launch");
+}
+
+mc_status mc_attn_prefill(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
+                          const mc_attention* a, uint16_t* o, size_t o_stride, float* lse, void* workspace,
+                          size_t ws_bytes, void* stream) {
+  mc_status s = check_attn_call(q, q_stride, b, c, a, o, o_stride, workspace, ws_bytes, true);
+  if (s != MC_OK) return s;
+  (void)hipGetLastError();
+  return hip_status(mc::launch_attn_prefill({q, q_stride}, c->D, batch_args(b), kv_args(c), score_args(a, c),
+                                            {o, o_stride}, lse, longest(b, c), workspace,
+                                            static_cast<hipStream_t>(stream)),
+                    "mc_attn_prefill launch");
+}
+
+mc_status mc_attn_importance_workspace(int Hq, int L, size_t* bytes) {
+  if (!bytes) return fail(MC_EINVAL, "bytes is NULL");
+  if (Hq < 1 || Hq > 256 || L < 1) return fail(MC_EINVAL, "bad shape Hq=%d L=%d", Hq, L);
+  if (L > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "L=%d above %d", L, MC_MAX_TOKENS);
+  *bytes = mc::attn_importance_bytes(Hq, L);
+  return MC_OK;
+}
+
+mc_status mc_attn_importance(const uint16_t* q, size_t q_stride, const float* lse, const mc_kv_batch* b,
+                             const mc_kv_cache* c, const mc_attention* a, const uint16_t* x_bf16, int d, float rho,
+                             float* importance, uint8_t* important, void* workspace, size_t ws_bytes, void* stream) {
+  mc_status s = check_cache(c);
+  if (s != MC_OK) return s;
+  if (!b) return fail(MC_EINVAL, "batch descriptor is NULL");
+  if (b->S != 1 || b->T < 1) return fail(MC_EINVAL, "S=%d, T=%d: one sequence of at least one token", b->S, b->T);
+  if (b->T > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "T=%d above %d", b->T, MC_MAX_TOKENS);
+  if (!b->page_table) return fail(MC_EINVAL, "page_table is NULL");
+  if ((long long)b->max_pages * c->page < b->T)
+    return fail(MC_EINVAL, "max_pages=%d do not hold %d tokens", b->max_pages, b->T);
+  s = check_attention(a, c);
+  if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
+  if (s != MC_OK) return s;
+  if (a->prefix) return fail(MC_EUNSUPPORTED, "a prefix: Eq. 6 is of causal attention");
+  if (d < 1) return fail(MC_EINVAL, "d=%d must be >= 1", d);
+  if (!(rho >= 0.0f && rho <= 1.0f)) return fail(MC_EINVAL, "rho %g outside [0, 1]", (double)rho);
+  if (!lse || !x_bf16 || !important || !workspace)
+    return fail(MC_EINVAL, "lse, x, important or workspace is NULL");
+  if (misaligned(workspace)) return fail(MC_EINVAL, "workspace is not 16-byte aligned");
+  const size_t need = mc::attn_importance_bytes(a->Hq, b->T);
+  if (ws_bytes < need) return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+  (void)hipGetLastError();
+  return hip_status(mc::launch_attn_importance({q, q_stride}, lse, c->D, batch_args(b), kv_args(c), score_args(a, c),
+                                               x_bf16, d, rho, importance, important, workspace,
+                                               static_cast<hipStream_t>(stream)),
+                    "mc_attn_importance launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,179 @@
+// attn.hpp -- the paged cache as the attention kernels see it: launch
+// arguments, address arithmetic, visibility and number formats.
+#pragma once
+
+#include "mc_internal.hpp"
+
+namespace mc {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_inff();
+constexpr int kKvBlock = 16;         // tokens of a cache block
+
+struct KvArgs {
+  char *k, *v;
+  size_t page_stride;                // bytes
+  int n_pages, Hkv, lb;              // lb: log2 of the blocks in a page
+  const float *k_scale, *v_scale;    // null for bf16
+};
+
+struct BatchArgs {
+  const int32_t *q_start, *kv_len, *page_table;
+  int S, T, max_pages;
+};
+
+struct ScoreArgs {
+  int Hq, g;                         // g = Hq / Hkv
+  float scale, softcap;
+  int window;
+  const float* slopes;
+  const int32_t* prefix;
+};
+
+// Partial results of a split: o [row][Hq][nsplit][D] (unnormalised, relative to
+// the part's own maximum), ml [row][Hq][nsplit][2] (maximum in the log2
+// domain, sum), row a row of the outputs.
+struct SplitArgs {
+  float *o, *ml;
+  int nsplit;
+};
+
+// The longest length the tables describe, and a sequence's length within it.
+__device__ __forceinline__ int kv_length(const KvArgs& c, const BatchArgs& b, int s) {
+  const long long most = ((long long)b.max_pages << c.lb) * kKvBlock;
+  const long long n = b.kv_len[s];
+  return (int)(n < 0 ? 0 : n > most ? (most > 0x7fffffff ? 0x7fffffff : most) : n);
+}
+
+__device__ __forceinline__ int kv_prefix(const ScoreArgs& a, int s, int len) {
+  if (!a.prefix) return 0;
+  const int p = a.prefix[s];
+  return p < 0 ? 0 : p > len ? len : p;
+}
+
+// A page number of the table, clamped into the cache.
+__device__ __forceinline__ int kv_page(const KvArgs& c, int p) {
+  return p < 0 ? 0 : p >= c.n_pages ? c.n_pages - 1 : p;
+}
+
+// Byte offset of block `blk` (a position / 16) of head h, on page p, the block
+// being BYTES long.
+template <int BYTES>
+__device__ __forceinline__ size_t kv_block_offset(const KvArgs& c, int p, int h, int blk) {
+  const int in_page = blk & ((1 << c.lb) - 1);
+  return (size_t)p * c.page_stride + (size_t)((h << c.lb) + in_page) * BYTES;
+}
+
+// The largest s in [0, S) with start[s] / div + mul * s <= key (0 if there is
+// none), found by the whole wave with 64 probes a round: one load for up to 64
+// sequences, two for 4096.  key must be wave-uniform; every s it returns is in
+// range whatever the array holds.
+__device__ __forceinline__ int find_sequence(const int32_t* __restrict__ start, int S, int key, int div, int mul,
+                                             int g) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = S;
+  while (n > 1) {
+    const int step = (n + 63) >> 6, at = lane * step;
+    bool below = lane == 0;
+    if (lane > 0 && at < n) {
+      const long long first = (long long)start[lo + at] * g;
+      below = first / div + (long long)mul * (lo + at) <= key;
+    }
+    const int last = 63 - __builtin_clzll(__ballot(below));
+    lo += last * step;
+    n = n - last * step < step ? n - last * step : step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Rows [first, first + n) of sequence s among the T packed ones.
+__device__ __forceinline__ void sequence_rows(const BatchArgs& b, int s, int& first, int& n) {
+  int lo = b.q_start[s], hi = b.q_start[s + 1];
+  lo = lo < 0 ? 0 : lo > b.T ? b.T : lo;
+  hi = hi < lo ? lo : hi > b.T ? b.T : hi;
+  first = lo;
+  n = hi - lo;
+}
+
+// ----------------------------------------------------------------- formats --
+
+__device__ __forceinline__ uint16_t bf16_bits(float f) {     // nearest even, NaN kept
+  const __bf16 h = (__bf16)f;
+  uint16_t b;
+  __builtin_memcpy(&b, &h, 2);
+  return b;
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const bf16x2 h = {(__bf16)lo, (__bf16)hi};
+  uint32_t b;
+  __builtin_memcpy(&b, &h, 4);
+  return b;
+}
+
+__device__ __forceinline__ bf16x8 as_bf16x8(const u32x4& v) {
+  bf16x8 r;
+  __builtin_memcpy(&r, &v, 16);
+  return r;
+}
+
+// Eight e4m3 codes (two words) as bf16: exact, bf16 holds every e4m3 value.
+__device__ __forceinline__ u32x4 e4m3_to_bf16(uint32_t a, uint32_t b) {
+  bf16x2 t[4];
+  t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
+  t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+  t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
+  t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+  u32x4 r;
+  __builtin_memcpy(&r, t, 16);
+  return r;
+}
+
+// Four e4m3 codes: nearest, ties to even, clamped to +-448 (the comparison
+// leaves a NaN as it is, and NaN converts to NaN).
+__device__ __forceinline__ float e4m3_clamp(float f) { return f > 448.0f ? 448.0f : f < -448.0f ? -448.0f : f; }
+
+__device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(a), e4m3_clamp(b), 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(c), e4m3_clamp(d), r, true);
+  return (uint32_t)r;
+}
+
+// ------------------------------------------------------------------ scores --
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// cap * tanh(x / cap) = cap * (1 - t) / (1 + t), t = exp(-2 |x| / cap), with x's
+// sign; off by 2^-23 cap at most, an fp32 rounding of a score near the cap.
+__device__ __forceinline__ float cap_score(float x, float cap, float inv_cap) {
+  const float t = exp2_fast(-2.0f * kLog2e * inv_cap * fabsf(x));
+  return copysignf(cap * (1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), x);
+}
+
+// A score in the log2 domain from the plain product q.k.  EXTRA: softcap
+// and / or slopes; scale2 = scale * log2(e), dist = j - i.
+struct ScoreConsts {
+  float scale, scale2, cap, inv_cap;
+};
+
+template <bool EXTRA>
+__device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float slope2, int dist) {
+  if (!EXTRA) return qk * c.scale2;
+  float s = qk * c.scale2;
+  if (c.cap > 0.0f) s = cap_score(qk * c.scale, c.cap, c.inv_cap) * kLog2e;
+  return s + slope2 * (float)dist;
+}
+
+// Joins the parts of every (row, head); ragged: rows outside its sequences are
+// left as they are.
+hipError_t launch_attn_join(const SplitArgs& sp, int rows, int Hq, int g, int D, const float* v_scale, RowsOut o,
+                            float* lse, const BatchArgs* ragged, hipStream_t stream);
+// At least rows * Hq * nsplit of any prefill call of up to T rows that splits.
+size_t attn_prefill_split_rows(int T, int Hq);
+
+}  // namespace mc

@@ -1,0 +1,257 @@
+// attn_importance.hip -- token importance (Sec. 3.3.2, Eq. 6) from a prompt's
+// queries, its cached keys and the softmax statistics of its attention, without
+// an attention map.
+//
+//   I_j = ||x_j||_1 * (1/Hq) * sum_h sum_{i >= j} exp(s_hij - lse_hi) / (L - j)
+//
+// A map would be Hq L^2 bf16 values, written and read; here each probability is
+// formed again where it is summed, one matrix product (half of the attention's)
+// and one exponential a pair.  Bound by the vector units: 16 pairs a lane of a 32 x 32
+// tile cost 8 matrix instructions (256 cycles of a SIMD for D = 128) and 16 x (an
+// exponential, a multiply-add and an add: 24 cycles).
+//
+// attn_colsum_kernel: a workgroup keeps 256 keys of one key-value head in
+// registers (64 a wave) and walks the rows below the diagonal, 32 at a time, of each of
+// the head's query heads; the queries come through LDS, two buffers.  Scores are keys x
+// rows, so a lane adds its own row's probabilities to 32 sums, one a key, and the 32
+// lanes' sums are joined once at the end.  The rows are dealt out to `slices` workgroups.
+// attn_finish_kernel: one wave a key: its partial sums, the norm of x_j, I_j and
+// the selection key that importance_select takes.
+#include "attn.hpp"
+
+namespace mc {
+
+constexpr int kColWaves = 4;
+constexpr int kColThreads = 64 * kColWaves;
+constexpr int kColKeys = 64 * kColWaves;      // keys of a workgroup
+constexpr int kColTarget = 2048;              // workgroups aimed at
+
+__host__ __device__ static inline int col_tiles(int L) { return (L + kColKeys - 1) / kColKeys; }
+
+// Row slices of a (key tile, key-value head): more than 8 rounds of the chip even
+// out the triangle, and no slice below one row tile of one head for the average tile.
+static int col_slices(int L, int Hkv, int g) {
+  const int wgs = col_tiles(L) * Hkv, n = (kColTarget + wgs - 1) / wgs;
+  const int most = (L + 31) / 32 * g;
+  return n > most ? most : n;
+}
+
+static size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+static size_t col_partial_bytes(int L, int Hkv, int g) {
+  return up256((size_t)col_tiles(L) * kColKeys * Hkv * col_slices(L, Hkv, g) * sizeof(float));
+}
+
+// Workspace: partial sums [Hkv * slices][tiles * 256] | selection keys.  The
+// slices depend on the number of key-value heads, which divides Hq.
+size_t attn_importance_bytes(int Hq, int L) {
+  size_t most = 0;
+  for (int Hkv = 1; Hkv <= Hq; ++Hkv)
+    if (Hq % Hkv == 0) {
+      const size_t b = col_partial_bytes(L, Hkv, Hq / Hkv);
+      if (b > most) most = b;
+    }
+  return most + up256((size_t)L * sizeof(uint64_t));
+}
+
+template <int D, bool E4, bool EXTRA>
+__global__ void __launch_bounds__(kColThreads, 2)
+    attn_colsum_kernel(RowsIn q, const float* __restrict__ lse, BatchArgs b, KvArgs c, ScoreArgs a, int L, int slices,
+                       float* __restrict__ partial) {
+  constexpr int DK = D / 16, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2), kRowBytes = 32 * D * 2;
+  __shared__ __attribute__((aligned(16))) char s_q[2][kRowBytes];
+  const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
+  int id = blockIdx.x;
+  const int hk = id % c.Hkv;
+  id /= c.Hkv;
+  const int slice = id % slices, tile = id / slices;
+  const int key0 = tile * kColKeys + 64 * wave;
+
+  // keys: lane (key n of 32, half) holds units half, half + 2, ... (bf16), or units of
+  // 16 whose first and last 8 dimensions go to two steps (e4m3)
+  bf16x8 kf[2][DK];
+  const int last_blk = (L - 1) >> 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int blk = min((key0 + 32 * h + n) >> 4, last_blk);
+    const int page = kv_page(c, b.page_table[blk >> c.lb]);
+    const char* kp = c.k + kv_block_offset<kBlockBytes>(c, page, hk, blk) + (n & 15) * 16 + half * 256;
+    if constexpr (E4) {
+#pragma unroll
+      for (int i = 0; i < DK / 2; ++i) {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(kp + 512 * i);
+        kf[h][2 * i] = as_bf16x8(e4m3_to_bf16(r[0], r[1]));
+        kf[h][2 * i + 1] = as_bf16x8(e4m3_to_bf16(r[2], r[3]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < DK; ++i) kf[h][i] = as_bf16x8(*reinterpret_cast<const u32x4*>(kp + 512 * i));
+    }
+  }
+
+  f32x16 acc[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[h][r] = 0.0f;
+  const float kscale = E4 ? c.k_scale[hk] : 1.0f;
+  const ScoreConsts sc = {a.scale * kscale, a.scale * kscale * kLog2e, a.softcap,
+                          a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f};
+
+  // (row tile, head of the group) pairs, from the diagonal down: pair y is head
+  // y % g of row tile t0 + y / g; this workgroup takes slice, slice + slices, ...
+  const int t0 = tile * (kColKeys / 32), nt = (L + 31) / 32;
+  const int t1 = a.window > 0 ? min((long long)nt, ((long long)tile * kColKeys + kColKeys - 1 + a.window - 1) / 32 + 1)
+                              : nt;
+  const int pairs = (t1 - t0) * a.g;
+  // LDS: unit (u, row) of the tile at u * 512 + row * 16, so that a step's read is
+  // contiguous; wave w copies 1/4 of the units
+  auto fetch = [&](int y, int buf) {
+    const int r0 = 32 * (t0 + y / a.g), head = hk * a.g + y % a.g;
+    const uint16_t* src = q.p + (size_t)min(r0 + n, L - 1) * q.stride + (size_t)head * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const int u = 2 * (D / 64 * wave + i);
+      lds_dma16(src + 8 * (u + half), &s_q[buf][u * 512]);
+    }
+  };
+  auto stat = [&](int y) {
+    const int r = 32 * (t0 + y / a.g) + n;
+    const float v = r < L ? lse[(size_t)r * a.Hq + hk * a.g + y % a.g] : kNegInf;
+    return v == kNegInf ? -kNegInf : v * kLog2e;     // a row without keys: every probability 0
+  };
+  float ls_next = 0.0f;
+  if (slice < pairs) {
+    fetch(slice, 0);
+    ls_next = stat(slice);
+  }
+  for (int y = slice, buf = 0; y < pairs; y += slices, buf ^= 1) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    const float ls = ls_next;
+    if (y + slices < pairs) {
+      fetch(y + slices, buf ^ 1);
+      ls_next = stat(y + slices);
+    }
+    const int r0 = 32 * (t0 + y / a.g), row = r0 + n;
+    if (r0 + 31 < key0) continue;     // above the wave's diagonal
+    const float slope2 = EXTRA && a.slopes ? a.slopes[hk * a.g + y % a.g] * kLog2e : 0.0f;
+    f32x16 sv[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sv[h][r] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DK; ++i) {
+      // unit 2 i + half, or for e4m3 units 2 (i & ~1) + 2 half + (i & 1): the
+      // dimensions of the key's unit
+      const int u = E4 ? 2 * (i & ~1) + 2 * half + (i & 1) : 2 * i + half;
+      const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(&s_q[buf][u * 512 + n * 16]));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][i], qv, sv[h], 0, 0, 0);
+    }
+    const bool whole = r0 >= key0 + 63 && (a.window == 0 || r0 + 31 - key0 < a.window);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = key0 + 32 * h + 8 * (r >> 2) + 4 * half + (r & 3);
+        float p = exp2_fast(score2<EXTRA>(sv[h][r], sc, slope2, j - row) - ls);
+        if (!whole) p = j <= row && (a.window == 0 || row - j < a.window) ? p : 0.0f;
+        acc[h][r] += p;
+      }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      for (int off = 16; off >= 1; off >>= 1) acc[h][r] += __shfl_xor(acc[h][r], off);
+  if (n == 0) {
+    float* out = partial + ((size_t)hk * slices + slice) * col_tiles(L) * kColKeys + key0 + 4 * half;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f32x4 w = {acc[h][4 * r], acc[h][4 * r + 1], acc[h][4 * r + 2], acc[h][4 * r + 3]};
+        *reinterpret_cast<f32x4*>(out + 32 * h + 8 * r) = w;
+      }
+  }
+}
+
+// One wave a key, 4 a workgroup: the parts over the lanes, then the row of x.
+constexpr int kFinishThreads = 256;
+
+__global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const float* __restrict__ partial, int parts,
+                                                                     int Hq, int L, const uint16_t* __restrict__ x,
+                                                                     int d, bool xvec, float* __restrict__ importance,
+                                                                     uint64_t* __restrict__ keys) {
+  const int lane = threadIdx.x & 63;
+  const int j = blockIdx.x * (kFinishThreads / 64) + wave_id();
+  if (j >= L) return;
+  float cs = 0.0f;
+  const size_t stride = (size_t)col_tiles(L) * kColKeys;
+  for (int i = lane; i < parts; i += 64) cs += partial[(size_t)i * stride + j];
+  float n1 = 0.0f;
+  const uint16_t* xr = x + (size_t)j * d;
+  if (xvec) {
+    for (int i = 8 * lane; i < d; i += 512) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(xr + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        n1 += fabsf(bf16_bits_to_float(v[e] & 0xffffu)) + fabsf(bf16_bits_to_float(v[e] >> 16));
+    }
+  } else {
+    for (int i = lane; i < d; i += 64) n1 += fabsf(bf16_bits_to_float(xr[i]));
+  }
+  for (int off = 32; off >= 1; off >>= 1) {
+    cs += __shfl_xor(cs, off);
+    n1 += __shfl_xor(n1, off);
+  }
+  if (lane == 0) {
+    const float I = n1 * (cs / (float)Hq) / (float)(L - j);
+    if (importance) importance[j] = I;
+    // I >= 0: its bits order like the value; ~j puts lower indices first
+    keys[j] = ((uint64_t)__float_as_uint(I) << 32) | (uint64_t)(0xffffffffu - (uint32_t)j);
+  }
+}
+
+template <int D, bool E4>
+static void colsum_launch(RowsIn q, const float* lse, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, int L,
+                          int slices, float* partial, hipStream_t stream) {
+  const dim3 grid((unsigned)((size_t)col_tiles(L) * slices * c.Hkv));
+  if (a.softcap > 0.0f || a.slopes)
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, true>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L,
+                       slices, partial);
+  else
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, false>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L,
+                       slices, partial);
+}
+
+hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const BatchArgs& b, const KvArgs& c,
+                                  const ScoreArgs& a, const uint16_t* x, int d, float rho, float* importance,
+                                  uint8_t* mask, void* ws, hipStream_t stream) {
+  const int L = b.T, slices = col_slices(L, c.Hkv, a.g);
+  float* partial = static_cast<float*>(ws);
+  uint64_t* keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + col_partial_bytes(L, c.Hkv, a.g));
+  const bool e4 = c.k_scale != nullptr;
+  timing_begin(stream, kSiteAttnColsum);
+  if (D == 64)
+    e4 ? colsum_launch<64, true>(q, lse, b, c, a, L, slices, partial, stream)
+       : colsum_launch<64, false>(q, lse, b, c, a, L, slices, partial, stream);
+  else
+    e4 ? colsum_launch<128, true>(q, lse, b, c, a, L, slices, partial, stream)
+       : colsum_launch<128, false>(q, lse, b, c, a, L, slices, partial, stream);
+  timing_end(stream, kSiteAttnColsum);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  const bool xvec = (d % 8) == 0 && (reinterpret_cast<uintptr_t>(x) % 16) == 0;
+  timing_begin(stream, kSiteAttnFinish);
+  hipLaunchKernelGGL(attn_finish_kernel, dim3((L + 3) / 4), dim3(kFinishThreads), 0, stream, partial,
+                     c.Hkv * slices, a.Hq, L, x, d, xvec, importance, keys);
+  timing_end(stream, kSiteAttnFinish);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  return launch_importance_select(keys, L, rho, mask, stream);
+}
+
+}  // namespace mc

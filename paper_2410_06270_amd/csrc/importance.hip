@@ -384,6 +384,10 @@ hipError_t launch_importance(const uint16_t* attn, int H, int L, const uint16_t*
   hipLaunchKernelGGL(importance_finish_kernel, dim3((L + kImpThreads / 64 - 1) / (kImpThreads / 64)),
                      dim3(kImpThreads), 0, stream, partial, H, L, hs, norms, importance, keys);
   timing_end(stream, kSiteImpFinish);
+  return launch_importance_select(keys, L, rho, mask, stream);
+}
+
+hipError_t launch_importance_select(const uint64_t* keys, int L, float rho, uint8_t* mask, hipStream_t stream) {
   timing_begin(stream, kSiteImpSelect);
   const int n = (int)floor((double)rho * L + 0.5);
   hipLaunchKernelGGL(importance_select_kernel, dim3(1), dim3(kImpSelectThreads), 0, stream, keys, L, n, mask);

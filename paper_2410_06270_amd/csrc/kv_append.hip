@@ -1,0 +1,297 @@
+// kv_append.hip -- new tokens into the paged cache: norm and rotation of
+// queries and keys, keys and values to their places.
+//
+//   y = x * w / sqrt(mean(x^2) + eps);   (y_a, y_b) <- (y_a c - y_b s, y_a s + y_b c)
+//
+// One launch, two kinds of workgroup.  A value unit of the cache holds 8 or 16
+// consecutive tokens of one dimension, so one lane reads 8 dimensions of all
+// the tokens of a unit and writes whole units, transposed in its registers.  A key
+// unit runs along the dimensions, and a norm over a row needs the whole row: one
+// workgroup takes one token's queries and keys, 16 bytes a lane.
+#include "attn.hpp"
+
+namespace mc {
+
+constexpr int kAppendThreads = 256;
+constexpr int kRowChunks = 4;        // chunks of 8 elements a thread holds at once
+
+// The largest number of unit groups that n new tokens from q_start on touch is
+// floor((n + 6) / U) + 1 (U = 8) and fewer for U = 16; sequence s owns the slots from
+// floor(q_start[s] / U) + 2 s on, at least floor(n / U) + 2 of them.
+__host__ __device__ static inline int append_slots(int T, int S, int U) { return T / U + 2 * S; }
+
+__device__ __forceinline__ float half_of(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xffff0000u : w << 16); }
+
+// Where a token goes: false if it is skipped.
+struct Place {
+  int pos, page;
+};
+__device__ __forceinline__ bool append_place(const KvArgs& c, const BatchArgs& b, int s, long long pos, int n_pos,
+                                             Place& out) {
+  if (pos < 0 || pos >= kv_length(c, b, s) || pos >= n_pos) return false;
+  out.pos = (int)pos;
+  out.page = b.page_table[(size_t)s * b.max_pages + (size_t)((out.pos >> 4) >> c.lb)];
+  return out.page >= 0 && out.page < c.n_pages;
+}
+
+// Values of one unit group: lanes hold 8 dimensions each, in pieces of 64.
+template <int D, bool E4>
+__device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int n_pos, int slot, int piece) {
+  constexpr int U = E4 ? 16 : 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
+  const int lane = threadIdx.x & 63, chunk = piece * 64 + lane;
+  const int s = find_sequence(b.q_start, b.S, slot, U, 2, 1);
+  const long long first = b.q_start[s], n = (long long)b.q_start[s + 1] - first;
+  const long long group = slot - (first / U + 2ll * s);
+  if (first < 0 || n <= 0 || group < 0) return;
+  const long long p0 = (long long)b.kv_len[s] - n;
+  const long long base = ((p0 > 0 ? p0 : 0) / U + group) * U;      // the group's first position
+  const long long lo = base > p0 ? base : p0, hi = base + U < p0 + n ? base + U : p0 + n;
+  Place at;
+  // a group lies in one block: its first token's page is every token's
+  if (lo >= hi || !append_place(c, b, s, lo, n_pos, at)) return;
+  long long end = kv_length(c, b, s);
+  if (end > n_pos) end = n_pos;
+  if (chunk >= c.Hkv * (D / 8)) return;
+  const int head = chunk / (D / 8), d0 = 8 * (chunk % (D / 8));
+  u32x4 raw[U];
+  bool all = true;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long pos = base + u, row = first + pos - p0;
+    const bool in = pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T;
+    raw[u] = u32x4{0u, 0u, 0u, 0u};
+    if (in) raw[u] = *reinterpret_cast<const u32x4*>(v.p + (size_t)row * v.stride + 8 * chunk);
+    all = all && in;
+  }
+  const int in_block = (int)(base & 15);
+  char* dst = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) +
+              (size_t)((in_block / U) * D + d0) * 16;
+  const float sc = E4 ? c.v_scale[head] : 1.0f;
+  if (all) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (E4) {
+          w[q] = e4m3_quad(half_of(raw[4 * q][i / 2], i & 1) / sc, half_of(raw[4 * q + 1][i / 2], i & 1) / sc,
+                           half_of(raw[4 * q + 2][i / 2], i & 1) / sc, half_of(raw[4 * q + 3][i / 2], i & 1) / sc);
+        } else {
+          const uint32_t a = raw[2 * q][i / 2], z = raw[2 * q + 1][i / 2];
+          w[q] = (i & 1) ? (a >> 16) | (z & 0xffff0000u) : (a & 0xffffu) | (z << 16);
+        }
+      }
+      *reinterpret_cast<u32x4*>(dst + 16 * i) = w;
+    }
+    return;
+  }
+  // a unit that other tokens share: element by element
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long long pos = base + u, row = first + pos - p0;
+    if (!(pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T)) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (E4)
+        dst[16 * i + u] = (char)e4m3_quad(half_of(raw[u][i / 2], i & 1) / sc, 0.0f, 0.0f, 0.0f);
+      else
+        reinterpret_cast<uint16_t*>(dst + 16 * i)[u] = (uint16_t)(raw[u][i / 2] >> (16 * (i & 1)));
+    }
+  }
+}
+
+__device__ __forceinline__ float square_sum(const u32x4& r) {
+  float s = 0.0f;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float a = half_of(r[q], 0), z = half_of(r[q], 1);
+    s += a * a;
+    s += z * z;
+  }
+  return s;
+}
+
+// Queries and keys of one token: chunk i of 8 elements in [0, nq + nk), the
+// queries' first.  A head's chunks lie in D/8 neighbouring lanes, and a thread's
+// chunks (256 apart) all start at the same dimension of their heads, so its cosines and
+// sines are loaded once.
+template <int D, bool E4>
+__device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, const BatchArgs& b, const KvArgs& c,
+                            RowsOut out, int t) {
+  constexpr int DU = D / 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
+  __shared__ float red[2][kAppendThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int nq = q.p ? Hq * DU : 0, total = nq + c.Hkv * DU;
+  const uint16_t* qr = q.p + (size_t)t * q.stride;
+  const uint16_t* kr = k.p + (size_t)t * k.stride;
+  auto load = [&](int i) {
+    u32x4 r = {0u, 0u, 0u, 0u};
+    if (i < total) r = *reinterpret_cast<const u32x4*>(i < nq ? qr + 8 * i : kr + 8 * (i - nq));
+    return r;
+  };
+  u32x4 raw[kRowChunks];
+#pragma unroll
+  for (int r = 0; r < kRowChunks; ++r) raw[r] = load(tid + r * kAppendThreads);
+
+  const int s = find_sequence(b.q_start, b.S, t, 1, 0, 1);
+  const long long first = b.q_start[s], last = b.q_start[s + 1];
+  Place at;
+  const bool in = t >= first && t < last &&
+                  append_place(c, b, s, (long long)b.kv_len[s] - (last - t), p.n_pos, at);
+  if (!in) return;                   // the same for the whole workgroup
+
+  const int d0 = 8 * (tid % DU), half = p.rot / 2;
+  const bool turns = d0 < p.rot;
+  const float* cs = p.rope + (size_t)at.pos * p.rot;
+  f32x4 tab[4];
+  if (turns) {
+    // rotation i's cosine and sine: i = d0/2 .. +3, or d0 mod half .. +7
+    const float* from = cs + (p.pairs ? d0 : 2 * (d0 < half ? d0 : d0 - half));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < 2 || !p.pairs) tab[i] = *reinterpret_cast<const f32x4*>(from + 4 * i);
+  }
+
+  float row_scale[2] = {1.0f, 1.0f};
+  if (p.q_norm && p.norm_row) {
+    float ss[2] = {0.0f, 0.0f};
+    for (int i = tid, r = 0; i < total; i += kAppendThreads, ++r) {
+      const float x = square_sum(r < kRowChunks ? raw[r & (kRowChunks - 1)] : load(i));
+      ss[i < nq ? 0 : 1] += x;
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      for (int off = 32; off >= 1; off >>= 1) ss[w] += __shfl_xor(ss[w], off);
+      if (lane == 0) red[w][tid >> 6] = ss[w];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      float x = 0.0f;
+      for (int i = 0; i < kAppendThreads / 64; ++i) x += red[w][i];
+      row_scale[w] = 1.0f / sqrtf(x / (float)((w == 0 ? Hq : c.Hkv) * D) + p.eps);
+    }
+  }
+
+  for (int i0 = 0; i0 < total; i0 += kRowChunks * kAppendThreads) {
+    if (i0) {
+#pragma unroll
+      for (int r = 0; r < kRowChunks; ++r) raw[r] = load(i0 + tid + r * kAppendThreads);
+    }
+#pragma unroll
+    for (int r = 0; r < kRowChunks; ++r) {
+      const int i = i0 + tid + r * kAppendThreads;
+      if (i - tid >= total) break;   // the same for the whole workgroup
+      const bool is_q = i < nq;
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = half_of(raw[r][j / 2], j & 1);
+      if (p.q_norm) {
+        float sc = row_scale[is_q ? 0 : 1];
+        if (!p.norm_row) {
+          float ss = square_sum(raw[r]);
+          for (int off = DU / 2; off >= 1; off >>= 1) ss += __shfl_xor(ss, off);
+          sc = 1.0f / sqrtf(ss / (float)D + p.eps);
+        }
+        u32x4 w = {0u, 0u, 0u, 0u};
+        if (i < total) {
+          const uint16_t* wp = is_q ? p.q_norm : p.k_norm;
+          w = *reinterpret_cast<const u32x4*>(wp + (p.norm_row ? 8 * (is_q ? i : i - nq) : d0));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * sc * half_of(w[j / 2], j & 1);
+      }
+      if (p.rot) {
+        if (p.pairs) {
+          if (turns) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
+              const float a = x[2 * j], z = x[2 * j + 1];
+              x[2 * j] = a * co - z * si;
+              x[2 * j + 1] = a * si + z * co;
+            }
+          }
+        } else {
+          const bool low = d0 < half;
+          const int from = turns ? lane + (low ? half / 8 : -(half / 8)) : lane;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float o = __shfl(x[j], from);
+            if (turns) {
+              const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
+              x[j] = low ? x[j] * co - o * si : o * si + x[j] * co;
+            }
+          }
+        }
+      }
+      if (i >= total) continue;
+      if (is_q) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+        *reinterpret_cast<u32x4*>(out.p + (size_t)t * out.stride + 8 * i) = w;
+      } else {
+        const int head = (i - nq) / DU;
+        char* dst = c.k + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) + (at.pos & 15) * 16;
+        if constexpr (E4) {
+          const float sc = c.k_scale[head];
+          u32x2 w = {e4m3_quad(x[0] / sc, x[1] / sc, x[2] / sc, x[3] / sc),
+                     e4m3_quad(x[4] / sc, x[5] / sc, x[6] / sc, x[7] / sc)};
+          *reinterpret_cast<u32x2*>(dst + (d0 / 16) * 256 + (d0 & 8)) = w;
+        } else {
+          u32x4 w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+          *reinterpret_cast<u32x4*>(dst + (d0 / 8) * 256) = w;
+        }
+      }
+    }
+  }
+}
+
+// The first nv workgroups write values (4 waves, each a unit group's piece),
+// the others one token's queries and keys.  Eight neighbouring tokens share the lines
+// of the key blocks, and workgroups go round the 8 XCDs in turn: row workgroup r
+// takes token 64 (r / 64) + 8 (r % 8) + r / 8 % 8, so that one XCD's cache sees
+// whole lines.
+template <int D, bool E4>
+__global__ void __launch_bounds__(kAppendThreads)
+    kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
+                     int slots, int pieces) {
+  const int blk = blockIdx.x;
+  if (blk < nv) {
+    const int w = blk * (kAppendThreads / 64) + wave_id();
+    if (w < slots * pieces) append_values<D, E4>(v, b, c, p.n_pos, w / pieces, w % pieces);
+    return;
+  }
+  const int r = blk - nv;
+  const int t = (r & ~63) + 8 * (r & 7) + ((r >> 3) & 7);
+  if (t < b.T) append_rows<D, E4>(q, k, Hq, p, b, c, out, t);
+}
+
+template <int D, bool E4>
+static void append_launch(RowsIn q, RowsIn k, RowsIn v, int Hq, const QkPrepArgs& p, const BatchArgs& b,
+                          const KvArgs& c, RowsOut out, hipStream_t stream) {
+  const int pieces = (c.Hkv * (D / 8) + 63) / 64, slots = append_slots(b.T, b.S, E4 ? 16 : 8);
+  const int per = kAppendThreads / 64, nv = (slots * pieces + per - 1) / per;
+  const int rows = (b.T + 63) / 64 * 64;
+  hipLaunchKernelGGL((kv_append_kernel<D, E4>), dim3(nv + rows), dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b,
+                     c, out, nv, slots, pieces);
+}
+
+hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const QkPrepArgs& p, const BatchArgs& b,
+                            const KvArgs& c, RowsOut out, hipStream_t stream) {
+  timing_begin(stream, kSiteKvAppend);
+  const bool e4 = c.k_scale != nullptr;
+  if (D == 64)
+    e4 ? append_launch<64, true>(q, k, v, Hq, p, b, c, out, stream)
+       : append_launch<64, false>(q, k, v, Hq, p, b, c, out, stream);
+  else
+    e4 ? append_launch<128, true>(q, k, v, Hq, p, b, c, out, stream)
+       : append_launch<128, false>(q, k, v, Hq, p, b, c, out, stream);
+  timing_end(stream, kSiteKvAppend);
+  return hipGetLastError();
+}
+
+}  // namespace mc

@@ -12,6 +12,7 @@ enum TimingSite {
   kSitePackSz, kSitePackCodes, kSiteExport, kSiteRouteFused, kSiteRouteSelect, kSiteRouteLists,
   kSiteGateUp, kSiteDown, kSiteCombine, kSitePrefillPrep, kSiteImpColsum, kSiteImpFinish, kSiteImpSelect,
   kSiteRmsNorm, kSiteRouter, kSiteGptqHessian, kSiteGptqFactor, kSiteGptqQuantize,
+  kSiteKvAppend, kSiteAttnDecode, kSiteAttnPrefill, kSiteAttnJoin, kSiteAttnColsum, kSiteAttnFinish,
   kNumSites
 };
 void timing_begin(hipStream_t stream, int site);
@@ -127,5 +128,39 @@ hipError_t launch_gptq_quantize(const float* W, const double* U, const uint8_t* 
 size_t importance_workspace_bytes(int H, int L);
 hipError_t launch_importance(const uint16_t* attn, int H, int L, const uint16_t* x, int d, float rho,
                              float* importance, uint8_t* mask, void* ws, hipStream_t stream);
+// mask_j = 1 for the floor(rho*L + 1/2) largest keys (distinct, L of them).
+hipError_t launch_importance_select(const uint64_t* keys, int L, float rho, uint8_t* mask, hipStream_t stream);
+
+// Attention over the paged cache (attn.hpp has the arguments' device forms).
+struct KvArgs;
+struct BatchArgs;
+struct ScoreArgs;
+struct QkPrepArgs {
+  const uint16_t *q_norm, *k_norm;   // null: no norm
+  int norm_row;
+  float eps;
+  int rot, pairs;
+  const float* rope;
+  int n_pos;
+};
+struct RowsIn {                      // rows of a matrix of bf16, `stride` elements apart
+  const uint16_t* p;
+  size_t stride;
+};
+struct RowsOut {
+  uint16_t* p;
+  size_t stride;
+};
+hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const QkPrepArgs& p, const BatchArgs& b,
+                            const KvArgs& c, RowsOut out, hipStream_t stream);
+size_t attn_workspace_bytes(int T, int Hq, int Hkv, int D);
+hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
+                              float* lse, int max_len, void* ws, hipStream_t stream);
+hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
+                               float* lse, int max_len, void* ws, hipStream_t stream);
+size_t attn_importance_bytes(int Hq, int L);
+hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const BatchArgs& b, const KvArgs& c,
+                                  const ScoreArgs& a, const uint16_t* x, int d, float rho, float* importance,
+                                  uint8_t* mask, void* ws, hipStream_t stream);
 
 }  // namespace mc

@@ -14,7 +14,8 @@ namespace {
 const char* const kSiteNames[kNumSites] = {
     "pack_scale_zero", "pack_codes", "export", "route_fused", "route_select",
     "route_lists",     "gateup",     "down",   "combine", "prefill_prep",
-    "importance_colsum", "importance_finish", "importance_select", "rmsnorm", "router", "gptq_hessian", "gptq_factor", "gptq_quantize"};
+    "importance_colsum", "importance_finish", "importance_select", "rmsnorm", "router", "gptq_hessian", "gptq_factor", "gptq_quantize",
+    "kv_append", "attn_decode", "attn_prefill", "attn_join", "attn_colsum", "attn_finish"};
 
 struct Pair {
   hipEvent_t start, stop;
