@@ -440,11 +440,24 @@ def _kv_dtype(dtype) -> int:
     return 1 if dtype == torch.float8_e4m3fn else 0
 
 
-def _here(*tensors):
-    """The tensors (None aside) are on the current device, on which the kernels run."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_on(dev: int, stream):
+    """The given stream, or the current one of device dev, as an address."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _here(*tensors) -> int:
+    """The current device, on which the kernels run and on which the tensors
+    (None aside) have to be."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        assert t is None or (t.is_cuda and t.device.index == dev), "tensors must be on the current device"
+        if t is not None and t.get_device() != dev:
+            raise AssertionError("tensors must be on the current device")
+    return dev
 
 
 class KVCache:
@@ -477,6 +490,7 @@ class KVCache:
         self.desc = _KVCache(n_pages, page, Hkv, D, kind, k.data_ptr(), v.data_ptr(), stride, nb, nb,
                              k_scale.data_ptr() if k_scale is not None else None,
                              v_scale.data_ptr() if v_scale is not None else None)
+        self.ref = ctypes.byref(self.desc)
 
 
 class KVBatch:
@@ -494,6 +508,7 @@ class KVBatch:
         self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
         self.desc = _KVBatch(S, self.T, max_pages, int(max_len), None if q_start is None else q_start.data_ptr(),
                              kv_len.data_ptr(), page_table.data_ptr())
+        self.ref = ctypes.byref(self.desc)
 
 
 class QKPrep:
@@ -512,6 +527,7 @@ class QKPrep:
         self.desc = _QKPrep(ptr(q_norm), ptr(k_norm), int(norm_row), float(eps),
                             0 if rope is None else 2 * rope.shape[1], int(rope_pairs), ptr(rope),
                             0 if rope is None else rope.shape[0])
+        self.ref = ctypes.byref(self.desc)
 
 
 class Attention:
@@ -525,32 +541,36 @@ class Attention:
         self.desc = _Attention(Hq, float(scale), float(softcap), int(window),
                                None if slopes is None else slopes.data_ptr(),
                                None if prefix is None else prefix.data_ptr())
+        self.ref = ctypes.byref(self.desc)
 
 
 def _row_matrix(t, rows: int, width: int):
-    """(pointer, elements between rows) of a bf16 matrix with contiguous rows."""
-    assert t.element_size() == 2 and t.dim() == 2 and tuple(t.shape) == (rows, width)
-    assert t.stride(1) == 1 or width == 1
-    return _ptr(t), max(width, t.stride(0)) if rows > 1 else (width + 7) // 8 * 8
+    """(address, elements between rows) of a bf16 matrix with contiguous rows."""
+    s0, s1 = t.stride()
+    assert t.shape == (rows, width) and t.element_size() == 2 and s1 == 1
+    return t.data_ptr(), s0 if rows > 1 else width
 
 
-def kv_append(q, k, v, prep, batch: KVBatch, cache: KVCache, q_out, stream=None, Hq=None):
+def kv_append(q, k, v, prep, batch: KVBatch, cache: KVCache, q_out, stream=None):
     """q [T][Hq*D], k and v [T][Hkv*D], q_out [T][Hq*D]: bf16, rows may be slices
     of wider ones; q and q_out may be None.  prep: QKPrep or None."""
-    _here(q, k, v, q_out, cache.k, batch.kv_len)
-    T, D = batch.T, cache.D
+    dev = _here(q, k, v, q_out, cache.k, batch.kv_len)
     assert batch.q_start is not None
+    T, D, kw = batch.T, cache.D, cache.Hkv * cache.D
+    qp, qs, op, os_, qw = None, 0, None, 0, D
     if q is not None:
-        Hq = q.shape[1] // D
-    qp, qs = (None, 0) if q is None else _row_matrix(q, T, Hq * D)
-    op, os_ = (None, 0) if q_out is None else _row_matrix(q_out, T, Hq * D)
-    kp, ks = _row_matrix(k, T, cache.Hkv * D)
-    vp, vs = _row_matrix(v, T, cache.Hkv * D)
-    if prep is not None and prep.q_norm is not None and prep.k_norm is not None:
-        assert prep.k_norm.numel() == (cache.Hkv * D if prep.norm_row else D)
-        assert q is None or prep.q_norm.numel() == (Hq * D if prep.norm_row else D)
-    _check(load().mc_kv_append(qp, qs, kp, ks, vp, vs, Hq or 1, None if prep is None else ctypes.byref(prep.desc),
-                               ctypes.byref(batch.desc), ctypes.byref(cache.desc), op, os_, _stream(stream)))
+        qw = q.shape[1]
+        assert qw % D == 0
+        qp, qs = _row_matrix(q, T, qw)
+    if q_out is not None:
+        op, os_ = _row_matrix(q_out, T, qw)
+    kp, ks = _row_matrix(k, T, kw)
+    vp, vs = _row_matrix(v, T, kw)
+    if prep is not None and prep.q_norm is not None:
+        assert prep.k_norm is None or prep.k_norm.numel() == (kw if prep.norm_row else D)
+        assert q is None or prep.q_norm.numel() == (qw if prep.norm_row else D)
+    _check(load().mc_kv_append(qp, qs, kp, ks, vp, vs, qw // D, None if prep is None else prep.ref, batch.ref,
+                               cache.ref, op, os_, _stream_on(dev, stream)))
 
 
 def attn_workspace(T: int, Hq: int, Hkv: int, D: int) -> int:
@@ -560,13 +580,14 @@ def attn_workspace(T: int, Hq: int, Hkv: int, D: int) -> int:
 
 
 def _attn(fn, rows, q, batch, cache, attn, o, workspace, lse, stream):
-    _here(q, o, lse, workspace, cache.k, batch.kv_len)
+    dev = _here(q, o, lse, workspace, cache.k, batch.kv_len)
+    width = attn.Hq * cache.D
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * attn.Hq)
     assert attn.prefix is None or attn.prefix.numel() == batch.S
-    qp, qs = _row_matrix(q, rows, attn.Hq * cache.D)
-    op, os_ = _row_matrix(o, rows, attn.Hq * cache.D)
-    _check(fn(qp, qs, ctypes.byref(batch.desc), ctypes.byref(cache.desc), ctypes.byref(attn.desc), op, os_, _ptr(lse),
-              _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    qp, qs = _row_matrix(q, rows, width)
+    op, os_ = _row_matrix(o, rows, width)
+    _check(fn(qp, qs, batch.ref, cache.ref, attn.ref, op, os_, None if lse is None else lse.data_ptr(),
+              workspace.data_ptr(), workspace.nbytes, _stream_on(dev, stream)))
 
 
 def attn_decode(q, batch: KVBatch, cache: KVCache, attn: Attention, o, workspace, lse=None, stream=None):
@@ -590,18 +611,17 @@ def attn_importance(q, lse, batch: KVBatch, cache: KVCache, attn: Attention, x, 
                     importance=None, stream=None):
     """q [L][Hq*D] bf16, lse [L][Hq] float32 (as attn_prefill wrote it), x [L][d] bf16;
     writes the protected mask (uint8 [L]) and, if given, the importance (float32 [L])."""
-    _here(q, lse, x, important, importance, workspace, cache.k)
-    L = batch.T
-    assert x.dim() == 2 and x.shape[0] == L and x.is_contiguous() and x.element_size() == 2
+    dev = _here(q, lse, x, important, importance, workspace, cache.k, batch.page_table)
+    L, d = batch.T, x.shape[1]
+    assert x.shape[0] == L and x.is_contiguous() and x.element_size() == 2
     assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == L * attn.Hq
     assert important.dtype == torch.uint8 and important.is_contiguous() and important.numel() == L
     assert importance is None or (importance.dtype == torch.float32 and importance.is_contiguous()
                                   and importance.numel() == L)
     qp, qs = _row_matrix(q, L, attn.Hq * cache.D)
-    _check(load().mc_attn_importance(qp, qs, _ptr(lse), ctypes.byref(batch.desc), ctypes.byref(cache.desc),
-                                     ctypes.byref(attn.desc), _ptr(x), x.shape[1], ctypes.c_float(rho),
-                                     _ptr(importance), _ptr(important), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(), _stream(stream)))
+    _check(load().mc_attn_importance(qp, qs, lse.data_ptr(), batch.ref, cache.ref, attn.ref, x.data_ptr(), d, rho,
+                                     None if importance is None else importance.data_ptr(), important.data_ptr(),
+                                     workspace.data_ptr(), workspace.nbytes, _stream_on(dev, stream)))
 
 
 def timing_enable(on: bool = True):

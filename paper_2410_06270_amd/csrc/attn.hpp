@@ -61,6 +61,12 @@ __device__ __forceinline__ int kv_page(const KvArgs& c, int p) {
   return p < 0 ? 0 : p >= c.n_pages ? c.n_pages - 1 : p;
 }
 
+// An entry of a device array that no kernel in flight writes, at a wave-uniform
+// index: a scalar load, which waits for no vector load before it.
+__device__ __forceinline__ int32_t uniform_entry(const int32_t* p, int i) {
+  return ((const __attribute__((address_space(4))) int32_t*)p)[__builtin_amdgcn_readfirstlane(i)];
+}
+
 // Byte offset of block `blk` (a position / 16) of head h, on page p, the block
 // being BYTES long.
 template <int BYTES>
@@ -98,6 +104,16 @@ __device__ __forceinline__ void sequence_rows(const BatchArgs& b, int s, int& fi
   hi = hi < lo ? lo : hi > b.T ? b.T : hi;
   first = lo;
   n = hi - lo;
+}
+
+// Waits for the wave's LDS accesses, then for the workgroup.  Unlike
+// __syncthreads() it leaves direct loads to LDS in flight: their arrival is
+// waited for by count (wait_vmcnt) before it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));     // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // ----------------------------------------------------------------- formats --

@@ -292,16 +292,22 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   }
 }
 
-// One wave a (row, head): the parts' maxima and sums over the lanes, then the
-// parts in order.  Parts without a visible key have l = 0 and no o.
+// One workgroup a (row, head).  Every wave finds the parts' factors
+// 2^(m - M) for itself; then D/4 threads take a part's row, 16 bytes each, the
+// 256 threads 8 (D = 128) or 16 parts at once, and their sums are joined in LDS in a fixed
+// order.  Parts without a visible key have l = 0 and no o.  (A wave for all parts of a
+// row took 56 us for 64 rows of 128 parts, this 8.)
+constexpr int kJoinThreads = 256;
+
 template <int D>
-__global__ void __launch_bounds__(256) attn_join_kernel(SplitArgs sp, int rows, int Hq, int g,
-                                                        const float* __restrict__ v_scale, RowsOut o,
-                                                        float* __restrict__ lse, const int32_t* __restrict__ q_start,
-                                                        int S) {
-  const int lane = threadIdx.x & 63;
-  const int w = blockIdx.x * 4 + wave_id();
-  if (w >= rows * Hq) return;
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, int Hq, int g,
+                                                                 const float* __restrict__ v_scale, RowsOut o,
+                                                                 float* __restrict__ lse,
+                                                                 const int32_t* __restrict__ q_start, int S) {
+  constexpr int kGroup = D / 4, kGroups = kJoinThreads / kGroup;
+  __shared__ float s_f[kMaxSplit];
+  __shared__ f32x4 s_o[kGroups][kGroup];
+  const int lane = threadIdx.x & 63, w = blockIdx.x;
   const int row = w / Hq, h = w - row * Hq;
   if (q_start && (row < q_start[0] || row >= q_start[S])) return;   // padding
   const float* ml = sp.ml + (size_t)w * sp.nsplit * 2;
@@ -323,40 +329,55 @@ __global__ void __launch_bounds__(256) attn_join_kernel(SplitArgs sp, int rows, 
   float L = 0.0f;
 #pragma unroll
   for (int i = 0; i < kMaxSplit / 64; ++i) {
-    mv[i] = lv[i] == 0.0f ? 0.0f : exp2_fast(mv[i] - M0);     // now the part's factor
-    L += lv[i] == 0.0f ? 0.0f : lv[i] * mv[i];
+    const float f = lv[i] == 0.0f ? 0.0f : exp2_fast(mv[i] - M0);
+    L += lv[i] == 0.0f ? 0.0f : lv[i] * f;
+    // -1: no o to read (a factor may itself be 0)
+    if (threadIdx.x < 64) s_f[lane + 64 * i] = lv[i] == 0.0f ? -1.0f : f;
   }
   for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
-  constexpr int E = D / 64;
-  float r[E] = {};
-  const float* po = sp.o + (size_t)w * sp.nsplit * D + E * lane;
-  for (int part = 0; part < sp.nsplit; ++part) {
-    const float f = __shfl(mv[0], part & 63), f1 = __shfl(mv[1], part & 63);
-    const float l0 = __shfl(lv[0], part & 63), l1 = __shfl(lv[1], part & 63);
-    if ((part < 64 ? l0 : l1) == 0.0f) continue;
+  __syncthreads();
+  const int grp = threadIdx.x / kGroup, d = threadIdx.x % kGroup;
+  const float* po = sp.o + (size_t)w * sp.nsplit * D + 4 * d;
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int part = grp; part < sp.nsplit; part += kGroups) {
+    const float f = s_f[part];
+    if (f == -1.0f) continue;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)part * D);
 #pragma unroll
-    for (int e = 0; e < E; ++e) r[e] += po[(size_t)part * D + e] * (part < 64 ? f : f1);
+    for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+  }
+  s_o[grp][d] = r;
+  __syncthreads();
+  if (threadIdx.x >= kGroup) return;
+#pragma unroll
+  for (int i = 1; i < kGroups; ++i) {
+    const f32x4 v = s_o[i][d];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] += v[e];
   }
   const float f = L == 0.0f ? 0.0f : (v_scale ? v_scale[h / g] : 1.0f) / L;
-  uint16_t* out = o.p + (size_t)row * o.stride + (size_t)h * D + E * lane;
-  if constexpr (E == 2)
-    *reinterpret_cast<uint32_t*>(out) = L == 0.0f ? 0u : bf16_pair(r[0] * f, r[1] * f);
-  else
-    *out = L == 0.0f ? (uint16_t)0 : bf16_bits(r[0] * f);
-  if (lse && lane == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
+  u32x2 out = {0u, 0u};
+  if (L != 0.0f) {
+    out[0] = bf16_pair(r[0] * f, r[1] * f);
+    out[1] = bf16_pair(r[2] * f, r[3] * f);
+  }
+  *reinterpret_cast<u32x2*>(o.p + (size_t)row * o.stride + (size_t)h * D + 4 * d) = out;
+  if (lse && d == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
 }
 
 hipError_t launch_attn_join(const SplitArgs& sp, int rows, int Hq, int g, int D, const float* v_scale, RowsOut o,
                             float* lse, const BatchArgs* ragged, hipStream_t stream) {
-  const dim3 grid((unsigned)(((size_t)rows * Hq + 3) / 4));
+  const dim3 grid((unsigned)((size_t)rows * Hq));
   const int32_t* q_start = ragged ? ragged->q_start : nullptr;
   const int S = ragged ? ragged->S : 0;
   timing_begin(stream, kSiteAttnJoin);
   if (D == 64)
-    hipLaunchKernelGGL(attn_join_kernel<64>, grid, dim3(256), 0, stream, sp, rows, Hq, g, v_scale, o, lse, q_start, S);
-  else
-    hipLaunchKernelGGL(attn_join_kernel<128>, grid, dim3(256), 0, stream, sp, rows, Hq, g, v_scale, o, lse, q_start,
+    hipLaunchKernelGGL(attn_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse, q_start,
                        S);
+  else
+    hipLaunchKernelGGL(attn_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse,
+                       q_start, S);
   timing_end(stream, kSiteAttnJoin);
   return hipGetLastError();
 }

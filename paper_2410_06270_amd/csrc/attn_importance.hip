@@ -12,11 +12,13 @@
 //
 // attn_colsum_kernel: a workgroup keeps 256 keys of one key-value head in
 // registers (64 a wave) and walks the rows below the diagonal, 32 at a time, of each of
-// the head's query heads; the queries come through LDS, two buffers.  Scores are keys x
+// the head's query heads; the queries come through LDS, a ring of 4 tiles.  Scores are keys x
 // rows, so a lane adds its own row's probabilities to 32 sums, one a key, and the 32
 // lanes' sums are joined once at the end.  The rows are dealt out to `slices` workgroups.
 // attn_finish_kernel: one wave a key: its partial sums, the norm of x_j, I_j and
 // the selection key that importance_select takes.
+#include <type_traits>
+
 #include "attn.hpp"
 
 namespace mc {
@@ -54,21 +56,28 @@ size_t attn_importance_bytes(int Hq, int L) {
   return most + up256((size_t)L * sizeof(uint64_t));
 }
 
+// Row tiles in flight: one is a few microseconds of memory latency away, its
+// products a fraction of one.
+constexpr int kColRing = 4;
+
 template <int D, bool E4, bool EXTRA>
 __global__ void __launch_bounds__(kColThreads, 2)
     attn_colsum_kernel(RowsIn q, const float* __restrict__ lse, BatchArgs b, KvArgs c, ScoreArgs a, int L, int slices,
                        float* __restrict__ partial) {
   constexpr int DK = D / 16, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2), kRowBytes = 32 * D * 2;
-  __shared__ __attribute__((aligned(16))) char s_q[2][kRowBytes];
+  constexpr int kLoads = D / 64 + 1;            // direct loads of a wave for a row tile
+  // a tile's queries, then its rows' lse: a copy for each wave, twice over the half waves
+  constexpr int kSlotBytes = kRowBytes + kColWaves * 256;
+  __shared__ __attribute__((aligned(16))) char s_ring[kColRing][kSlotBytes];
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % c.Hkv;
   id /= c.Hkv;
-  const int slice = id % slices, tile = id / slices;
+  const int slice = id % slices, tile = id / slices;     // the first keys have the most rows: they go first
   const int key0 = tile * kColKeys + 64 * wave;
 
   // keys: lane (key n of 32, half) holds units half, half + 2, ... (bf16), or units of
-  // 16 whose first and last 8 dimensions go to two steps (e4m3)
+  // 16 whose first and last 8 dimensions go to two steps (e4m3).
   bf16x8 kf[2][DK];
   const int last_blk = (L - 1) >> 4;
 #pragma unroll
@@ -101,41 +110,36 @@ __global__ void __launch_bounds__(kColThreads, 2)
   // (row tile, head of the group) pairs, from the diagonal down: pair y is head
   // y % g of row tile t0 + y / g; this workgroup takes slice, slice + slices, ...
   const int t0 = tile * (kColKeys / 32), nt = (L + 31) / 32;
-  const int t1 = a.window > 0 ? min((long long)nt, ((long long)tile * kColKeys + kColKeys - 1 + a.window - 1) / 32 + 1)
-                              : nt;
-  const int pairs = (t1 - t0) * a.g;
+  const long long wend = a.window > 0 ? ((long long)(tile + 1) * kColKeys + a.window - 2) / 32 + 1 : nt;
+  const int t1 = wend < nt ? (int)wend : nt;
+  const int pairs = (t1 - t0) * a.g, count = pairs > slice ? (pairs - slice + slices - 1) / slices : 0;
+  const int step_t = slices / a.g, step_h = slices - step_t * a.g;
+  auto next = [&](int& t, int& h) {
+    t += step_t;
+    h += step_h;
+    if (h >= a.g) {
+      h -= a.g;
+      ++t;
+    }
+  };
   // LDS: unit (u, row) of the tile at u * 512 + row * 16, so that a step's read is
-  // contiguous; wave w copies 1/4 of the units
-  auto fetch = [&](int y, int buf) {
-    const int r0 = 32 * (t0 + y / a.g), head = hk * a.g + y % a.g;
-    const uint16_t* src = q.p + (size_t)min(r0 + n, L - 1) * q.stride + (size_t)head * D;
+  // contiguous; wave w copies a quarter of the units
+  int ft = t0 + slice / a.g, fh = slice % a.g;           // the next pair to fetch
+  int ct = ft, ch = fh;                                  // the next to work on
+  auto fetch = [&](char* slot) {
+    const int row = min(32 * ft + n, L - 1), head = hk * a.g + fh;
+    const uint16_t* src = q.p + (size_t)row * q.stride + (size_t)head * D;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
       const int u = 2 * (D / 64 * wave + i);
-      lds_dma16(src + 8 * (u + half), &s_q[buf][u * 512]);
+      lds_dma16(src + 8 * (u + half), slot + u * 512);
     }
+    lds_dma4(lse + (size_t)row * a.Hq + head, slot + kRowBytes + 256 * wave);
+    next(ft, fh);
   };
-  auto stat = [&](int y) {
-    const int r = 32 * (t0 + y / a.g) + n;
-    const float v = r < L ? lse[(size_t)r * a.Hq + hk * a.g + y % a.g] : kNegInf;
-    return v == kNegInf ? -kNegInf : v * kLog2e;     // a row without keys: every probability 0
-  };
-  float ls_next = 0.0f;
-  if (slice < pairs) {
-    fetch(slice, 0);
-    ls_next = stat(slice);
-  }
-  for (int y = slice, buf = 0; y < pairs; y += slices, buf ^= 1) {
-    wait_vmcnt<0>();
-    __syncthreads();
-    const float ls = ls_next;
-    if (y + slices < pairs) {
-      fetch(y + slices, buf ^ 1);
-      ls_next = stat(y + slices);
-    }
-    const int r0 = 32 * (t0 + y / a.g), row = r0 + n;
-    if (r0 + 31 < key0) continue;     // above the wave's diagonal
-    const float slope2 = EXTRA && a.slopes ? a.slopes[hk * a.g + y % a.g] * kLog2e : 0.0f;
+
+  auto work = [&](auto masked, const char* slot, int row0, float ls, float slope2) {
+    constexpr bool MASKED = decltype(masked)::value;
     f32x16 sv[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -146,20 +150,51 @@ __global__ void __launch_bounds__(kColThreads, 2)
       // unit 2 i + half, or for e4m3 units 2 (i & ~1) + 2 half + (i & 1): the
       // dimensions of the key's unit
       const int u = E4 ? 2 * (i & ~1) + 2 * half + (i & 1) : 2 * i + half;
-      const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(&s_q[buf][u * 512 + n * 16]));
+      const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(slot + u * 512 + n * 16));
 #pragma unroll
       for (int h = 0; h < 2; ++h) sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][i], qv, sv[h], 0, 0, 0);
     }
-    const bool whole = r0 >= key0 + 63 && (a.window == 0 || r0 + 31 - key0 < a.window);
+    const int row = row0 + n;
+    const int low = a.window > 0 && row >= a.window ? row - a.window : -1, high = row < L ? row : -1;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = key0 + 32 * h + 8 * (r >> 2) + 4 * half + (r & 3);
-        float p = exp2_fast(score2<EXTRA>(sv[h][r], sc, slope2, j - row) - ls);
-        if (!whole) p = j <= row && (a.window == 0 || row - j < a.window) ? p : 0.0f;
+        float p = exp2_fast(EXTRA ? score2<EXTRA>(sv[h][r], sc, slope2, j - row) - ls
+                                  : __builtin_fmaf(sv[h][r], sc.scale2, -ls));
+        if (MASKED) p = ((j <= high) & (j > low)) ? p : 0.0f;
         acc[h][r] += p;
       }
+  };
+
+  // Slots of the ring are distinct and passed as such: a read of the current one
+  // then does not wait for the loads into the others.  The first fetches are rounds
+  // of the loop without work.
+  auto round = [&](const char* __restrict__ cur, char* __restrict__ nxt, bool more, bool ready) {
+    if (more) fetch(nxt);
+    if (!ready) return;
+    const int row0 = 32 * ct;
+    const float slope2 = EXTRA && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
+    next(ct, ch);
+    if (row0 + 31 < key0) return;                        // above the wave's diagonal
+    const float v = *reinterpret_cast<const float*>(cur + kRowBytes + 256 * wave + 4 * lane);
+    const float ls = v == kNegInf ? -kNegInf : v * kLog2e;       // a row without keys: every probability 0
+    if (row0 >= key0 + 63 && row0 + 32 <= L && (a.window == 0 || row0 + 31 - key0 < a.window))
+      work(std::false_type{}, cur, row0, ls, slope2);
+    else
+      work(std::true_type{}, cur, row0, ls, slope2);
+  };
+  for (int i = 1 - kColRing; i < count; ++i) {
+    // tile i's loads are the oldest of those of up to kColRing - 1 tiles; the
+    // barrier also ends every wave's reads of the slot that the next fetch overwrites
+    if (i + kColRing - 2 < count)
+      wait_vmcnt<(kColRing - 2) * kLoads>();
+    else
+      wait_vmcnt<0>();
+    lds_barrier();
+    round(s_ring[(i + kColRing) % kColRing], s_ring[(i + 2 * kColRing - 1) % kColRing], i + kColRing - 1 < count,
+          i >= 0);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h)

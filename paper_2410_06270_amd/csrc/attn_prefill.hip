@@ -19,6 +19,8 @@
 // row's maximum and sum are in-lane but for one exchange between the half waves,
 // and the score rows are dealt so that the lane's keys are the ones that it
 // supplies to O^T = V^T P^T: the weights never leave their registers.
+#include <type_traits>
+
 #include "attn.hpp"
 
 namespace mc {
@@ -50,8 +52,20 @@ size_t attn_prefill_split_rows(int T, int Hq) {
   return all < most ? all : most;
 }
 
-// The other half wave's value of x: lanes l and l ^ 32 swap.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// The larger of x in lanes l and l ^ 32, and the sum of both.
+__device__ __forceinline__ float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The running maximum follows a larger score only when it is left behind by more
+// than this (log2): weights up to 2^8 lose nothing in fp32 sums or in bf16, and most
+// tiles need no scaling and no exchange between the half waves.
+constexpr float kMaxSlack = 8.0f;
 
 // Largest magnitude bits of the eight bf16 of w, by pairs (for the search for
 // infinities and NaN: those have all exponent bits set).
@@ -74,7 +88,7 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   constexpr int DT = D / 32, DK = D / 16;      // value tiles; score steps
   constexpr int kTileBytes = kPreKeys * D * 2, kBlk = kKvBlock * D * 2;      // in LDS: bf16
   constexpr int kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);                   // in the cache
-  __shared__ __attribute__((aligned(16))) char s_kv[2][2][kTileBytes];       // [buffer][k, v]
+  __shared__ __attribute__((aligned(16))) char s_kv[2][2 * kTileBytes];      // [buffer], keys then values
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % c.Hkv;
@@ -105,14 +119,18 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const bool wave_live = wrow < count * a.g;
   const int wpos_first = pos0 + wrow / a.g, wpos_last = pos0 + min(wrow + 31, count * a.g - 1) / a.g;
 
-  // queries: lane (row n, half) holds units half, half + 2, ... of its row
+  // queries: lane (row n, half) holds units half, half + 2, ... of its row (a row
+  // that is not live takes another's).  A negative scale turns their signs, so that
+  // the largest product is the largest score.
   bf16x8 qf[DK];
   {
     const uint16_t* qr = q.p + (size_t)(first + tok) * q.stride + (size_t)head * D + 8 * half;
+    const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
     for (int i = 0; i < DK; ++i) {
-      u32x4 r = {0u, 0u, 0u, 0u};
-      if (live) r = *reinterpret_cast<const u32x4*>(qr + 16 * i);
+      u32x4 r = *reinterpret_cast<const u32x4*>(qr + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] ^= sign;
       qf[i] = as_bf16x8(r);
     }
   }
@@ -133,33 +151,36 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each.
   constexpr int kPieces = kBlockBytes / 1024;
   u32x4 stage[E4 ? 2 * kPieces : 1];
-  auto fetch = [&](int t, int buf) {
-    const int blk = min((tile_key(t) >> 4) + wave, last_blk);
-    const int page = kv_page(c, __builtin_amdgcn_readfirstlane(pages[blk >> c.lb]));
-    const size_t off = kv_block_offset<kBlockBytes>(c, page, hk, blk) + 16 * lane;
+  // The page number comes a tile earlier: its load would otherwise hold up the
+  // tile's own.
+  auto tile_blk = [&](int t) { return min((tile_key(t) >> 4) + wave, last_blk); };
+  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(t, t_end - 1)) >> c.lb); };
+  auto fetch = [&](int t, char* to, int page) {
+    const size_t off = kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk,
+                                                    tile_blk(t)) + 16 * lane;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       if constexpr (E4) {
         stage[i] = *reinterpret_cast<const u32x4*>(c.k + off + 1024 * i);
         stage[kPieces + i] = *reinterpret_cast<const u32x4*>(c.v + off + 1024 * i);
       } else {
-        lds_dma16(c.k + off + 1024 * i, &s_kv[buf][0][wave * kBlk + 1024 * i]);
-        lds_dma16(c.v + off + 1024 * i, &s_kv[buf][1][wave * kBlk + 1024 * i]);
+        lds_dma16(c.k + off + 1024 * i, to + wave * kBlk + 1024 * i);
+        lds_dma16(c.v + off + 1024 * i, to + kTileBytes + wave * kBlk + 1024 * i);
       }
     }
   };
   // e4m3: the fetched units, widened to the bf16 units of the block.  Unit x of the
   // keys is (16 dimensions, token): two bf16 units, 256 bytes apart; of the values
   // (dimension, 16 tokens): D * 16 apart.
-  auto put = [&](int buf) {
+  auto put = [&](char* to) {
     if constexpr (E4) {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
         const int x = 64 * i + lane;
-        char* kd = &s_kv[buf][0][wave * kBlk + (x >> 4) * 512 + (x & 15) * 16];
+        char* kd = to + wave * kBlk + (x >> 4) * 512 + (x & 15) * 16;
         *reinterpret_cast<u32x4*>(kd) = e4m3_to_bf16(stage[i][0], stage[i][1]);
         *reinterpret_cast<u32x4*>(kd + 256) = e4m3_to_bf16(stage[i][2], stage[i][3]);
-        char* vd = &s_kv[buf][1][wave * kBlk + x * 16];
+        char* vd = to + kTileBytes + wave * kBlk + x * 16;
         *reinterpret_cast<u32x4*>(vd) = e4m3_to_bf16(stage[kPieces + i][0], stage[kPieces + i][1]);
         *reinterpret_cast<u32x4*>(vd + D * 16) = e4m3_to_bf16(stage[kPieces + i][2], stage[kPieces + i][3]);
       }
@@ -173,7 +194,7 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
   float m = kNegInf, l = 0.0f;       // l: of the lane's own keys
   const float kscale = E4 ? c.k_scale[hk] : 1.0f;
-  const ScoreConsts sc = {a.scale * kscale, a.scale * kscale * kLog2e, a.softcap,
+  const ScoreConsts sc = {fabsf(a.scale) * kscale, fabsf(a.scale) * kscale * kLog2e, a.softcap,
                           a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f};
   const float slope2 = EXTRA && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
   // keys of a score tile: row m of the tile is key (m with bits 2 and 3 swapped)
@@ -181,149 +202,171 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int koff = (krow >> 4) * kBlk + (krow & 15) * 16 + half * 256;
   const int voff = half * D * 16 + n * 16;
 
-  if (t_begin < t_end) {
-    fetch(t_begin, 0);
-    put(0);
-  }
-  for (int t = t_begin, buf = 0; t < t_end; ++t, buf ^= 1) {
-    // this tile is in LDS once every wave's loads are (the barrier also ends every
-    // wave's reads of the other buffer, which the next tile then overwrites)
-    if constexpr (!E4) wait_vmcnt<0>();
-    __syncthreads();
-    const int key0 = tile_key(t);
-    if (key0 + kPreKeys > len) {     // what lies behind the sequence may be anything: no value of it counts
-      for (int i = threadIdx.x; i < kTileBytes / 16; i += kPreThreads) {
-        // unit i of the value tile: block i / (2D), token group (i / D) % 2
-        const int k0 = key0 + 16 * (i / (2 * D)) + 8 * ((i / D) & 1);
-        if (k0 + 8 > len) {
-          u32x4 w = *reinterpret_cast<u32x4*>(&s_kv[buf][1][16 * i]);
+  // the row sees the keys below rpre and in (rlow, pos]
+  const int rlow = a.window > 0 && pos >= a.window ? pos - a.window : -1, rpre = pos >= 0 ? pre : 0;
+  // (j counted from the first of the tile's keys that the half wave takes)
+  struct Mask {
+    int pos, low, pre;
+  };
+  auto visible = [&](const Mask& k, int j) { return ((j <= k.pos) & (j > k.low)) | (j < k.pre); };
+  // The product with a tile of values some of which are not finite: those are left
+  // out of it and added, key by key, to the rows that see them (a weight is
+  // positive, so it changes neither an infinity nor a NaN).
+  auto add_odd = [&](const char* vs, const u32x4 (&p)[4], int key0) {
+    int h = half, vo = voff;
+    asm volatile("" : "+v"(h), "+v"(vo));              // nothing of this is computed ahead of the loop
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (k0 + 2 * e >= len) w[e] = 0u;
-            else if (k0 + 2 * e + 1 >= len) w[e] &= 0xffffu;
-          }
-          *reinterpret_cast<u32x4*>(&s_kv[buf][1][16 * i]) = w;
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(vs + vo + i * kBlk + 512 * d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = (v[e] & 0x7f80u) == 0x7f80u ? v[e] & 0xffff0000u : v[e];
+          v[e] = (v[e] & 0x7f800000u) == 0x7f800000u ? v[e] & 0xffffu : v[e];
+        }
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(p[i]), acc[d], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll 1
+    for (int e = 0; e < kPreKeys; ++e) {
+      const bool in = visible(Mask{pos - key0, rlow - key0, rpre - key0}, e);
+      // dimension 32 d + 8 (r / 4) + 4 half + r % 4 of key e
+      const char* vk = vs + (e >> 4) * kBlk + ((e >> 3) & 1) * D * 16 + 64 * h + 2 * (e & 7);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t w = *reinterpret_cast<const uint16_t*>(vk + 16 * (32 * d + 8 * (r >> 2) + (r & 3)));
+          acc[d][r] += in && (w & 0x7f80u) == 0x7f80u ? bf16_bits_to_float(w) : 0.0f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+
+  // One tile.  MASKED: some key is hidden from some row of the wave.
+  auto tile = [&](auto masked, const char* kv, int key0) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const char* ks = kv + koff;
+    const char* vs = kv + kTileBytes;
+    f32x16 sv[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sv[h][r] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DK; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const u32x4*>(ks + 2 * h * kBlk + 512 * i)), qf[i], sv[h], 0, 0, 0);
+    // score (h, 8 w + e) of the lane is of key key0 + 32 h + 16 w + 8 half + e
+    const int hkey = key0 + 8 * half;
+    const Mask mask = {pos - hkey, rlow - hkey, rpre - hkey};
+    float x[32];
+    float mx = kNegInf;
+    if (MASKED || EXTRA) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int j = 32 * (e >> 4) + 16 * ((e >> 3) & 1) + (e & 7);
+        x[e] = score2<EXTRA>(sv[e >> 4][e & 15], sc, slope2, j - mask.pos);
+        if (MASKED) x[e] = visible(mask, j) ? x[e] : kNegInf;
+        mx = fmaxf(mx, x[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
+      mx *= sc.scale2;
+    }
+    if (__any(mx > m + kMaxSlack)) {
+      const float m_new = fmaxf(m, halves_max(mx));
+      const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
+      m = m_new;
+    }
+    const float m0 = m == kNegInf ? 0.0f : m;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      x[e] = exp2_fast(MASKED || EXTRA ? x[e] - m0 : __builtin_fmaf(sv[e >> 4][e & 15], sc.scale2, -m0));
+      l += x[e];
+    }
+    if (MASKED) asm volatile("" : "+v"(l));     // summed here: the weights' registers are needed below
+    u32x4 p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[i][e] = bf16_pair(x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
+    if (MASKED) {
+      // a value that is not finite must not reach the rows that do not see it
+      u16x2 most = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i)
+        most = magnitude_max(most, *reinterpret_cast<const u32x4*>(vs + voff + (i / DT) * kBlk + (i % DT) * 512));
+      asm volatile("" : : : "memory");     // the tile is read again: its registers are needed elsewhere
+      if (__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) {
+        add_odd(vs, p, key0);
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const u32x4*>(vs + voff + i * kBlk + 512 * d)), as_bf16x8(p[i]), acc[d], 0, 0, 0);
+  };
+
+  // Round t: the loads of tile t + 1, then tile t.  The buffers are distinct and
+  // passed as such: reads of one do not wait for the loads into the other.
+  int page = t_begin < t_end ? page_of(t_begin) : 0;     // of tile t + 1
+  auto round = [&](char* __restrict__ cur, char* __restrict__ nxt, int t) {
+    const int key0 = tile_key(t);
+    if (t >= t_begin && key0 + kPreKeys > len) {
+      // what lies behind the sequence may be anything: no value of it counts
+      int i = threadIdx.x;
+      asm volatile("" : "+v"(i));
+#pragma unroll 1
+      for (; i < kTileBytes / 16; i += kPreThreads) {
+        // unit i of the value tile: block i / (2D), token group (i / D) % 2
+        const int over = key0 + 16 * (i / (2 * D)) + 8 * ((i / D) & 1) + 8 - len;   // hidden tokens of the unit
+        if (over > 0) {
+          u32x4 w = *reinterpret_cast<u32x4*>(cur + kTileBytes + 16 * i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = over >= 8 - 2 * e ? 0u : over == 7 - 2 * e ? w[e] & 0xffffu : w[e];
+          *reinterpret_cast<u32x4*>(cur + kTileBytes + 16 * i) = w;
         }
       }
-      __syncthreads();
+      lds_barrier();
     }
-    if (t + 1 < t_end) fetch(t + 1, buf ^ 1);
-    const bool none = key0 > wpos_last && key0 >= pre;
-    if (wave_live && !none) {
-      const char* ks = s_kv[buf][0];
-      const char* vs = s_kv[buf][1];
-      f32x16 sv[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sv[h][r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < DK; ++i)
-          sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              as_bf16x8(*reinterpret_cast<const u32x4*>(ks + koff + 2 * h * kBlk + 512 * i)), qf[i], sv[h], 0, 0, 0);
-      }
-      // score (h, 8 w + e) of the lane is of key key0 + 32 h + 16 w + 8 half + e
+    if (t + 1 < t_end) {
+      const int next = page_of(t + 2);
+      fetch(t + 1, nxt, page);
+      page = next;
+    }
+    if (t >= t_begin && wave_live && (key0 <= wpos_last || key0 < pre)) {
       const bool whole = (wpos_first >= 0 && key0 + kPreKeys <= pre) ||
                          (key0 + kPreKeys - 1 <= wpos_first && (a.window == 0 || key0 > wpos_last - a.window));
-      float x[32];
-      uint32_t seen = 0;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const int j = key0 + 32 * (e >> 4) + 16 * ((e >> 3) & 1) + 8 * half + (e & 7);
-        x[e] = score2<EXTRA>(sv[e >> 4][e & 15], sc, slope2, j - pos);
-        if (!whole) {
-          const bool in = (j <= pos && (a.window == 0 || j > pos - a.window)) || (pos >= 0 && j < pre);
-          x[e] = in ? x[e] : kNegInf;
-          seen |= in ? 1u << e : 0u;
-        }
-      }
-      float mx = x[0];
-#pragma unroll
-      for (int e = 1; e < 32; ++e) mx = fmaxf(mx, x[e]);
-      mx = fmaxf(mx, other_half(mx));
-      const float m_new = fmaxf(m, mx);
-      if (__any(m_new > m)) {
-        const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
-        l *= alpha;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
-        m = m_new;
-      }
-      const float m0 = m == kNegInf ? 0.0f : m;
-#pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        x[e] = exp2_fast(x[e] - m0);
-        l += x[e];
-      }
-      bool odd = false;
-      if (!whole) {
-        // a value that is not finite must not reach the rows that do not see it
-        u16x2 most = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 4 * DT; ++i)
-          most = magnitude_max(most, *reinterpret_cast<const u32x4*>(vs + (i / DT) * kBlk + voff + (i % DT) * 512));
-        odd = __any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4 pr;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pr[e] = bf16_pair(x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
-        const bf16x8 p = as_bf16x8(pr);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          u32x4 v = *reinterpret_cast<const u32x4*>(vs + i * kBlk + voff + 512 * d);
-          if (odd) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
-              if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
-            }
-          }
-          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), p, acc[d], 0, 0, 0);
-        }
-      }
-      if (odd) {
-        // the values left out above, to the rows that see them: products of the
-        // places of one kind of value (infinity, its negative, NaN) with the rows'
-        // visible keys; where one counts any, the value is added
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {
-          const float add = kind == 0 ? -kNegInf : kind == 1 ? kNegInf : __builtin_nanf("");
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            f32x16 found;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) found[r] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              __builtin_amdgcn_sched_barrier(0);     // one at a time: registers, not speed
-              const u32x4 v = *reinterpret_cast<const u32x4*>(vs + i * kBlk + voff + 512 * d);
-              u32x4 at, vis;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                auto is = [&](uint32_t w) {
-                  return kind == 0 ? w == 0x7f80u : kind == 1 ? w == 0xff80u : (w & 0x7fffu) > 0x7f80u;
-                };
-                at[e] = (is(v[e] & 0xffffu) ? 0x3f80u : 0u) | (is(v[e] >> 16) ? 0x3f800000u : 0u);
-                vis[e] = ((seen >> (8 * i + 2 * e)) & 1u ? 0x3f80u : 0u) |
-                         ((seen >> (8 * i + 2 * e + 1)) & 1u ? 0x3f800000u : 0u);
-              }
-              found = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(at), as_bf16x8(vis), found, 0, 0, 0);
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (found[r] > 0.0f) acc[d][r] += add;
-          }
-        }
-      }
+      if (whole)
+        tile(std::false_type{}, cur, key0);
+      else
+        tile(std::true_type{}, cur, key0);
     }
-    if (E4 && t + 1 < t_end) put(buf ^ 1);
+    if (E4 && t + 1 < t_end) put(nxt);
+  };
+  for (int t = t_begin - 1; t < t_end; ++t) {
+    // tile t is in LDS once every wave's loads are; the barrier also ends every
+    // wave's reads of the other buffer
+    if constexpr (!E4) wait_vmcnt<0>();
+    lds_barrier();
+    round(s_kv[t & 1], s_kv[(t + 1) & 1], t);
   }
 
-  l += other_half(l);
+  l = halves_sum(l);
   if (!live) return;
   const float m0 = m == kNegInf ? 0.0f : m;
   const size_t out_row = (size_t)(first + tok);

@@ -101,6 +101,12 @@ __device__ __forceinline__ void lds_dma16(const void* src, void* dst) {
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
+// The same with 4 bytes a lane, to dst + 4*l.
+__device__ __forceinline__ void lds_dma4(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+}
+
 // ------------------------------------------------------------------ layout --
 // Lane l of a 16x128 tile holds, for MFMA step u (32 columns) and register v
 // (0..3), the codes of columns 32u + 8*(l/16) + 2v (low half) and +1 (high
