@@ -164,25 +164,29 @@ __device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// cap * tanh(x / cap) = cap * (1 - t) / (1 + t), t = exp(-2 |x| / cap), with x's
-// sign; off by 2^-23 cap at most, an fp32 rounding of a score near the cap.
-__device__ __forceinline__ float cap_score(float x, float cap, float inv_cap) {
-  const float t = exp2_fast(-2.0f * kLog2e * inv_cap * fabsf(x));
-  return copysignf(cap * (1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), x);
-}
-
-// A score in the log2 domain from the plain product q.k.  EXTRA: softcap
-// and / or slopes; scale2 = scale * log2(e), dist = j - i.
+// A score in the log2 domain from the plain product q.k.  cap tanh(x / cap) =
+// cap - 2 cap u with u = 1 / (1 + exp(2 x / cap)): off by some 2^-23 cap, an fp32
+// rounding of a score near the cap.
 struct ScoreConsts {
-  float scale, scale2, cap, inv_cap;
+  float scale2;          // scale * log2(e)
+  float cap2, cap_in;    // softcap * log2(e); 2 log2(e) scale / softcap
 };
 
-template <bool EXTRA>
+__device__ __forceinline__ ScoreConsts score_consts(float scale, float softcap) {
+  return {scale * kLog2e, softcap * kLog2e, softcap > 0.0f ? 2.0f * kLog2e * (scale / softcap) : 0.0f};
+}
+
+__device__ __forceinline__ float cap_unit(float qk, const ScoreConsts& c) {
+  return __builtin_amdgcn_rcpf(1.0f + exp2_fast(qk * c.cap_in));
+}
+
+// MODE: 0 plain, 1 capped, 2 slopes (capped or not); dist = j - i.
+template <int MODE>
 __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float slope2, int dist) {
-  if (!EXTRA) return qk * c.scale2;
+  if (MODE == 0) return qk * c.scale2;
   float s = qk * c.scale2;
-  if (c.cap > 0.0f) s = cap_score(qk * c.scale, c.cap, c.inv_cap) * kLog2e;
-  return s + slope2 * (float)dist;
+  if (MODE == 1 || c.cap2 > 0.0f) s = __builtin_fmaf(-2.0f * c.cap2, cap_unit(qk, c), c.cap2);
+  return MODE == 1 ? s : s + slope2 * (float)dist;
 }
 
 // Joins the parts of every (row, head); ragged: rows outside its sequences are

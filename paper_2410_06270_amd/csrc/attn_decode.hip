@@ -48,7 +48,7 @@ struct DecodeStep {
   u32x4 k[kTiles][kChunks], v[D / 16];
 };
 
-template <int D, bool E4, bool EXTRA>
+template <int D, bool E4, int MODE>
 __global__ void __launch_bounds__(kDecThreads, 2)
     attn_decode_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                        int head_tiles) {
@@ -118,9 +118,8 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = kNegInf, l = 0.0f;       // l: of the lane's own keys
   const float kscale = E4 ? c.k_scale[hk] : 1.0f;
-  const ScoreConsts sc = {a.scale * kscale, a.scale * kscale * kLog2e, a.softcap,
-                          a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f};
-  const float slope2 = EXTRA && a.slopes && n < heads ? a.slopes[head0 + n] * kLog2e : 0.0f;
+  const ScoreConsts sc = score_consts(a.scale * kscale, a.softcap);
+  const float slope2 = MODE == 2 && a.slopes && n < heads ? a.slopes[head0 + n] * kLog2e : 0.0f;
 
   auto compute = [&](Step& st, int i) {
     const int key0 = step_blk(i) << 4;
@@ -144,7 +143,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
     const int lane_key = key0 + 4 * KT * quarter;
     float x[4 * KT];
 #pragma unroll
-    for (int e = 0; e < 4 * KT; ++e) x[e] = score2<EXTRA>(sv[e / 4][e % 4], sc, slope2, lane_key + e - pos);
+    for (int e = 0; e < 4 * KT; ++e) x[e] = score2<MODE>(sv[e / 4][e % 4], sc, slope2, lane_key + e - pos);
     const bool whole = (key0 >= wstart && key0 + KS <= len) || key0 + KS <= pre;
     if (!whole) {
       // keys out of sight: weight 0, and values 0 whatever the cache holds there
@@ -396,11 +395,14 @@ template <int D, bool E4>
 static void decode_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                           const SplitArgs& sp, int head_tiles, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)b.S * c.Hkv * head_tiles * sp.nsplit));
-  if (a.softcap > 0.0f || a.slopes)
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, true>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
+  if (a.slopes)
+    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 2>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
+                       head_tiles);
+  else if (a.softcap > 0.0f)
+    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 1>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
                        head_tiles);
   else
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, false>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
+    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 0>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
                        head_tiles);
 }
 

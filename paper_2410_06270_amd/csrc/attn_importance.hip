@@ -60,7 +60,7 @@ size_t attn_importance_bytes(int Hq, int L) {
 // products a fraction of one.
 constexpr int kColRing = 4;
 
-template <int D, bool E4, bool EXTRA>
+template <int D, bool E4, int MODE>
 __global__ void __launch_bounds__(kColThreads, 2)
     attn_colsum_kernel(RowsIn q, const float* __restrict__ lse, BatchArgs b, KvArgs c, ScoreArgs a, int L, int slices,
                        float* __restrict__ partial) {
@@ -104,8 +104,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[h][r] = 0.0f;
   const float kscale = E4 ? c.k_scale[hk] : 1.0f;
-  const ScoreConsts sc = {a.scale * kscale, a.scale * kscale * kLog2e, a.softcap,
-                          a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f};
+  const ScoreConsts sc = score_consts(a.scale * kscale, a.softcap);
 
   // (row tile, head of the group) pairs, from the diagonal down: pair y is head
   // y % g of row tile t0 + y / g; this workgroup takes slice, slice + slices, ...
@@ -161,8 +160,8 @@ __global__ void __launch_bounds__(kColThreads, 2)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = key0 + 32 * h + 8 * (r >> 2) + 4 * half + (r & 3);
-        float p = exp2_fast(EXTRA ? score2<EXTRA>(sv[h][r], sc, slope2, j - row) - ls
-                                  : __builtin_fmaf(sv[h][r], sc.scale2, -ls));
+        float p = exp2_fast(MODE ? score2<MODE>(sv[h][r], sc, slope2, j - row) - ls
+                                 : __builtin_fmaf(sv[h][r], sc.scale2, -ls));
         if (MASKED) p = ((j <= high) & (j > low)) ? p : 0.0f;
         acc[h][r] += p;
       }
@@ -175,7 +174,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
     if (more) fetch(nxt);
     if (!ready) return;
     const int row0 = 32 * ct;
-    const float slope2 = EXTRA && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
+    const float slope2 = MODE == 2 && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
     next(ct, ch);
     if (row0 + 31 < key0) return;                        // above the wave's diagonal
     const float v = *reinterpret_cast<const float*>(cur + kRowBytes + 256 * wave + 4 * lane);
@@ -254,12 +253,15 @@ template <int D, bool E4>
 static void colsum_launch(RowsIn q, const float* lse, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, int L,
                           int slices, float* partial, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)col_tiles(L) * slices * c.Hkv));
-  if (a.softcap > 0.0f || a.slopes)
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, true>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L,
-                       slices, partial);
+  if (a.slopes)
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 2>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
+                       partial);
+  else if (a.softcap > 0.0f)
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 1>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
+                       partial);
   else
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, false>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L,
-                       slices, partial);
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 0>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
+                       partial);
 }
 
 hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const BatchArgs& b, const KvArgs& c,

@@ -67,28 +67,64 @@ __device__ __forceinline__ float halves_sum(float x) {
 // tiles need no scaling and no exchange between the half waves.
 constexpr float kMaxSlack = 8.0f;
 
-// Largest magnitude bits of the eight bf16 of w, by pairs (for the search for
-// infinities and NaN: those have all exponent bits set).
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ u16x2 magnitude_max(u16x2 acc, const u32x4& w) {
+// A tile of values that some row does not see whole.  Those behind its first n
+// keys may be anything and become 0; so do infinities and NaN, which a weight of 0
+// would not keep from the rows that do not see them.  Returns whether the thread met
+// any of those (they are added to the rows that see them at the end).
+template <int D>
+__device__ __forceinline__ bool clean_values(char* vt, int n) {
+  uint32_t odd = 0;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < kPreKeys * D / 8; i += kPreThreads) {
+    // unit i of the tile: block i / (2D), token group (i / D) % 2
+    const int over = 16 * (i / (2 * D)) + 8 * ((i / D) & 1) + 8 - n;      // hidden tokens of the unit
+    u32x4 w = *reinterpret_cast<u32x4*>(vt + 16 * i);
+    bool change = over > 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t t = w[i] & 0x7fff7fffu;
-    u16x2 h;
-    __builtin_memcpy(&h, &t, 4);
-    acc = __builtin_elementwise_max(acc, h);
+    for (int e = 0; e < 4; ++e) {
+      w[e] = over >= 8 - 2 * e ? 0u : over == 7 - 2 * e ? w[e] & 0xffffu : w[e];
+      const uint32_t lo = (w[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+      const uint32_t hi = (w[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+      odd |= lo | hi;
+      change = change || (lo | hi);
+      w[e] &= ~(lo | hi);
+    }
+    if (change) *reinterpret_cast<u32x4*>(vt + 16 * i) = w;
   }
-  return acc;
+  return odd != 0;
 }
 
-template <int D, bool E4, bool EXTRA>
+// The order of a round's instructions: LDS reads kReadAhead matrix instructions
+// before their use, and between the matrix instructions of the scores the vector work on
+// the other tile.
+constexpr int kReadAhead = 5;
+
+template <int DK, int DT>
+__device__ __forceinline__ void interleave() {
+  constexpr int kMfmas = 2 * DK + 4 * DT;
+  __builtin_amdgcn_sched_group_barrier(0x100, kReadAhead, 0);      // LDS reads
+#pragma unroll
+  for (int i = 0; i < kMfmas; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);             // matrix
+    if (i + kReadAhead < kMfmas) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    if (i < 2 * DK) __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * DK), 0);
+  }
+}
+
+// MODE: 0 plain scores, 1 capped ones, 2 slopes (capped or not).
+template <int D, bool E4, int MODE>
 __global__ void __launch_bounds__(kPreThreads, 2)
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                         int slots) {
   constexpr int DT = D / 32, DK = D / 16;      // value tiles; score steps
   constexpr int kTileBytes = kPreKeys * D * 2, kBlk = kKvBlock * D * 2;      // in LDS: bf16
   constexpr int kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);                   // in the cache
-  __shared__ __attribute__((aligned(16))) char s_kv[2][2 * kTileBytes];      // [buffer], keys then values
+  constexpr int kPieces = kBlockBytes / 1024, kUnit = E4 ? 16 : 8;
+  // one array: for several the compiler keeps marks of its own that replace those
+  // of the parameters of round() below, and then waits for every load before a read
+  __shared__ __attribute__((aligned(16))) char s_lds[4 * kTileBytes + (E4 ? kPreWaves * 2 * kBlockBytes : 0)];
+  char* const s_k[2] = {s_lds, s_lds + kTileBytes};
+  char* const s_v[2] = {s_lds + 2 * kTileBytes, s_lds + 3 * kTileBytes};
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % c.Hkv;
@@ -98,8 +134,8 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int s = find_sequence(b.q_start, b.S, slot, kPreRows, 1, a.g);
   int first, count;
   sequence_rows(b, s, first, count);
-  const long long base64 = (long long)b.q_start[s] * a.g / kPreRows + s;
-  const long long row0l = (slot - base64) * kPreRows;
+  const long long slot0 = (long long)b.q_start[s] * a.g / kPreRows + s;
+  const long long row0l = (slot - slot0) * kPreRows;
   if (row0l < 0 || row0l >= (long long)count * a.g) return;
   const int row0 = (int)row0l;
 
@@ -148,42 +184,26 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int last_blk = len > 0 ? (len - 1) >> 4 : 0;
   auto tile_key = [&](int t) { return (t < ia ? t : t - ia + ib) * kPreKeys; };
 
-  // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each.
-  constexpr int kPieces = kBlockBytes / 1024;
-  u32x4 stage[E4 ? 2 * kPieces : 1];
-  // The page number comes a tile earlier: its load would otherwise hold up the
-  // tile's own.
+  // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each.  A
+  // page number comes a round before the loads that it is for.
   auto tile_blk = [&](int t) { return min((tile_key(t) >> 4) + wave, last_blk); };
-  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(t, t_end - 1)) >> c.lb); };
-  auto fetch = [&](int t, char* to, int page) {
-    const size_t off = kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk,
-                                                    tile_blk(t)) + 16 * lane;
+  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(max(t, t_begin), t_end - 1)) >> c.lb); };
+  auto fetch = [&](const char* from, int t, int page, char* to) {
+    const char* src = from + kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk, tile_blk(t)) + 16 * lane;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) lds_dma16(src + 1024 * i, to + 1024 * i);
+  };
+  // e4m3: a fetched block's units, widened to bf16 units.  Unit x of the keys is
+  // (16 dimensions, token): two bf16 units, 256 bytes apart; of the values (dimension,
+  // 16 tokens): D * 16 apart.
+  auto widen = [&](const char* raw, bool keys, char* to) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      if constexpr (E4) {
-        stage[i] = *reinterpret_cast<const u32x4*>(c.k + off + 1024 * i);
-        stage[kPieces + i] = *reinterpret_cast<const u32x4*>(c.v + off + 1024 * i);
-      } else {
-        lds_dma16(c.k + off + 1024 * i, to + wave * kBlk + 1024 * i);
-        lds_dma16(c.v + off + 1024 * i, to + kTileBytes + wave * kBlk + 1024 * i);
-      }
-    }
-  };
-  // e4m3: the fetched units, widened to the bf16 units of the block.  Unit x of the
-  // keys is (16 dimensions, token): two bf16 units, 256 bytes apart; of the values
-  // (dimension, 16 tokens): D * 16 apart.
-  auto put = [&](char* to) {
-    if constexpr (E4) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int x = 64 * i + lane;
-        char* kd = to + wave * kBlk + (x >> 4) * 512 + (x & 15) * 16;
-        *reinterpret_cast<u32x4*>(kd) = e4m3_to_bf16(stage[i][0], stage[i][1]);
-        *reinterpret_cast<u32x4*>(kd + 256) = e4m3_to_bf16(stage[i][2], stage[i][3]);
-        char* vd = to + kTileBytes + wave * kBlk + x * 16;
-        *reinterpret_cast<u32x4*>(vd) = e4m3_to_bf16(stage[kPieces + i][0], stage[kPieces + i][1]);
-        *reinterpret_cast<u32x4*>(vd + D * 16) = e4m3_to_bf16(stage[kPieces + i][2], stage[kPieces + i][3]);
-      }
+      const u32x4 w = *reinterpret_cast<const u32x4*>(raw + 1024 * i + 16 * lane);
+      const int x = 64 * i + lane;
+      char* d = to + (keys ? (x >> 4) * 512 + (x & 15) * 16 : x * 16);
+      *reinterpret_cast<u32x4*>(d) = e4m3_to_bf16(w[0], w[1]);
+      *reinterpret_cast<u32x4*>(d + (keys ? 256 : D * 16)) = e4m3_to_bf16(w[2], w[3]);
     }
   };
 
@@ -193,10 +213,9 @@ __global__ void __launch_bounds__(kPreThreads, 2)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
   float m = kNegInf, l = 0.0f;       // l: of the lane's own keys
-  const float kscale = E4 ? c.k_scale[hk] : 1.0f;
-  const ScoreConsts sc = {fabsf(a.scale) * kscale, fabsf(a.scale) * kscale * kLog2e, a.softcap,
-                          a.softcap > 0.0f ? 1.0f / a.softcap : 0.0f};
-  const float slope2 = EXTRA && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+  const float kscale = E4 ? c.k_scale[hk] : 1.0f, scale = fabsf(a.scale) * kscale;
+  const ScoreConsts sc = score_consts(scale, a.softcap);
+  const float slope2 = MODE == 2 && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
   // keys of a score tile: row m of the tile is key (m with bits 2 and 3 swapped)
   const int krow = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);
   const int koff = (krow >> 4) * kBlk + (krow & 15) * 16 + half * 256;
@@ -209,48 +228,9 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     int pos, low, pre;
   };
   auto visible = [&](const Mask& k, int j) { return ((j <= k.pos) & (j > k.low)) | (j < k.pre); };
-  // The product with a tile of values some of which are not finite: those are left
-  // out of it and added, key by key, to the rows that see them (a weight is
-  // positive, so it changes neither an infinity nor a NaN).
-  auto add_odd = [&](const char* vs, const u32x4 (&p)[4], int key0) {
-    int h = half, vo = voff;
-    asm volatile("" : "+v"(h), "+v"(vo));              // nothing of this is computed ahead of the loop
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        u32x4 v = *reinterpret_cast<const u32x4*>(vs + vo + i * kBlk + 512 * d);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = (v[e] & 0x7f80u) == 0x7f80u ? v[e] & 0xffff0000u : v[e];
-          v[e] = (v[e] & 0x7f800000u) == 0x7f800000u ? v[e] & 0xffffu : v[e];
-        }
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(p[i]), acc[d], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll 1
-    for (int e = 0; e < kPreKeys; ++e) {
-      const bool in = visible(Mask{pos - key0, rlow - key0, rpre - key0}, e);
-      // dimension 32 d + 8 (r / 4) + 4 half + r % 4 of key e
-      const char* vk = vs + (e >> 4) * kBlk + ((e >> 3) & 1) * D * 16 + 64 * h + 2 * (e & 7);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const uint32_t w = *reinterpret_cast<const uint16_t*>(vk + 16 * (32 * d + 8 * (r >> 2) + (r & 3)));
-          acc[d][r] += in && (w & 0x7f80u) == 0x7f80u ? bf16_bits_to_float(w) : 0.0f;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  };
 
-  // One tile.  MASKED: some key is hidden from some row of the wave.
-  auto tile = [&](auto masked, const char* kv, int key0) {
-    constexpr bool MASKED = decltype(masked)::value;
-    const char* ks = kv + koff;
-    const char* vs = kv + kTileBytes;
-    f32x16 sv[2];
+  // Scores of a tile: (h, 8 w + e) of the lane is of key 32 h + 16 w + 8 half + e.
+  auto qk = [&](const char* kt, f32x16 (&sv)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -260,25 +240,59 @@ __global__ void __launch_bounds__(kPreThreads, 2)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const u32x4*>(ks + 2 * h * kBlk + 512 * i)), qf[i], sv[h], 0, 0, 0);
-    // score (h, 8 w + e) of the lane is of key key0 + 32 h + 16 w + 8 half + e
-    const int hkey = key0 + 8 * half;
-    const Mask mask = {pos - hkey, rlow - hkey, rpre - hkey};
-    float x[32];
+            as_bf16x8(*reinterpret_cast<const u32x4*>(kt + koff + 2 * h * kBlk + 512 * i)), qf[i], sv[h], 0, 0, 0);
+  };
+  // Weights of a tile, from plain products (mul: the scale) or scores (mul: 1).
+  auto weigh = [&](const f32x16 (&sv)[2], float mul, u32x4 (&p)[4]) {
+    const float m0 = m == kNegInf ? 0.0f : m;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        x[e] = exp2_fast(__builtin_fmaf(sv[i >> 3][(2 * i + e) & 15], mul, -m0));
+        sum[e] += x[e];
+      }
+      p[i >> 2][i & 3] = bf16_pair(x[0], x[1]);
+    }
+    l += sum[0] + sum[1];
+  };
+  auto pv = [&](const char* vt, const u32x4 (&p)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const u32x4*>(vt + voff + i * kBlk + 512 * d)), as_bf16x8(p[i]), acc[d], 0, 0,
+            0);
+  };
+  // A tile's scores in place of its products, where it is masked or the score is not
+  // a multiple of the product, and the running maximum.  Returns what weigh multiplies by.
+  auto settle = [&](f32x16 (&sv)[2], int key0) {
+    const bool masked = !((wpos_first >= 0 && key0 + kPreKeys <= pre) ||
+                          (key0 + kPreKeys - 1 <= wpos_first && (a.window == 0 || key0 > wpos_last - a.window)));
     float mx = kNegInf;
-    if (MASKED || EXTRA) {
+    if (masked || MODE) {
+      const int hkey = key0 + 8 * half;
+      const Mask k = {pos - hkey, rlow - hkey, rpre - hkey};
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         const int j = 32 * (e >> 4) + 16 * ((e >> 3) & 1) + (e & 7);
-        x[e] = score2<EXTRA>(sv[e >> 4][e & 15], sc, slope2, j - mask.pos);
-        if (MASKED) x[e] = visible(mask, j) ? x[e] : kNegInf;
-        mx = fmaxf(mx, x[e]);
+        sv[e >> 4][e & 15] = score2<MODE>(sv[e >> 4][e & 15], sc, slope2, j - k.pos);
       }
-    } else {
+      if (masked) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
-      mx *= sc.scale2;
+        for (int e = 0; e < 32; ++e) {
+          const int j = 32 * (e >> 4) + 16 * ((e >> 3) & 1) + (e & 7);
+          sv[e >> 4][e & 15] = visible(k, j) ? sv[e >> 4][e & 15] : kNegInf;
+        }
+      }
     }
+#pragma unroll
+    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
+    const float mul = masked || MODE ? 1.0f : sc.scale2;
+    mx *= mul;
     if (__any(mx > m + kMaxSlack)) {
       const float m_new = fmaxf(m, halves_max(mx));
       const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
@@ -289,81 +303,131 @@ __global__ void __launch_bounds__(kPreThreads, 2)
         for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
       m = m_new;
     }
-    const float m0 = m == kNegInf ? 0.0f : m;
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      x[e] = exp2_fast(MASKED || EXTRA ? x[e] - m0 : __builtin_fmaf(sv[e >> 4][e & 15], sc.scale2, -m0));
-      l += x[e];
-    }
-    if (MASKED) asm volatile("" : "+v"(l));     // summed here: the weights' registers are needed below
-    u32x4 p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[i][e] = bf16_pair(x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
-    if (MASKED) {
-      // a value that is not finite must not reach the rows that do not see it
-      u16x2 most = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 4 * DT; ++i)
-        most = magnitude_max(most, *reinterpret_cast<const u32x4*>(vs + voff + (i / DT) * kBlk + (i % DT) * 512));
-      asm volatile("" : : : "memory");     // the tile is read again: its registers are needed elsewhere
-      if (__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) {
-        add_odd(vs, p, key0);
-        return;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const u32x4*>(vs + voff + i * kBlk + 512 * d)), as_bf16x8(p[i]), acc[d], 0, 0, 0);
+    return mul;
+  };
+  // a tile with a key that some row of the workgroup does not see
+  auto edge = [&](int key0) {
+    return !((pos_first >= 0 && key0 + kPreKeys <= pre) ||
+             (key0 + kPreKeys - 1 <= pos_first && (a.window == 0 || key0 > pos_last - a.window)));
   };
 
-  // Round t: the loads of tile t + 1, then tile t.  The buffers are distinct and
-  // passed as such: reads of one do not wait for the loads into the other.
-  int page = t_begin < t_end ? page_of(t_begin) : 0;     // of tile t + 1
-  auto round = [&](char* __restrict__ cur, char* __restrict__ nxt, int t) {
-    const int key0 = tile_key(t);
-    if (t >= t_begin && key0 + kPreKeys > len) {
-      // what lies behind the sequence may be anything: no value of it counts
-      int i = threadIdx.x;
-      asm volatile("" : "+v"(i));
-#pragma unroll 1
-      for (; i < kTileBytes / 16; i += kPreThreads) {
-        // unit i of the value tile: block i / (2D), token group (i / D) % 2
-        const int over = key0 + 16 * (i / (2 * D)) + 8 * ((i / D) & 1) + 8 - len;   // hidden tokens of the unit
-        if (over > 0) {
-          u32x4 w = *reinterpret_cast<u32x4*>(cur + kTileBytes + 16 * i);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = over >= 8 - 2 * e ? 0u : over == 7 - 2 * e ? w[e] & 0xffffu : w[e];
-          *reinterpret_cast<u32x4*>(cur + kTileBytes + 16 * i) = w;
-        }
-      }
-      lds_barrier();
-    }
-    if (t + 1 < t_end) {
-      const int next = page_of(t + 2);
-      fetch(t + 1, nxt, page);
-      page = next;
-    }
-    if (t >= t_begin && wave_live && (key0 <= wpos_last || key0 < pre)) {
-      const bool whole = (wpos_first >= 0 && key0 + kPreKeys <= pre) ||
-                         (key0 + kPreKeys - 1 <= wpos_first && (a.window == 0 || key0 > wpos_last - a.window));
-      if (whole)
-        tile(std::false_type{}, cur, key0);
-      else
-        tile(std::true_type{}, cur, key0);
-    }
-    if (E4 && t + 1 < t_end) put(nxt);
+  // Round t: the scores of tile t + 1 beside the weights of tile t, whose values
+  // then are added up: the matrix units work on one tile while the vector units
+  // work on the other.  Loads: keys of tile t + 2 and values of t + 1 (e4m3: of one
+  // more, those of this round being widened).  The buffers are distinct and passed as
+  // such: reads of one do not wait for the loads into another.
+  int page_k = 0, page_v = 0;                          // of the next round's loads
+  float mul = 1.0f;
+  bool odd = false;
+  char* raw_k = s_lds + 4 * kTileBytes + wave * 2 * kBlockBytes;      // e4m3 only
+  char* raw_v = raw_k + (E4 ? kBlockBytes : 0);
+  auto load_k = [&](int t, char* kt) {
+    if (t < t_end) fetch(c.k, t, page_k, E4 ? raw_k : kt + wave * kBlk);
+    page_k = page_of(t + 1);
   };
-  for (int t = t_begin - 1; t < t_end; ++t) {
-    // tile t is in LDS once every wave's loads are; the barrier also ends every
-    // wave's reads of the other buffer
+  auto load_v = [&](int t, char* vt) {
+    if (t < t_end) fetch(c.v, t, page_v, E4 ? raw_v : vt + wave * kBlk);
+    page_v = page_of(t + 1);
+  };
+  auto lds_done = [&]() {                              // what was read may be overwritten
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
+    asm volatile("" ::: "memory");
+  };
+  auto round = [&](const char* __restrict__ kt, const char* __restrict__ vt, char* __restrict__ knext,
+                   char* __restrict__ vnext, f32x16 (&cur)[2], f32x16 (&nxt)[2], int t) {
+    if constexpr (E4) {
+      if (t + 2 < t_end) widen(raw_k, true, knext + wave * kBlk);
+      if (t + 1 < t_end) widen(raw_v, false, vnext + wave * kBlk);
+      lds_done();
+      load_k(t + 3, knext);
+      load_v(t + 2, vnext);
+    } else {
+      load_k(t + 2, knext);
+      load_v(t + 1, vnext);
+    }
+    if (!wave_live) return;
+    // (the last round's next tile is whatever its buffer holds, and not used)
+    u32x4 p[4];
+    qk(kt, nxt);
+    weigh(cur, mul, p);
+    pv(vt, p);
+    interleave<DK, DT>();
+    if (t + 1 < t_end) mul = settle(nxt, tile_key(t + 1));
+  };
+  // what the last round loaded is in LDS once every wave's loads are; the barrier
+  // also ends every wave's reads of the buffers that this round fills
+  auto begin_round = [&](char* vt, int t) {
     if constexpr (!E4) wait_vmcnt<0>();
     lds_barrier();
-    round(s_kv[t & 1], s_kv[(t + 1) & 1], t);
+    if constexpr (E4) wait_vmcnt<0>();
+    if (edge(tile_key(t))) {
+      odd = clean_values<D>(vt, len - tile_key(t)) || odd;
+      lds_barrier();
+    }
+  };
+  if (t_begin < t_end) {
+    f32x16 sa[2], sb[2];
+    page_k = page_of(t_begin);
+    page_v = page_k;
+    load_k(t_begin, s_k[0]);
+    if constexpr (E4) {
+      wait_vmcnt<0>();
+      widen(raw_k, true, s_k[0] + wave * kBlk);
+      lds_done();
+    }
+    load_k(t_begin + 1, s_k[1]);
+    load_v(t_begin, s_v[0]);
+    if constexpr (E4) {
+      wait_vmcnt<0>();
+      if (t_begin + 1 < t_end) widen(raw_k, true, s_k[1] + wave * kBlk);
+      widen(raw_v, false, s_v[0] + wave * kBlk);
+      lds_done();
+      load_k(t_begin + 2, s_k[0]);
+      load_v(t_begin + 1, s_v[1]);
+    } else {
+      wait_vmcnt<0>();
+    }
+    lds_barrier();
+    if (wave_live) {
+      qk(s_k[0], sa);
+      mul = settle(sa, tile_key(t_begin));
+    }
+    for (int t = t_begin; t < t_end; t += 2) {
+      begin_round(s_v[0], t);
+      round(s_k[1], s_v[0], s_k[0], s_v[1], sa, sb, t);
+      if (t + 1 == t_end) break;
+      begin_round(s_v[1], t + 1);
+      round(s_k[0], s_v[1], s_k[1], s_v[0], sb, sa, t + 1);
+    }
+    // whether any wave met values that clean_values left out
+    lds_barrier();
+    const int any_odd = __any(odd) ? 1 : 0;
+    int* flags = reinterpret_cast<int*>(s_k[0]);
+    if (lane == 0) flags[wave] = any_odd;
+    lds_barrier();
+    if (flags[0] | flags[1] | flags[2] | flags[3]) {
+      // they go to the rows that see them: a weight is positive and changes neither an
+      // infinity nor a NaN.  The lane sums dimensions 32 d + 8 (r / 4) + 4 half + r % 4.
+#pragma unroll 1
+      for (int i = 0; i < (t_end - t_begin) * kPreKeys; ++i) {
+        const int t = t_begin + i / kPreKeys, j = tile_key(t) + i % kPreKeys;
+        if (j >= len || !edge(tile_key(t))) continue;
+        const int blk = j >> 4, page = kv_page(c, pages[blk >> c.lb]), u = (j & 15) / kUnit;
+        const char* vj = c.v + kv_block_offset<kBlockBytes>(c, page, hk, blk) + u * D * 16 + 64 * half +
+                         (j % kUnit) * (E4 ? 1 : 2);
+        const bool in = visible(Mask{pos, rlow, rpre}, j);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const char* at = vj + 16 * (32 * d + 8 * (r >> 2) + (r & 3));
+            const uint32_t w = E4 ? *reinterpret_cast<const uint8_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+            const bool is_odd = E4 ? (w & 0x7fu) == 0x7fu : (w & 0x7f80u) == 0x7f80u;
+            acc[d][r] += in && is_odd ? (E4 ? __builtin_nanf("") : bf16_bits_to_float(w)) : 0.0f;
+          }
+      }
+    }
   }
 
   l = halves_sum(l);
@@ -406,12 +470,15 @@ template <int D, bool E4>
 static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                            const SplitArgs& sp, int slots, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)slots * c.Hkv * sp.nsplit));
-  if (a.softcap > 0.0f || a.slopes)
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, true>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
+  if (a.slopes)
+    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 2>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
+                       slots);
+  else if (a.softcap > 0.0f)
+    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 1>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
                        slots);
   else
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, false>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse,
-                       sp, slots);
+    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 0>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
+                       slots);
 }
 
 hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
