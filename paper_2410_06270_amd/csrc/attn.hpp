@@ -160,6 +160,41 @@ __device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d
   return (uint32_t)r;
 }
 
+// ---------------------------------------------------------- between lanes --
+// The larger, and the sum, of x in lanes l and l ^ 32 (half waves) or l ^ 16 (their rows).
+__device__ __forceinline__ float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float rows_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// x of the lane that the DPP control names, within the row of 16.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+
+// The sum over the lane's half wave: neighbours, pairs of a quad, quads of 8
+// (mirrored), eights of a row (mirrored), the two rows.
+__device__ __forceinline__ float half_wave_sum(float x) {
+  x += dpp<0xb1>(x);
+  x += dpp<0x4e>(x);
+  x += dpp<0x141>(x);
+  x += dpp<0x140>(x);
+  return rows_sum(x);
+}
+
 // ------------------------------------------------------------------ scores --
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

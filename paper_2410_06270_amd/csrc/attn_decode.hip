@@ -171,8 +171,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < 4 * KT; ++e) mx = fmaxf(mx, x[e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = halves_max(rows_max(mx));
     const float m_new = fmaxf(m, mx);
     if (__any(m_new > m)) {
       const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
@@ -234,8 +233,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   }
 
   // join the four waves
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  l = halves_sum(rows_sum(l));
   if (quarter == 0) {
     s_ml[0][wave][n] = m;
     s_ml[1][wave][n] = l;
@@ -365,18 +363,68 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, i
   if (lse && d == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
 }
 
+// Few parts: D/4 threads a (row, head), 16 bytes of a part each.  (4096 rows of
+// 16 heads in two parts: 78 us by the kernel above, @JOIN2@ by this.)
+constexpr int kJoinFew = 8;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(SplitArgs sp, int all, int Hq, int g,
+                                                                     const float* __restrict__ v_scale, RowsOut o,
+                                                                     float* __restrict__ lse,
+                                                                     const int32_t* __restrict__ q_start, int S) {
+  constexpr int kGroup = D / 4;
+  const int w = blockIdx.x * (kJoinThreads / kGroup) + threadIdx.x / kGroup, d = threadIdx.x % kGroup;
+  if (w >= all) return;
+  const int row = w / Hq, h = w - row * Hq;
+  if (q_start && (row < q_start[0] || row >= q_start[S])) return;   // padding
+  const float* ml = sp.ml + (size_t)w * sp.nsplit * 2;
+  float M = kNegInf;
+  for (int part = 0; part < sp.nsplit; ++part)
+    if (ml[2 * part + 1] != 0.0f) M = fmaxf(M, ml[2 * part]);
+  const float M0 = M == kNegInf ? 0.0f : M;
+  const float* po = sp.o + (size_t)w * sp.nsplit * D + 4 * d;
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+  float L = 0.0f;
+  for (int part = 0; part < sp.nsplit; ++part) {
+    const float l = ml[2 * part + 1];
+    if (l == 0.0f) continue;
+    const float f = exp2_fast(ml[2 * part] - M0);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)part * D);
+    L += l * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+  }
+  const float f = L == 0.0f ? 0.0f : (v_scale ? v_scale[h / g] : 1.0f) / L;
+  u32x2 out = {0u, 0u};
+  if (L != 0.0f) {
+    out[0] = bf16_pair(r[0] * f, r[1] * f);
+    out[1] = bf16_pair(r[2] * f, r[3] * f);
+  }
+  *reinterpret_cast<u32x2*>(o.p + (size_t)row * o.stride + (size_t)h * D + 4 * d) = out;
+  if (lse && d == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
+}
+
 hipError_t launch_attn_join(const SplitArgs& sp, int rows, int Hq, int g, int D, const float* v_scale, RowsOut o,
                             float* lse, const BatchArgs* ragged, hipStream_t stream) {
-  const dim3 grid((unsigned)((size_t)rows * Hq));
+  const int all = rows * Hq, per = kJoinThreads / (D / 4);
   const int32_t* q_start = ragged ? ragged->q_start : nullptr;
   const int S = ragged ? ragged->S : 0;
   timing_begin(stream, kSiteAttnJoin);
-  if (D == 64)
-    hipLaunchKernelGGL(attn_join_kernel<64>, grid, dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse, q_start,
-                       S);
-  else
-    hipLaunchKernelGGL(attn_join_kernel<128>, grid, dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse,
+  if (sp.nsplit <= kJoinFew) {
+    const dim3 grid((all + per - 1) / per);
+    if (D == 64)
+      hipLaunchKernelGGL(attn_join_few_kernel<64>, grid, dim3(kJoinThreads), 0, stream, sp, all, Hq, g, v_scale, o, lse,
+                         q_start, S);
+    else
+      hipLaunchKernelGGL(attn_join_few_kernel<128>, grid, dim3(kJoinThreads), 0, stream, sp, all, Hq, g, v_scale, o,
+                         lse, q_start, S);
+  } else if (D == 64) {
+    hipLaunchKernelGGL(attn_join_kernel<64>, dim3(all), dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse,
                        q_start, S);
+  } else {
+    hipLaunchKernelGGL(attn_join_kernel<128>, dim3(all), dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse,
+                       q_start, S);
+  }
   timing_end(stream, kSiteAttnJoin);
   return hipGetLastError();
 }

@@ -26,16 +26,20 @@ namespace mc {
 constexpr int kColWaves = 4;
 constexpr int kColThreads = 64 * kColWaves;
 constexpr int kColKeys = 64 * kColWaves;      // keys of a workgroup
-constexpr int kColTarget = 2048;              // workgroups aimed at
 
 __host__ __device__ static inline int col_tiles(int L) { return (L + kColKeys - 1) / kColKeys; }
 
-// Row slices of a (key tile, key-value head): more than 8 rounds of the chip even
-// out the triangle, and no slice below one row tile of one head for the average tile.
+// Row slices of a (key tile, key-value head).  A workgroup costs some 5 us of
+// loading its keys and joining its sums, a round of the loop under 1: about kColRounds
+// rounds each, between two workgroups a CU and eight (which evens out the triangle).
+constexpr int kColRounds = 32, kColLeast = 512, kColMost = 2048;
+
 static int col_slices(int L, int Hkv, int g) {
-  const int wgs = col_tiles(L) * Hkv, n = (kColTarget + wgs - 1) / wgs;
-  const int most = (L + 31) / 32 * g;
-  return n > most ? most : n;
+  const long long tiles = (L + 31) / 32, wgs = (long long)col_tiles(L) * Hkv;
+  long long want = wgs * tiles * g / 2 / kColRounds;
+  want = want < kColLeast ? kColLeast : want > kColMost ? kColMost : want;
+  const long long n = (want + wgs - 1) / wgs, most = tiles * g;
+  return (int)(n > most ? most : n);
 }
 
 static size_t up256(size_t b) { return (b + 255) / 256 * 256; }
@@ -68,35 +72,13 @@ __global__ void __launch_bounds__(kColThreads, 2)
   constexpr int kLoads = D / 64 + 1;            // direct loads of a wave for a row tile
   // a tile's queries, then its rows' lse: a copy for each wave, twice over the half waves
   constexpr int kSlotBytes = kRowBytes + kColWaves * 256;
-  __shared__ __attribute__((aligned(16))) char s_ring[kColRing][kSlotBytes];
+  __shared__ __attribute__((aligned(16))) char s_ring[kColRing * kSlotBytes];
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % c.Hkv;
   id /= c.Hkv;
   const int slice = id % slices, tile = id / slices;     // the first keys have the most rows: they go first
   const int key0 = tile * kColKeys + 64 * wave;
-
-  // keys: lane (key n of 32, half) holds units half, half + 2, ... (bf16), or units of
-  // 16 whose first and last 8 dimensions go to two steps (e4m3).
-  bf16x8 kf[2][DK];
-  const int last_blk = (L - 1) >> 4;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int blk = min((key0 + 32 * h + n) >> 4, last_blk);
-    const int page = kv_page(c, b.page_table[blk >> c.lb]);
-    const char* kp = c.k + kv_block_offset<kBlockBytes>(c, page, hk, blk) + (n & 15) * 16 + half * 256;
-    if constexpr (E4) {
-#pragma unroll
-      for (int i = 0; i < DK / 2; ++i) {
-        const u32x4 r = *reinterpret_cast<const u32x4*>(kp + 512 * i);
-        kf[h][2 * i] = as_bf16x8(e4m3_to_bf16(r[0], r[1]));
-        kf[h][2 * i + 1] = as_bf16x8(e4m3_to_bf16(r[2], r[3]));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < DK; ++i) kf[h][i] = as_bf16x8(*reinterpret_cast<const u32x4*>(kp + 512 * i));
-    }
-  }
 
   f32x16 acc[2];
 #pragma unroll
@@ -137,9 +119,38 @@ __global__ void __launch_bounds__(kColThreads, 2)
     next(ft, fh);
   };
 
-  auto work = [&](auto masked, const char* slot, int row0, float ls, float slope2) {
-    constexpr bool MASKED = decltype(masked)::value;
-    f32x16 sv[2];
+  // the first tiles' loads, then the keys', and a wait for all of them: the
+  // compiler would otherwise wait for the keys, and with them for every tile, in each
+  // round
+#pragma unroll
+  for (int i = 0; i < kColRing - 1; ++i)
+    if (i < count) fetch(s_ring + i * kSlotBytes);
+  // keys: lane (key n of 32, half) holds units half, half + 2, ... (bf16), or units of
+  // 16 whose first and last 8 dimensions go to two steps (e4m3).
+  bf16x8 kf[2][DK];
+  const int last_blk = (L - 1) >> 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int blk = min((key0 + 32 * h + n) >> 4, last_blk);
+    const int page = kv_page(c, b.page_table[blk >> c.lb]);
+    const char* kp = c.k + kv_block_offset<kBlockBytes>(c, page, hk, blk) + (n & 15) * 16 + half * 256;
+    if constexpr (E4) {
+#pragma unroll
+      for (int i = 0; i < DK / 2; ++i) {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(kp + 512 * i);
+        kf[h][2 * i] = as_bf16x8(e4m3_to_bf16(r[0], r[1]));
+        kf[h][2 * i + 1] = as_bf16x8(e4m3_to_bf16(r[2], r[3]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < DK; ++i) kf[h][i] = as_bf16x8(*reinterpret_cast<const u32x4*>(kp + 512 * i));
+    }
+  }
+
+  wait_vmcnt<0>();
+
+  // Products of a tile: keys 32 h + 8 (r / 4) + 4 half + r % 4 of row n.
+  auto qk = [&](const char* slot, f32x16 (&sv)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -153,38 +164,68 @@ __global__ void __launch_bounds__(kColThreads, 2)
 #pragma unroll
       for (int h = 0; h < 2; ++h) sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][i], qv, sv[h], 0, 0, 0);
     }
-    const int row = row0 + n;
-    const int low = a.window > 0 && row >= a.window ? row - a.window : -1, high = row < L ? row : -1;
+  };
+  // Adds a tile's probabilities.
+  struct Tile {
+    int row0;
+    float ls, slope2;    // log2(e) lse of the lane's row; of its head
+    bool live, masked;   // reaches below the wave's diagonal; not wholly
+  };
+  auto add = [&](auto masked, const f32x16 (&sv)[2], const Tile& t) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int row = t.row0 + n, key = key0 + 4 * half;
+    const int low = (a.window > 0 && row >= a.window ? row - a.window : -1) - key, high = (row < L ? row : -1) - key;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int j = key0 + 32 * h + 8 * (r >> 2) + 4 * half + (r & 3);
-        float p = exp2_fast(MODE ? score2<MODE>(sv[h][r], sc, slope2, j - row) - ls
-                                 : __builtin_fmaf(sv[h][r], sc.scale2, -ls));
+        const int j = 32 * h + 8 * (r >> 2) + (r & 3);
+        float p = exp2_fast(MODE ? score2<MODE>(sv[h][r], sc, t.slope2, j + key - row) - t.ls
+                                 : __builtin_fmaf(sv[h][r], sc.scale2, -t.ls));
         if (MASKED) p = ((j <= high) & (j > low)) ? p : 0.0f;
         acc[h][r] += p;
       }
   };
 
-  // Slots of the ring are distinct and passed as such: a read of the current one
-  // then does not wait for the loads into the others.  The first fetches are rounds
-  // of the loop without work.
-  auto round = [&](const char* __restrict__ cur, char* __restrict__ nxt, bool more, bool ready) {
-    if (more) fetch(nxt);
-    if (!ready) return;
-    const int row0 = 32 * ct;
-    const float slope2 = MODE == 2 && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
-    next(ct, ch);
-    if (row0 + 31 < key0) return;                        // above the wave's diagonal
-    const float v = *reinterpret_cast<const float*>(cur + kRowBytes + 256 * wave + 4 * lane);
-    const float ls = v == kNegInf ? -kNegInf : v * kLog2e;       // a row without keys: every probability 0
-    if (row0 >= key0 + 63 && row0 + 32 <= L && (a.window == 0 || row0 + 31 - key0 < a.window))
-      work(std::false_type{}, cur, row0, ls, slope2);
-    else
-      work(std::true_type{}, cur, row0, ls, slope2);
+  // Round i: the products of tile i beside the probabilities of tile i - 1.  Slots
+  // of the ring are distinct and passed as such: a read of the current one then does
+  // not wait for the loads into the others.
+  Tile prev = {0, 0.0f, 0.0f, false, false};
+  auto round = [&](const char* __restrict__ cur, char* __restrict__ nxt, f32x16 (&sv)[2], f32x16 (&sp)[2], int i) {
+    if (i + kColRing - 1 < count) fetch(nxt);
+    Tile t = {32 * ct, 0.0f, 0.0f, false, false};
+    if (i < count) {
+      t.slope2 = MODE == 2 && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
+      next(ct, ch);
+      t.live = t.row0 + 31 >= key0;
+      t.masked = !(t.row0 >= key0 + 63 && t.row0 + 32 <= L && (a.window == 0 || t.row0 + 31 - key0 < a.window));
+      const float v = *reinterpret_cast<const float*>(cur + kRowBytes + 256 * wave + 4 * lane);
+      t.ls = v == kNegInf ? -kNegInf : v * kLog2e;       // a row without keys: every probability 0
+    }
+    if (t.live && prev.live && !prev.masked) {
+      qk(cur, sv);
+      add(std::false_type{}, sp, prev);
+      // LDS reads ahead of their products, and between the products the vector work
+      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+      for (int m = 0; m < 2 * DK; ++m) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (m & 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 96 / (2 * DK), 0);
+      }
+    } else {
+      if (t.live) qk(cur, sv);
+      if (prev.live) {
+        if (prev.masked)
+          add(std::true_type{}, sp, prev);
+        else
+          add(std::false_type{}, sp, prev);
+      }
+    }
+    prev = t;
   };
-  for (int i = 1 - kColRing; i < count; ++i) {
+  f32x16 sa[2], sb[2];
+  auto begin_round = [&](int i) {
     // tile i's loads are the oldest of those of up to kColRing - 1 tiles; the
     // barrier also ends every wave's reads of the slot that the next fetch overwrites
     if (i + kColRing - 2 < count)
@@ -192,14 +233,19 @@ __global__ void __launch_bounds__(kColThreads, 2)
     else
       wait_vmcnt<0>();
     lds_barrier();
-    round(s_ring[(i + kColRing) % kColRing], s_ring[(i + 2 * kColRing - 1) % kColRing], i + kColRing - 1 < count,
-          i >= 0);
+  };
+  auto slot_of = [&](int i) { return s_ring + (i % kColRing) * kSlotBytes; };
+  for (int i = 0; i <= count; i += 2) {
+    begin_round(i);
+    round(slot_of(i), slot_of(i + kColRing - 1), sa, sb, i);
+    if (i == count) break;
+    begin_round(i + 1);
+    round(slot_of(i + 1), slot_of(i + kColRing), sb, sa, i + 1);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      for (int off = 16; off >= 1; off >>= 1) acc[h][r] += __shfl_xor(acc[h][r], off);
+    for (int r = 0; r < 16; ++r) acc[h][r] = half_wave_sum(acc[h][r]);
   if (n == 0) {
     float* out = partial + ((size_t)hk * slices + slice) * col_tiles(L) * kColKeys + key0 + 4 * half;
 #pragma unroll
@@ -224,15 +270,24 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const float
   if (j >= L) return;
   float cs = 0.0f;
   const size_t stride = (size_t)col_tiles(L) * kColKeys;
+#pragma unroll 4
   for (int i = lane; i < parts; i += 64) cs += partial[(size_t)i * stride + j];
   float n1 = 0.0f;
   const uint16_t* xr = x + (size_t)j * d;
   if (xvec) {
-    for (int i = 8 * lane; i < d; i += 512) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(xr + i);
+    // eight loads at a time: latency is what a row's few loads cost
+    for (int i = 8 * lane; i < d; i += 8 * 512) {
+      u32x4 v[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        n1 += fabsf(bf16_bits_to_float(v[e] & 0xffffu)) + fabsf(bf16_bits_to_float(v[e] >> 16));
+      for (int u = 0; u < 8; ++u) {
+        v[u] = u32x4{0u, 0u, 0u, 0u};
+        if (i + 512 * u < d) v[u] = *reinterpret_cast<const u32x4*>(xr + i + 512 * u);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          n1 += fabsf(bf16_bits_to_float(v[u][e] & 0xffffu)) + fabsf(bf16_bits_to_float(v[u][e] >> 16));
     }
   } else {
     for (int i = lane; i < d; i += 64) n1 += fabsf(bf16_bits_to_float(xr[i]));

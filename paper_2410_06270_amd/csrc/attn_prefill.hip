@@ -52,16 +52,6 @@ size_t attn_prefill_split_rows(int T, int Hq) {
   return all < most ? all : most;
 }
 
-// The larger of x in lanes l and l ^ 32, and the sum of both.
-__device__ __forceinline__ float halves_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float halves_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // The running maximum follows a larger score only when it is left behind by more
 // than this (log2): weights up to 2^8 lose nothing in fp32 sums or in bf16, and most
 // tiles need no scaling and no exchange between the half waves.
@@ -95,8 +85,8 @@ __device__ __forceinline__ bool clean_values(char* vt, int n) {
 }
 
 // The order of a round's instructions: LDS reads kReadAhead matrix instructions
-// before their use, and between the matrix instructions of the scores the vector work on
-// the other tile.
+// before their use, and the vector work spread over the spaces between all of them: the
+// first products with the values need only the first weights.
 constexpr int kReadAhead = 5;
 
 template <int DK, int DT>
@@ -107,7 +97,7 @@ __device__ __forceinline__ void interleave() {
   for (int i = 0; i < kMfmas; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);             // matrix
     if (i + kReadAhead < kMfmas) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    if (i < 2 * DK) __builtin_amdgcn_sched_group_barrier(0x002, 112 / (2 * DK), 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 128 / kMfmas, 0);  // vector
   }
 }
 
@@ -130,7 +120,12 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int hk = id % c.Hkv;
   id /= c.Hkv;
   const int split = id % sp.nsplit;
-  const int slot = slots - 1 - id / sp.nsplit;       // later rows see more keys: they go first
+  // Later rows see more keys: the later half of the row tiles goes first, from the
+  // last on, then the other from the first on, so that where all workgroups are on the chip
+  // at once a CU has a long and a short one (4096 tokens of 16 heads, 528
+  // workgroups: 108 us from the last to the first, 105 so).
+  const int turn = id / sp.nsplit, later = (slots + 1) / 2;
+  const int slot = turn < later ? slots - 1 - turn : turn - later;
   const int s = find_sequence(b.q_start, b.S, slot, kPreRows, 1, a.g);
   int first, count;
   sequence_rows(b, s, first, count);
@@ -184,12 +179,13 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int last_blk = len > 0 ? (len - 1) >> 4 : 0;
   auto tile_key = [&](int t) { return (t < ia ? t : t - ia + ib) * kPreKeys; };
 
-  // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each.  A
-  // page number comes a round before the loads that it is for.
+  // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each, both
+  // at the same offset.  A page number comes a round before the loads that it is for.
   auto tile_blk = [&](int t) { return min((tile_key(t) >> 4) + wave, last_blk); };
-  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(max(t, t_begin), t_end - 1)) >> c.lb); };
-  auto fetch = [&](const char* from, int t, int page, char* to) {
-    const char* src = from + kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk, tile_blk(t)) + 16 * lane;
+  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(t, t_end - 1)) >> c.lb); };
+  auto offset_of = [&](int t, int page) { return kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk, tile_blk(t)); };
+  auto fetch = [&](const char* from, size_t off, char* to) {
+    const char* src = from + off + 16 * lane;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) lds_dma16(src + 1024 * i, to + 1024 * i);
   };
@@ -267,12 +263,17 @@ __global__ void __launch_bounds__(kPreThreads, 2)
             as_bf16x8(*reinterpret_cast<const u32x4*>(vt + voff + i * kBlk + 512 * d)), as_bf16x8(p[i]), acc[d], 0, 0,
             0);
   };
+  auto largest = [&](const f32x16 (&sv)[2]) {
+    float mx = kNegInf;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
+    return mx;
+  };
   // A tile's scores in place of its products, where it is masked or the score is not
   // a multiple of the product, and the running maximum.  Returns what weigh multiplies by.
-  auto settle = [&](f32x16 (&sv)[2], int key0) {
+  auto settle = [&](f32x16 (&sv)[2], float mx, int key0) {
     const bool masked = !((wpos_first >= 0 && key0 + kPreKeys <= pre) ||
                           (key0 + kPreKeys - 1 <= wpos_first && (a.window == 0 || key0 > wpos_last - a.window)));
-    float mx = kNegInf;
     if (masked || MODE) {
       const int hkey = key0 + 8 * half;
       const Mask k = {pos - hkey, rlow - hkey, rpre - hkey};
@@ -288,11 +289,11 @@ __global__ void __launch_bounds__(kPreThreads, 2)
           sv[e >> 4][e & 15] = visible(k, j) ? sv[e >> 4][e & 15] : kNegInf;
         }
       }
+      mx = MODE == 1 && !masked ? score2<1>(mx, sc, 0.0f, 0) : largest(sv);
+    } else {
+      mx *= sc.scale2;
     }
-#pragma unroll
-    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
     const float mul = masked || MODE ? 1.0f : sc.scale2;
-    mx *= mul;
     if (__any(mx > m + kMaxSlack)) {
       const float m_new = fmaxf(m, halves_max(mx));
       const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
@@ -316,18 +317,20 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   // work on the other.  Loads: keys of tile t + 2 and values of t + 1 (e4m3: of one
   // more, those of this round being widened).  The buffers are distinct and passed as
   // such: reads of one do not wait for the loads into another.
-  int page_k = 0, page_v = 0;                          // of the next round's loads
+  int page = 0, page_tile = 0;                         // of the next tile of keys, and which
+  size_t off_v = 0;                                    // of the next tile of values
   float mul = 1.0f;
   bool odd = false;
   char* raw_k = s_lds + 4 * kTileBytes + wave * 2 * kBlockBytes;      // e4m3 only
   char* raw_v = raw_k + (E4 ? kBlockBytes : 0);
-  auto load_k = [&](int t, char* kt) {
-    if (t < t_end) fetch(c.k, t, page_k, E4 ? raw_k : kt + wave * kBlk);
-    page_k = page_of(t + 1);
-  };
-  auto load_v = [&](int t, char* vt) {
-    if (t < t_end) fetch(c.v, t, page_v, E4 ? raw_v : vt + wave * kBlk);
-    page_v = page_of(t + 1);
+  // the values of tile t - 1 and the keys of tile t
+  auto load = [&](int t, char* kt, char* vt) {
+    if (t > t_begin && t <= t_end) fetch(c.v, off_v, E4 ? raw_v : vt + wave * kBlk);
+    if (t >= t_end) return;
+    const size_t off = offset_of(t, page);
+    page_tile = t + 1;
+    fetch(c.k, off, E4 ? raw_k : kt + wave * kBlk);
+    off_v = off;
   };
   auto lds_done = [&]() {                              // what was read may be overwritten
     asm volatile("" ::: "memory");
@@ -340,20 +343,23 @@ __global__ void __launch_bounds__(kPreThreads, 2)
       if (t + 2 < t_end) widen(raw_k, true, knext + wave * kBlk);
       if (t + 1 < t_end) widen(raw_v, false, vnext + wave * kBlk);
       lds_done();
-      load_k(t + 3, knext);
-      load_v(t + 2, vnext);
+      load(t + 3, knext, vnext);
     } else {
-      load_k(t + 2, knext);
-      load_v(t + 1, vnext);
+      load(t + 2, knext, vnext);
     }
-    if (!wave_live) return;
-    // (the last round's next tile is whatever its buffer holds, and not used)
-    u32x4 p[4];
-    qk(kt, nxt);
-    weigh(cur, mul, p);
-    pv(vt, p);
-    interleave<DK, DT>();
-    if (t + 1 < t_end) mul = settle(nxt, tile_key(t + 1));
+    if (wave_live) {
+      // (the last round's next tile is whatever its buffer holds, and not used)
+      u32x4 p[4];
+      qk(kt, nxt);
+      weigh(cur, mul, p);
+      pv(vt, p);
+      const float mx = largest(nxt);
+      interleave<DK, DT>();
+      if (t + 1 < t_end) mul = settle(nxt, mx, tile_key(t + 1));
+    }
+    // here, and not with the loads: a scalar load under way makes the wait for an
+    // LDS read a wait for all of them
+    page = page_of(page_tile);
   };
   // what the last round loaded is in LDS once every wave's loads are; the barrier
   // also ends every wave's reads of the buffers that this round fills
@@ -368,30 +374,30 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   };
   if (t_begin < t_end) {
     f32x16 sa[2], sb[2];
-    page_k = page_of(t_begin);
-    page_v = page_k;
-    load_k(t_begin, s_k[0]);
+    page = page_of(t_begin);
+    load(t_begin, s_k[0], s_v[1]);
+    page = page_of(page_tile);
     if constexpr (E4) {
       wait_vmcnt<0>();
       widen(raw_k, true, s_k[0] + wave * kBlk);
       lds_done();
     }
-    load_k(t_begin + 1, s_k[1]);
-    load_v(t_begin, s_v[0]);
+    load(t_begin + 1, s_k[1], s_v[0]);
+    page = page_of(page_tile);
     if constexpr (E4) {
       wait_vmcnt<0>();
       if (t_begin + 1 < t_end) widen(raw_k, true, s_k[1] + wave * kBlk);
       widen(raw_v, false, s_v[0] + wave * kBlk);
       lds_done();
-      load_k(t_begin + 2, s_k[0]);
-      load_v(t_begin + 1, s_v[1]);
+      load(t_begin + 2, s_k[0], s_v[1]);
+      page = page_of(page_tile);
     } else {
       wait_vmcnt<0>();
     }
     lds_barrier();
     if (wave_live) {
       qk(s_k[0], sa);
-      mul = settle(sa, tile_key(t_begin));
+      mul = settle(sa, largest(sa), tile_key(t_begin));
     }
     for (int t = t_begin; t < t_end; t += 2) {
       begin_round(s_v[0], t);
