@@ -26,16 +26,22 @@ constexpr int kDecThreads = 64 * kDecWaves;
 constexpr int kDecHeads = 16;        // query heads of a workgroup
 constexpr int kMaxSplit = 128;
 
-// The parts a cache is cut into: enough for about kDecTarget workgroups (8 waves
-// of a CU's registers are 2 workgroups, so several rounds of them, which evens
-// out ragged lengths), none shorter than one step of every wave.
-constexpr int kDecTarget = 2048;
+// The parts a cache is cut into.  Enough to fill the chip (two workgroups of 4 waves
+// fit a CU's registers), as long as every wave has a step; more, up to
+// kDecTarget workgroups, where a part keeps kDecPart bytes of keys and values: the
+// shorter the parts, the less a long sequence of a ragged batch is waited for (48
+// sequences of 300 to 8191 tokens: 158 us at one round of workgroups, 145 at four), and
+// the more their starts and the join cost (64 sequences of 512: 23 and 30).
+constexpr int kDecFill = 512, kDecTarget = 2048, kDecPart = 192 << 10;
 
-static int decode_splits(int S, int Hkv, int head_tiles, int max_len, int keys) {
+static int decode_splits(int S, int Hkv, int head_tiles, int max_len, int keys, int key_bytes) {
   const long long wgs = (long long)S * Hkv * head_tiles;
-  long long n = kDecTarget / wgs;
-  const long long most = ((long long)max_len + keys - 1) / keys;
-  n = n > most ? most : n;
+  const long long steps = ((long long)max_len + keys - 1) / keys;
+  const long long fill = kDecFill / wgs, more = kDecTarget / wgs;
+  long long n = (long long)max_len * key_bytes / kDecPart;
+  n = n > more ? more : n;
+  n = n < fill ? fill : n;
+  n = n > steps ? steps : n;
   return (int)(n < 1 ? 1 : n > kMaxSplit ? kMaxSplit : n);
 }
 
@@ -100,6 +106,10 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   const int koff = (E4 ? (n & 3) : 8 * ((n >> 2) & 1) + (n & 3)) * 16 + quarter * 256;
   const int voff = (E4 ? 0 : (quarter & 1) * D * 16) + n * 16;
 
+  // Values are read once and by whole lines: past the caches (64 sequences of 4096
+  // e4m3 tokens, 537 MB: 101 -> 84 us; of 1024 bf16 tokens and 16 heads 95 -> 84).  A
+  // load of keys takes half of each line that it touches, the next the other half: those
+  // stay ordinary loads (non-temporal ones: 54 us for 48 at 4 x 32768 e4m3 tokens).
   auto load = [&](Step& st, int i, int kp, int vp) {
     const int blk = step_blk(i);
     const int kb = min(blk + kblk, last_blk), vb = min(blk + vblk, last_blk);
@@ -110,7 +120,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
 #pragma unroll
       for (int u = 0; u < KC; ++u) st.k[t][u] = *reinterpret_cast<const u32x4*>(kp0 + 64 * t + 1024 * u);
 #pragma unroll
-    for (int t = 0; t < DT; ++t) st.v[t] = *reinterpret_cast<const u32x4*>(vp0 + 256 * t);
+    for (int t = 0; t < DT; ++t) st.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp0 + 256 * t));
   };
 
   f32x4 acc[DT];
@@ -460,7 +470,7 @@ hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs&
   const int head_tiles = (a.g + kDecHeads - 1) / kDecHeads;
   if (a.window > 0 && !a.prefix && a.window < max_len) max_len = a.window;
   SplitArgs sp;
-  sp.nsplit = decode_splits(b.S, c.Hkv, head_tiles, max_len, (e4 ? 64 : 32) * kDecWaves);
+  sp.nsplit = decode_splits(b.S, c.Hkv, head_tiles, max_len, (e4 ? 64 : 32) * kDecWaves, D * (e4 ? 2 : 4));
   sp.o = static_cast<float*>(ws);
   sp.ml = sp.o + (size_t)b.S * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnDecode);
