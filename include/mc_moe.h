@@ -452,7 +452,7 @@ typedef struct mc_qk_prep {
  *   (y_a, y_b) <- (y_a cos - y_b sin, y_a sin + y_b cos)   (each rotated pair)
  * in fp32, rounded once: queries to bf16 into q_out, keys to the cache's type;
  * values are stored as they are.  An e4m3 code is the nearest one (ties to even)
- * of y / scale[h] clamped to +-448; NaN stays NaN.
+ * of y * (1 / scale[h]), both in fp32, clamped to +-448; NaN stays NaN.
  * q [T][Hq*D], k and v [T][Hkv*D] bf16 with the given elements between rows
  * (multiples of 8, so that slices of one fused projection serve); q_out
  * likewise, and it may be q itself (same stride).  q and q_out may both be

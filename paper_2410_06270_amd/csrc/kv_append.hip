@@ -7,13 +7,13 @@
 // consecutive tokens of one dimension, so one lane reads 8 dimensions of all
 // the tokens of a unit and writes whole units, transposed in its registers.  A key
 // unit runs along the dimensions, and a norm over a row needs the whole row: one
-// workgroup takes one token's queries and keys, 16 bytes a lane.
+// wave takes one token's queries and keys, 16 bytes a lane and load.
 #include "attn.hpp"
 
 namespace mc {
 
 constexpr int kAppendThreads = 256;
-constexpr int kRowChunks = 4;        // chunks of 8 elements a thread holds at once
+constexpr int kRowChunks = 8;        // chunks of 8 elements a lane holds at once
 
 // The largest number of unit groups that n new tokens from q_start on touch is
 // floor((n + 6) / U) + 1 (U = 8) and fewer for U = 16; sequence s owns the slots from
@@ -66,7 +66,7 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
   const int in_block = (int)(base & 15);
   char* dst = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) +
               (size_t)((in_block / U) * D + d0) * 16;
-  const float sc = E4 ? c.v_scale[head] : 1.0f;
+  const float sc = E4 ? 1.0f / c.v_scale[head] : 1.0f;
   if (all) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -74,8 +74,8 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if constexpr (E4) {
-          w[q] = e4m3_quad(half_of(raw[4 * q][i / 2], i & 1) / sc, half_of(raw[4 * q + 1][i / 2], i & 1) / sc,
-                           half_of(raw[4 * q + 2][i / 2], i & 1) / sc, half_of(raw[4 * q + 3][i / 2], i & 1) / sc);
+          w[q] = e4m3_quad(half_of(raw[4 * q][i / 2], i & 1) * sc, half_of(raw[4 * q + 1][i / 2], i & 1) * sc,
+                           half_of(raw[4 * q + 2][i / 2], i & 1) * sc, half_of(raw[4 * q + 3][i / 2], i & 1) * sc);
         } else {
           const uint32_t a = raw[2 * q][i / 2], z = raw[2 * q + 1][i / 2];
           w[q] = (i & 1) ? (a >> 16) | (z & 0xffff0000u) : (a & 0xffffu) | (z << 16);
@@ -93,7 +93,7 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (E4)
-        dst[16 * i + u] = (char)e4m3_quad(half_of(raw[u][i / 2], i & 1) / sc, 0.0f, 0.0f, 0.0f);
+        dst[16 * i + u] = (char)e4m3_quad(half_of(raw[u][i / 2], i & 1) * sc, 0.0f, 0.0f, 0.0f);
       else
         reinterpret_cast<uint16_t*>(dst + 16 * i)[u] = (uint16_t)(raw[u][i / 2] >> (16 * (i & 1)));
     }
@@ -111,117 +111,124 @@ __device__ __forceinline__ float square_sum(const u32x4& r) {
   return s;
 }
 
-// Queries and keys of one token: chunk i of 8 elements in [0, nq + nk), the
-// queries' first.  A head's chunks lie in D/8 neighbouring lanes, and a thread's
-// chunks (256 apart) all start at the same dimension of their heads, so its cosines and
-// sines are loaded once.
-template <int D, bool E4>
+// The sum over the D/8 lanes of a head.
+template <int DU>
+__device__ __forceinline__ float head_sum(float x) {
+  x += dpp<0xb1>(x);
+  x += dpp<0x4e>(x);
+  x += dpp<0x141>(x);
+  if (DU == 16) x += dpp<0x140>(x);
+  return x;
+}
+
+// Queries and keys of one token, by one wave: chunk i of 8 elements in [0, nq + nk),
+// the queries' first, 64 neighbouring ones at a time.  A head's chunks lie in D/8
+// neighbouring lanes, and a lane's chunks all start at the same dimension of their
+// heads, so that its cosines and sines are loaded once for the token.
+template <int D, bool E4, int NORM>
 __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, const BatchArgs& b, const KvArgs& c,
                             RowsOut out, int t) {
   constexpr int DU = D / 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
-  __shared__ float red[2][kAppendThreads / 64];
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int lane = threadIdx.x & 63;
   const int nq = q.p ? Hq * DU : 0, total = nq + c.Hkv * DU;
   const uint16_t* qr = q.p + (size_t)t * q.stride;
   const uint16_t* kr = k.p + (size_t)t * k.stride;
-  auto load = [&](int i) {
-    u32x4 r = {0u, 0u, 0u, 0u};
-    if (i < total) r = *reinterpret_cast<const u32x4*>(i < nq ? qr + 8 * i : kr + 8 * (i - nq));
-    return r;
-  };
   u32x4 raw[kRowChunks];
+  auto load = [&](int i0) {
 #pragma unroll
-  for (int r = 0; r < kRowChunks; ++r) raw[r] = load(tid + r * kAppendThreads);
+    for (int r = 0; r < kRowChunks; ++r) {
+      const int i = i0 + 64 * r + lane;
+      raw[r] = u32x4{0u, 0u, 0u, 0u};
+      if (i < total) raw[r] = *reinterpret_cast<const u32x4*>(i < nq ? qr + 8 * i : kr + 8 * (i - nq));
+    }
+  };
+  load(0);
 
   const int s = find_sequence(b.q_start, b.S, t, 1, 0, 1);
   const long long first = b.q_start[s], last = b.q_start[s + 1];
   Place at;
-  const bool in = t >= first && t < last &&
-                  append_place(c, b, s, (long long)b.kv_len[s] - (last - t), p.n_pos, at);
-  if (!in) return;                   // the same for the whole workgroup
+  if (!(t >= first && t < last && append_place(c, b, s, (long long)b.kv_len[s] - (last - t), p.n_pos, at))) return;
 
-  const int d0 = 8 * (tid % DU), half = p.rot / 2;
-  const bool turns = d0 < p.rot;
-  const float* cs = p.rope + (size_t)at.pos * p.rot;
+  const int d0 = 8 * (lane % DU), half = p.rot / 2;
+  const bool turns = d0 < p.rot, low = d0 < half;
   f32x4 tab[4];
   if (turns) {
     // rotation i's cosine and sine: i = d0/2 .. +3, or d0 mod half .. +7
-    const float* from = cs + (p.pairs ? d0 : 2 * (d0 < half ? d0 : d0 - half));
+    const float* from = p.rope + (size_t)at.pos * p.rot + (p.pairs ? d0 : 2 * (low ? d0 : d0 - half));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < 2 || !p.pairs) tab[i] = *reinterpret_cast<const f32x4*>(from + 4 * i);
   }
+  const int partner = turns ? lane + (low ? half / 8 : -(half / 8)) : lane;
 
+  u32x4 wq = {}, wk = {};
+  if (NORM == 1) {
+    wq = *reinterpret_cast<const u32x4*>(p.q_norm + d0);
+    wk = *reinterpret_cast<const u32x4*>(p.k_norm + d0);
+  }
   float row_scale[2] = {1.0f, 1.0f};
-  if (p.q_norm && p.norm_row) {
+  if (NORM == 2) {
     float ss[2] = {0.0f, 0.0f};
-    for (int i = tid, r = 0; i < total; i += kAppendThreads, ++r) {
-      const float x = square_sum(r < kRowChunks ? raw[r & (kRowChunks - 1)] : load(i));
-      ss[i < nq ? 0 : 1] += x;
-    }
+    for (int i0 = 0; i0 < total; i0 += 64 * kRowChunks) {
+      if (i0) load(i0);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      for (int off = 32; off >= 1; off >>= 1) ss[w] += __shfl_xor(ss[w], off);
-      if (lane == 0) red[w][tid >> 6] = ss[w];
+      for (int r = 0; r < kRowChunks; ++r) {
+        const float x = square_sum(raw[r]);
+        const bool is_q = i0 + 64 * r + lane < nq;
+        ss[0] += is_q ? x : 0.0f;
+        ss[1] += is_q ? 0.0f : x;
+      }
     }
-    __syncthreads();
+    if (total > 64 * kRowChunks) load(0);
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      float x = 0.0f;
-      for (int i = 0; i < kAppendThreads / 64; ++i) x += red[w][i];
-      row_scale[w] = 1.0f / sqrtf(x / (float)((w == 0 ? Hq : c.Hkv) * D) + p.eps);
-    }
+    for (int w = 0; w < 2; ++w)
+      row_scale[w] = __builtin_amdgcn_rsqf(halves_sum(half_wave_sum(ss[w])) / (float)((w == 0 ? Hq : c.Hkv) * D) +
+                                           p.eps);
   }
 
-  for (int i0 = 0; i0 < total; i0 += kRowChunks * kAppendThreads) {
-    if (i0) {
-#pragma unroll
-      for (int r = 0; r < kRowChunks; ++r) raw[r] = load(i0 + tid + r * kAppendThreads);
-    }
+  for (int i0 = 0; i0 < total; i0 += 64 * kRowChunks) {
+    if (i0) load(i0);
 #pragma unroll
     for (int r = 0; r < kRowChunks; ++r) {
-      const int i = i0 + tid + r * kAppendThreads;
-      if (i - tid >= total) break;   // the same for the whole workgroup
+      if (i0 + 64 * r >= total) break;           // the same for the whole wave
+      const int i = i0 + 64 * r + lane;
       const bool is_q = i < nq;
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = half_of(raw[r][j / 2], j & 1);
-      if (p.q_norm) {
-        float sc = row_scale[is_q ? 0 : 1];
-        if (!p.norm_row) {
-          float ss = square_sum(raw[r]);
-          for (int off = DU / 2; off >= 1; off >>= 1) ss += __shfl_xor(ss, off);
-          sc = 1.0f / sqrtf(ss / (float)D + p.eps);
-        }
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (i < total) {
-          const uint16_t* wp = is_q ? p.q_norm : p.k_norm;
-          w = *reinterpret_cast<const u32x4*>(wp + (p.norm_row ? 8 * (is_q ? i : i - nq) : d0));
-        }
+      if (NORM) {
+        const float sc = NORM == 2 ? row_scale[is_q ? 0 : 1]
+                                   : __builtin_amdgcn_rsqf(head_sum<DU>(square_sum(raw[r])) * (1.0f / D) + p.eps);
+        u32x4 w = is_q ? wq : wk;
+        if (NORM == 2 && i < total)
+          w = *reinterpret_cast<const u32x4*>(is_q ? p.q_norm + 8 * i : p.k_norm + 8 * (i - nq));
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = x[j] * sc * half_of(w[j / 2], j & 1);
       }
-      if (p.rot) {
-        if (p.pairs) {
-          if (turns) {
+      if (p.rot && p.pairs) {
+        if (turns) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
-              const float a = x[2 * j], z = x[2 * j + 1];
-              x[2 * j] = a * co - z * si;
-              x[2 * j + 1] = a * si + z * co;
-            }
+          for (int j = 0; j < 4; ++j) {
+            const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
+            const float a = x[2 * j], z = x[2 * j + 1];
+            x[2 * j] = a * co - z * si;
+            x[2 * j + 1] = a * si + z * co;
           }
+        }
+      } else if (p.rot) {
+        float o[8];
+        if (p.rot == 128) {                      // the partner is 8 lanes on in the row of 16
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = dpp<0x128>(x[j]);
         } else {
-          const bool low = d0 < half;
-          const int from = turns ? lane + (low ? half / 8 : -(half / 8)) : lane;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = __shfl(x[j], partner);
+        }
+        if (turns) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float o = __shfl(x[j], from);
-            if (turns) {
-              const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
-              x[j] = low ? x[j] * co - o * si : o * si + x[j] * co;
-            }
+            const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
+            x[j] = x[j] * co + (low ? -o[j] : o[j]) * si;
           }
         }
       }
@@ -235,9 +242,9 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
         const int head = (i - nq) / DU;
         char* dst = c.k + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) + (at.pos & 15) * 16;
         if constexpr (E4) {
-          const float sc = c.k_scale[head];
-          u32x2 w = {e4m3_quad(x[0] / sc, x[1] / sc, x[2] / sc, x[3] / sc),
-                     e4m3_quad(x[4] / sc, x[5] / sc, x[6] / sc, x[7] / sc)};
+          const float sc = 1.0f / c.k_scale[head];
+          u32x2 w = {e4m3_quad(x[0] * sc, x[1] * sc, x[2] * sc, x[3] * sc),
+                     e4m3_quad(x[4] * sc, x[5] * sc, x[6] * sc, x[7] * sc)};
           *reinterpret_cast<u32x2*>(dst + (d0 / 16) * 256 + (d0 & 8)) = w;
         } else {
           u32x4 w;
@@ -251,11 +258,11 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 }
 
 // The first nv workgroups write values (4 waves, each a unit group's piece),
-// the others one token's queries and keys.  Eight neighbouring tokens share the lines
-// of the key blocks, and workgroups go round the 8 XCDs in turn: row workgroup r
-// takes token 64 (r / 64) + 8 (r % 8) + r / 8 % 8, so that one XCD's cache sees
-// whole lines.
-template <int D, bool E4>
+// the others the queries and keys of 4 tokens, one a wave.  Eight neighbouring tokens
+// share the lines of the key blocks, and workgroups go round the 8 XCDs in turn: of 16
+// row workgroups, number r and r + 8 take 8 neighbouring tokens, so that one XCD's cache
+// sees whole lines.
+template <int D, bool E4, int NORM>
 __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
                      int slots, int pieces) {
@@ -266,8 +273,8 @@ __global__ void __launch_bounds__(kAppendThreads)
     return;
   }
   const int r = blk - nv;
-  const int t = (r & ~63) + 8 * (r & 7) + ((r >> 3) & 7);
-  if (t < b.T) append_rows<D, E4>(q, k, Hq, p, b, c, out, t);
+  const int t = 4 * ((r & ~15) + 2 * (r & 7) + ((r >> 3) & 1)) + wave_id();
+  if (t < b.T) append_rows<D, E4, NORM>(q, k, Hq, p, b, c, out, t);
 }
 
 template <int D, bool E4>
@@ -275,9 +282,16 @@ static void append_launch(RowsIn q, RowsIn k, RowsIn v, int Hq, const QkPrepArgs
                           const KvArgs& c, RowsOut out, hipStream_t stream) {
   const int pieces = (c.Hkv * (D / 8) + 63) / 64, slots = append_slots(b.T, b.S, E4 ? 16 : 8);
   const int per = kAppendThreads / 64, nv = (slots * pieces + per - 1) / per;
-  const int rows = (b.T + 63) / 64 * 64;
-  hipLaunchKernelGGL((kv_append_kernel<D, E4>), dim3(nv + rows), dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b,
-                     c, out, nv, slots, pieces);
+  const dim3 grid(nv + (b.T + 63) / 64 * 16);
+  if (!p.q_norm)
+    hipLaunchKernelGGL((kv_append_kernel<D, E4, 0>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
+                       nv, slots, pieces);
+  else if (!p.norm_row)
+    hipLaunchKernelGGL((kv_append_kernel<D, E4, 1>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
+                       nv, slots, pieces);
+  else
+    hipLaunchKernelGGL((kv_append_kernel<D, E4, 2>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
+                       nv, slots, pieces);
 }
 
 hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const QkPrepArgs& p, const BatchArgs& b,
