@@ -36,7 +36,8 @@ __device__ __forceinline__ bool append_place(const KvArgs& c, const BatchArgs& b
 
 // Values of one unit group: lanes hold 8 dimensions each, in pieces of 64.
 template <int D, bool E4>
-__device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int n_pos, int slot, int piece) {
+__device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int n_pos, int slot, int piece,
+                              u32x4* lds) {
   constexpr int U = E4 ? 16 : 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
   const int lane = threadIdx.x & 63, chunk = piece * 64 + lane;
   const int s = find_sequence(b.q_start, b.S, slot, U, 2, 1);
@@ -51,23 +52,28 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
   if (lo >= hi || !append_place(c, b, s, lo, n_pos, at)) return;
   long long end = kv_length(c, b, s);
   if (end > n_pos) end = n_pos;
-  if (chunk >= c.Hkv * (D / 8)) return;
-  const int head = chunk / (D / 8), d0 = 8 * (chunk % (D / 8));
+  const int chunks = c.Hkv * (D / 8);
+  const bool mine = chunk < chunks;
+  const int head = mine ? chunk / (D / 8) : 0, d0 = 8 * (chunk % (D / 8));
   u32x4 raw[U];
-  bool all = true;
+  bool all = true;                               // the same for the whole wave
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const long long pos = base + u, row = first + pos - p0;
     const bool in = pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T;
     raw[u] = u32x4{0u, 0u, 0u, 0u};
-    if (in) raw[u] = *reinterpret_cast<const u32x4*>(v.p + (size_t)row * v.stride + 8 * chunk);
+    if (in && mine) raw[u] = *reinterpret_cast<const u32x4*>(v.p + (size_t)row * v.stride + 8 * chunk);
     all = all && in;
   }
   const int in_block = (int)(base & 15);
-  char* dst = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) +
-              (size_t)((in_block / U) * D + d0) * 16;
+  auto unit_of = [&](int h) {                    // the group's first unit of head h
+    return c.v + kv_block_offset<kBlockBytes>(c, at.page, h, at.pos >> 4) + (size_t)(in_block / U) * D * 16;
+  };
   const float sc = E4 ? 1.0f / c.v_scale[head] : 1.0f;
   if (all) {
+    // The lane's 8 units lie side by side.  They go out 64 side by side at a time, by
+    // way of LDS: stores of a lane's own units touch 64 lines each for 16 bytes.  The
+    // places in LDS are turned by the lane so that neither side meets a bank twice.
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       u32x4 w;
@@ -81,10 +87,20 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
           w[q] = (i & 1) ? (a >> 16) | (z & 0xffff0000u) : (a & 0xffffu) | (z << 16);
         }
       }
-      *reinterpret_cast<u32x4*>(dst + 16 * i) = w;
+      lds[8 * lane + (i ^ (lane & 7))] = w;
+    }
+    asm volatile("" ::: "memory");               // the wave's own: its LDS accesses are in order
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int u = 64 * k + lane, l = u >> 3, ch = piece * 64 + l;
+      const u32x4 w = lds[8 * l + ((u & 7) ^ (l & 7))];
+      if (ch < chunks)
+        *reinterpret_cast<u32x4*>(unit_of(ch / (D / 8)) + 16 * (8 * (ch % (D / 8)) + (u & 7))) = w;
     }
     return;
   }
+  if (!mine) return;
+  char* dst = unit_of(head) + 16 * d0;
   // a unit that other tokens share: element by element
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -266,10 +282,12 @@ template <int D, bool E4, int NORM>
 __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
                      int slots, int pieces) {
+  __shared__ u32x4 s_units[kAppendThreads * 8];
   const int blk = blockIdx.x;
   if (blk < nv) {
     const int w = blk * (kAppendThreads / 64) + wave_id();
-    if (w < slots * pieces) append_values<D, E4>(v, b, c, p.n_pos, w / pieces, w % pieces);
+    if (w < slots * pieces)
+      append_values<D, E4>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 512);
     return;
   }
   const int r = blk - nv;
