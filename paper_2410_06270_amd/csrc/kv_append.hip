@@ -13,7 +13,8 @@
 namespace mc {
 
 constexpr int kAppendThreads = 256;
-constexpr int kRowChunks = 8;        // chunks of 8 elements a lane holds at once
+// Chunks of 8 elements that a lane holds at once.
+__host__ __device__ constexpr int row_chunks(int norm) { return norm == 2 ? 8 : 4; }
 
 // The largest number of unit groups that n new tokens from q_start on touch is
 // floor((n + 6) / U) + 1 (U = 8) and fewer for U = 16; sequence s owns the slots from
@@ -121,8 +122,8 @@ __device__ __forceinline__ float square_sum(const u32x4& r) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const float a = half_of(r[q], 0), z = half_of(r[q], 1);
-    s += a * a;
-    s += z * z;
+    s = __builtin_fmaf(a, a, s);
+    s = __builtin_fmaf(z, z, s);
   }
   return s;
 }
@@ -137,13 +138,16 @@ __device__ __forceinline__ float head_sum(float x) {
   return x;
 }
 
-// Queries and keys of one token, by one wave: chunk i of 8 elements in [0, nq + nk),
-// the queries' first, 64 neighbouring ones at a time.  A head's chunks lie in D/8
-// neighbouring lanes, and a lane's chunks all start at the same dimension of their
-// heads, so that its cosines and sines are loaded once for the token.
+// Queries and keys of one token: chunk i of 8 elements in [0, nq + nk), the queries'
+// first, 64 neighbouring ones at a time.  A head's chunks lie in D/8 neighbouring
+// lanes, and a lane's chunks all start at the same dimension of their heads, so that
+// its cosines and sines are loaded once.  A norm over the row needs one wave for the
+// token; without it a wave takes one of its parts of 64 kRowChunks chunks: shorter waves
+// overlap their loads, arithmetic and stores better.
 template <int D, bool E4, int NORM>
 __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, const BatchArgs& b, const KvArgs& c,
-                            RowsOut out, int t) {
+                            RowsOut out, int t, int part) {
+  constexpr int kRowChunks = row_chunks(NORM);
   constexpr int DU = D / 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
   const int lane = threadIdx.x & 63;
   const int nq = q.p ? Hq * DU : 0, total = nq + c.Hkv * DU;
@@ -158,7 +162,7 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
       if (i < total) raw[r] = *reinterpret_cast<const u32x4*>(i < nq ? qr + 8 * i : kr + 8 * (i - nq));
     }
   };
-  load(0);
+  load(64 * kRowChunks * part);
 
   const int s = find_sequence(b.q_start, b.S, t, 1, 0, 1);
   const long long first = b.q_start[s], last = b.q_start[s + 1];
@@ -174,6 +178,13 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < 2 || !p.pairs) tab[i] = *reinterpret_cast<const f32x4*>(from + 4 * i);
+    if (low && !p.pairs) {                       // y_a cos - y_b sin, y_b cos + y_a sin
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        tab[i][1] = -tab[i][1];
+        tab[i][3] = -tab[i][3];
+      }
+    }
   }
   const int partner = turns ? lane + (low ? half / 8 : -(half / 8)) : lane;
 
@@ -202,8 +213,9 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
                                            p.eps);
   }
 
-  for (int i0 = 0; i0 < total; i0 += 64 * kRowChunks) {
-    if (i0) load(i0);
+  const int begin = NORM == 2 ? 0 : 64 * kRowChunks * part, end = NORM == 2 ? total : begin + 64 * kRowChunks;
+  for (int i0 = begin; i0 < end; i0 += 64 * kRowChunks) {
+    if (i0 != begin) load(i0);
 #pragma unroll
     for (int r = 0; r < kRowChunks; ++r) {
       if (i0 + 64 * r >= total) break;           // the same for the whole wave
@@ -227,8 +239,8 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
           for (int j = 0; j < 4; ++j) {
             const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
             const float a = x[2 * j], z = x[2 * j + 1];
-            x[2 * j] = a * co - z * si;
-            x[2 * j + 1] = a * si + z * co;
+            x[2 * j] = __builtin_fmaf(-z, si, a * co);
+            x[2 * j + 1] = __builtin_fmaf(z, co, a * si);
           }
         }
       } else if (p.rot) {
@@ -244,7 +256,7 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
-            x[j] = x[j] * co + (low ? -o[j] : o[j]) * si;
+            x[j] = __builtin_fmaf(o[j], si, x[j] * co);
           }
         }
       }
@@ -274,14 +286,14 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 }
 
 // The first nv workgroups write values (4 waves, each a unit group's piece),
-// the others the queries and keys of 4 tokens, one a wave.  Eight neighbouring tokens
-// share the lines of the key blocks, and workgroups go round the 8 XCDs in turn: of 16
-// row workgroups, number r and r + 8 take 8 neighbouring tokens, so that one XCD's cache
-// sees whole lines.
+// the others queries and keys, 4 neighbouring tokens each, a part of theirs.  Eight
+// neighbouring tokens share the lines of the key blocks, and workgroups go round the 8
+// XCDs in turn: of 16 row workgroups of a part, number r and r + 8 take 8 neighbouring
+// tokens, so that one XCD's cache sees whole lines.
 template <int D, bool E4, int NORM>
 __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
-                     int slots, int pieces) {
+                     int slots, int pieces, int parts) {
   __shared__ u32x4 s_units[kAppendThreads * 8];
   const int blk = blockIdx.x;
   if (blk < nv) {
@@ -290,9 +302,9 @@ __global__ void __launch_bounds__(kAppendThreads)
       append_values<D, E4>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 512);
     return;
   }
-  const int r = blk - nv;
-  const int t = 4 * ((r & ~15) + 2 * (r & 7) + ((r >> 3) & 1)) + wave_id();
-  if (t < b.T) append_rows<D, E4, NORM>(q, k, Hq, p, b, c, out, t);
+  const int r0 = blk - nv, group = r0 / (16 * parts), in = r0 - group * 16 * parts, r = in & 15;
+  const int t = 4 * (16 * group + 2 * (r & 7) + (r >> 3)) + wave_id();
+  if (t < b.T) append_rows<D, E4, NORM>(q, k, Hq, p, b, c, out, t, in >> 4);
 }
 
 template <int D, bool E4>
@@ -300,16 +312,18 @@ static void append_launch(RowsIn q, RowsIn k, RowsIn v, int Hq, const QkPrepArgs
                           const KvArgs& c, RowsOut out, hipStream_t stream) {
   const int pieces = (c.Hkv * (D / 8) + 63) / 64, slots = append_slots(b.T, b.S, E4 ? 16 : 8);
   const int per = kAppendThreads / 64, nv = (slots * pieces + per - 1) / per;
-  const dim3 grid(nv + (b.T + 63) / 64 * 16);
+  const int chunks = ((q.p ? Hq : 0) + c.Hkv) * (D / 8);
+  auto launch = [&](auto kernel, int parts) {
+    hipLaunchKernelGGL(kernel, dim3(nv + (b.T + 63) / 64 * 16 * parts), dim3(kAppendThreads), 0, stream, q, k, v, Hq, p,
+                       b, c, out, nv, slots, pieces, parts);
+  };
+  const int each = 64 * row_chunks(0);
   if (!p.q_norm)
-    hipLaunchKernelGGL((kv_append_kernel<D, E4, 0>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
-                       nv, slots, pieces);
+    launch(kv_append_kernel<D, E4, 0>, (chunks + each - 1) / each);
   else if (!p.norm_row)
-    hipLaunchKernelGGL((kv_append_kernel<D, E4, 1>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
-                       nv, slots, pieces);
+    launch(kv_append_kernel<D, E4, 1>, (chunks + each - 1) / each);
   else
-    hipLaunchKernelGGL((kv_append_kernel<D, E4, 2>), grid, dim3(kAppendThreads), 0, stream, q, k, v, Hq, p, b, c, out,
-                       nv, slots, pieces);
+    launch(kv_append_kernel<D, E4, 2>, 1);
 }
 
 hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const QkPrepArgs& p, const BatchArgs& b,
