@@ -349,12 +349,16 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     }
     if (wave_live) {
       // (the last round's next tile is whatever its buffer holds, and not used)
+      // Where the scores need vector work of their own (settle), the wave with matrix
+      // work goes first: chunks of capped scores 416 -> 366 us; plain ones gain nothing.
+      if (MODE) __builtin_amdgcn_s_setprio(1);
       u32x4 p[4];
       qk(kt, nxt);
       weigh(cur, mul, p);
       pv(vt, p);
       const float mx = largest(nxt);
       interleave<DK, DT>();
+      if (MODE) __builtin_amdgcn_s_setprio(0);
       if (t + 1 < t_end) mul = settle(nxt, mx, tile_key(t + 1));
     }
     // here, and not with the loads: a scalar load under way makes the wait for an
