@@ -421,7 +421,7 @@ typedef struct mc_kv_cache {
 
 typedef struct mc_kv_batch {
   int S, T;                  /* sequences; rows of q, k, v and the outputs */
-  int max_pages;             /* row length of page_table */
+  int max_pages;             /* row length of page_table; max_pages*page at most 2^30 */
   int max_len;               /* host: a length that few sequences exceed, as a hint
                                 for how the work is split; 0 = max_pages*page.
                                 Results do not depend on it beyond rounding */
@@ -478,13 +478,15 @@ typedef struct mc_attention {
   int Hq;                    /* query heads, a multiple of Hkv, up to 256 */
   float scale;               /* finite */
   float softcap;             /* 0: none; else positive */
-  int window;                /* 0: none; else positive */
+  int window;                /* 0: none; else positive (2^30 and more: none) */
   const float *slopes;       /* device [Hq] or NULL */
   const int32_t *prefix;     /* device [S] or NULL */
 } mc_attention;
 
 /* Workspace bytes of mc_attn_decode (T = its S) and mc_attn_prefill; they
- * serve every smaller T too.  Errors: MC_EINVAL, MC_EUNSUPPORTED. */
+ * serve every smaller T too.  A workspace holds nothing from one call to the
+ * next: calls (and replays of captured ones) that run one after another may share
+ * one, calls that may overlap need one each.  Errors: MC_EINVAL, MC_EUNSUPPORTED. */
 mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t *bytes);
 
 /* Attention of one new token a sequence: row s of q at position kv_len[s] - 1
@@ -497,6 +499,7 @@ mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t *bytes);
  * q [S][Hq*D] bf16 and o likewise with their elements between rows (multiples
  * of 8); lse [S][Hq] fp32 or NULL.  The cache is split over its length where
  * the batch is small, the parts joined in a fixed order (deterministic).
+ * Limits: Hq and Hkv as above, S at most MC_MAX_TOKENS, S*Hkv below 2^24.
  * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
 mc_status mc_attn_decode(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
                          const mc_attention *a, uint16_t *o, size_t o_stride, float *lse, void *workspace,
@@ -505,7 +508,8 @@ mc_status mc_attn_decode(const uint16_t *q, size_t q_stride, const mc_kv_batch *
 /* The same for every new token of a ragged batch (prompts, chunks of prompts
  * over what the cache holds already, several tokens of a decoding sequence):
  * q, o [T][Hq*D] and lse [T][Hq] in the batch's rows; rows at a negative
- * position see no key.  Errors as mc_attn_decode. */
+ * position see no key.  Limits: S and T at most MC_MAX_TOKENS, S*Hkv + T*Hq/128
+ * below 2^24.  Errors as mc_attn_decode. */
 mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
                           const mc_attention *a, uint16_t *o, size_t o_stride, float *lse, void *workspace,
                           size_t ws_bytes, void *stream);

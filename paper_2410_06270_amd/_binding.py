@@ -460,6 +460,23 @@ def _here(*tensors) -> int:
     return dev
 
 
+def _here_too(dev: int, *descriptors):
+    """The descriptors' tensors (None and descriptors without any aside) lie on device dev."""
+    for d in descriptors:
+        if d is not None and d.dev is not None and d.dev != dev:
+            raise AssertionError("the descriptors' tensors must be on the current device")
+
+
+def _device_of(*tensors):
+    """The one CUDA device of a descriptor's tensors (None aside; None if there are none)."""
+    found = {t.get_device() for t in tensors if t is not None}
+    assert len(found) <= 1 and -1 not in found, "a descriptor's tensors lie on one GPU"
+    return found.pop() if found else None
+
+
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16)      # bf16, or its bits
+
+
 class KVCache:
     """Device buffers + descriptor of a paged cache (torch-allocated, or the
     given k and v: [n_pages][..] with contiguous pages, which may be slices of
@@ -477,7 +494,7 @@ class KVCache:
         if v is None:
             v = torch.zeros((n_pages, per // e), dtype=dtype, device=device)
         for t in (k, v):
-            assert t.element_size() == e and t.is_cuda and t.shape[0] == n_pages
+            assert t.dtype in ((torch.float8_e4m3fn, torch.uint8) if kind else _BF16) and t.shape[0] == n_pages
             assert t.numel() * e == n_pages * per and t[0].is_contiguous()
         stride = k.stride(0) * e if n_pages > 1 else per
         assert n_pages == 1 or v.stride(0) * e == stride, "k and v differ in their page stride"
@@ -486,6 +503,7 @@ class KVCache:
                 assert t is not None and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == Hkv
         self.n_pages, self.page, self.Hkv, self.D, self.dtype = n_pages, page, Hkv, D, dtype
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.dev = _device_of(k, v, k_scale, v_scale)
         nb = (n_pages - 1) * stride + per
         self.desc = _KVCache(n_pages, page, Hkv, D, kind, k.data_ptr(), v.data_ptr(), stride, nb, nb,
                              k_scale.data_ptr() if k_scale is not None else None,
@@ -501,11 +519,12 @@ class KVBatch:
     def __init__(self, kv_len, page_table, q_start=None, T=None, max_len: int = 0):
         S, max_pages = page_table.shape
         for t in (kv_len, page_table) + (() if q_start is None else (q_start,)):
-            assert t.dtype == torch.int32 and t.is_contiguous() and t.is_cuda
+            assert t.dtype == torch.int32 and t.is_contiguous()
         assert kv_len.numel() == S and (q_start is None or q_start.numel() == S + 1)
         assert q_start is None or T is not None, "q_start comes with T, the number of rows"
         self.S, self.T, self.max_pages = S, S if T is None else int(T), max_pages
         self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
+        self.dev = _device_of(kv_len, page_table, q_start)
         self.desc = _KVBatch(S, self.T, max_pages, int(max_len), None if q_start is None else q_start.data_ptr(),
                              kv_len.data_ptr(), page_table.data_ptr())
         self.ref = ctypes.byref(self.desc)
@@ -521,7 +540,8 @@ class QKPrep:
         if rope is not None:
             assert rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2
         for t in (q_norm, k_norm):
-            assert t is None or (t.element_size() == 2 and t.is_contiguous())
+            assert t is None or (t.dtype in _BF16 and t.is_contiguous())
+        self.dev = _device_of(rope, q_norm, k_norm)
         self.rope, self.q_norm, self.k_norm, self.norm_row = rope, q_norm, k_norm, bool(norm_row)
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self.desc = _QKPrep(ptr(q_norm), ptr(k_norm), int(norm_row), float(eps),
@@ -537,6 +557,7 @@ class Attention:
     def __init__(self, Hq: int, scale: float, softcap: float = 0.0, window: int = 0, slopes=None, prefix=None):
         assert slopes is None or (slopes.dtype == torch.float32 and slopes.is_contiguous() and slopes.numel() == Hq)
         assert prefix is None or (prefix.dtype == torch.int32 and prefix.is_contiguous())
+        self.dev = _device_of(slopes, prefix)
         self.Hq, self.slopes, self.prefix = Hq, slopes, prefix
         self.desc = _Attention(Hq, float(scale), float(softcap), int(window),
                                None if slopes is None else slopes.data_ptr(),
@@ -547,14 +568,15 @@ class Attention:
 def _row_matrix(t, rows: int, width: int):
     """(address, elements between rows) of a bf16 matrix with contiguous rows."""
     s0, s1 = t.stride()
-    assert t.shape == (rows, width) and t.element_size() == 2 and s1 == 1
+    assert t.shape == (rows, width) and t.dtype in _BF16 and s1 == 1
     return t.data_ptr(), s0 if rows > 1 else width
 
 
 def kv_append(q, k, v, prep, batch: KVBatch, cache: KVCache, q_out, stream=None):
     """q [T][Hq*D], k and v [T][Hkv*D], q_out [T][Hq*D]: bf16, rows may be slices
     of wider ones; q and q_out may be None.  prep: QKPrep or None."""
-    dev = _here(q, k, v, q_out, cache.k, batch.kv_len)
+    dev = _here(q, k, v, q_out)
+    _here_too(dev, cache, batch, prep)
     assert batch.q_start is not None
     T, D, kw = batch.T, cache.D, cache.Hkv * cache.D
     qp, qs, op, os_, qw = None, 0, None, 0, D
@@ -580,7 +602,8 @@ def attn_workspace(T: int, Hq: int, Hkv: int, D: int) -> int:
 
 
 def _attn(fn, rows, q, batch, cache, attn, o, workspace, lse, stream):
-    dev = _here(q, o, lse, workspace, cache.k, batch.kv_len)
+    dev = _here(q, o, lse, workspace)
+    _here_too(dev, cache, batch, attn)
     width = attn.Hq * cache.D
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * attn.Hq)
     assert attn.prefix is None or attn.prefix.numel() == batch.S
@@ -611,9 +634,10 @@ def attn_importance(q, lse, batch: KVBatch, cache: KVCache, attn: Attention, x, 
                     importance=None, stream=None):
     """q [L][Hq*D] bf16, lse [L][Hq] float32 (as attn_prefill wrote it), x [L][d] bf16;
     writes the protected mask (uint8 [L]) and, if given, the importance (float32 [L])."""
-    dev = _here(q, lse, x, important, importance, workspace, cache.k, batch.page_table)
+    dev = _here(q, lse, x, important, importance, workspace)
+    _here_too(dev, cache, batch, attn)
     L, d = batch.T, x.shape[1]
-    assert x.shape[0] == L and x.is_contiguous() and x.element_size() == 2
+    assert x.shape[0] == L and x.is_contiguous() and x.dtype in _BF16
     assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == L * attn.Hq
     assert important.dtype == torch.uint8 and important.is_contiguous() and important.numel() == L
     assert importance is None or (importance.dtype == torch.float32 and importance.is_contiguous()

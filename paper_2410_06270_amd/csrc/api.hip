@@ -755,16 +755,25 @@ mc_status check_cache(const mc_kv_cache* c) {
   return MC_OK;
 }
 
-mc_status check_batch(const mc_kv_batch* b, bool ragged) {
+// Positions stay in 31 bits with room for a tile behind the last.
+constexpr long long kMaxPositions = 1 << 30;
+
+mc_status check_table(const mc_kv_batch* b, const mc_kv_cache* c) {
+  if (b->max_pages < 1) return fail(MC_EINVAL, "max_pages=%d must be >= 1", b->max_pages);
+  if ((long long)b->max_pages * c->page > kMaxPositions)
+    return fail(MC_EUNSUPPORTED, "max_pages=%d of %d tokens: above 2^30 positions", b->max_pages, c->page);
+  if (!b->page_table) return fail(MC_EINVAL, "page_table is NULL");
+  return MC_OK;
+}
+
+mc_status check_batch(const mc_kv_batch* b, const mc_kv_cache* c, bool ragged) {
   if (!b) return fail(MC_EINVAL, "batch descriptor is NULL");
   if (b->S < 1 || (ragged && b->T < 1)) return fail(MC_EINVAL, "S=%d and T=%d must be >= 1", b->S, b->T);
   if (b->S > MC_MAX_TOKENS || (ragged && b->T > MC_MAX_TOKENS))
     return fail(MC_EUNSUPPORTED, "S=%d or T=%d above %d", b->S, b->T, MC_MAX_TOKENS);
-  if (b->max_pages < 1 || b->max_len < 0)
-    return fail(MC_EINVAL, "max_pages=%d must be >= 1 and max_len=%d >= 0", b->max_pages, b->max_len);
-  if (!b->kv_len || !b->page_table || (ragged && !b->q_start))
-    return fail(MC_EINVAL, "q_start, kv_len or page_table is NULL");
-  return MC_OK;
+  if (b->max_len < 0) return fail(MC_EINVAL, "max_len=%d must be >= 0", b->max_len);
+  if (!b->kv_len || (ragged && !b->q_start)) return fail(MC_EINVAL, "q_start or kv_len is NULL");
+  return check_table(b, c);
 }
 
 mc_status check_attention(const mc_attention* a, const mc_kv_cache* c) {
@@ -797,21 +806,26 @@ mc::BatchArgs batch_args(const mc_kv_batch* b) {
 }
 
 mc::ScoreArgs score_args(const mc_attention* a, const mc_kv_cache* c) {
-  return {a->Hq, a->Hq / c->Hkv, a->scale, a->softcap, a->window, a->slopes, a->prefix};
+  // a window of all positions is none
+  return {a->Hq, a->Hq / c->Hkv, a->scale, a->softcap, a->window >= kMaxPositions ? 0 : a->window, a->slopes,
+          a->prefix};
 }
 
 int longest(const mc_kv_batch* b, const mc_kv_cache* c) {
   const long long most = (long long)b->max_pages * c->page;
   if (b->max_len > 0 && b->max_len < most) return b->max_len;
-  return (int)std::min<long long>(most, 0x7fffffff);
+  return (int)most;
 }
 
 mc_status check_attn_call(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
                           const mc_attention* a, const uint16_t* o, size_t o_stride, const void* ws, size_t ws_bytes,
                           bool ragged) {
   mc_status s = check_cache(c);
-  if (s == MC_OK) s = check_batch(b, ragged);
+  if (s == MC_OK) s = check_batch(b, c, ragged);
   if (s == MC_OK) s = check_attention(a, c);
+  // a launch holds less than 2^32 threads
+  if (s == MC_OK && (long long)b->S * c->Hkv + (ragged ? (long long)b->T * a->Hq / 128 : 0) >= 1 << 24)
+    s = fail(MC_EUNSUPPORTED, "S*Hkv%s at or above 2^24", ragged ? " + T*Hq/128" : "");
   if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
   if (s == MC_OK) s = check_rows("o", o, o_stride, (size_t)a->Hq * c->D);
   if (s != MC_OK) return s;
@@ -837,7 +851,7 @@ mc_status mc_kv_append(const uint16_t* q, size_t q_stride, const uint16_t* k, si
                        size_t v_stride, int Hq, const mc_qk_prep* prep, const mc_kv_batch* b, const mc_kv_cache* c,
                        uint16_t* q_out, size_t out_stride, void* stream) {
   mc_status s = check_cache(c);
-  if (s == MC_OK) s = check_batch(b, true);
+  if (s == MC_OK) s = check_batch(b, c, true);
   if (s != MC_OK) return s;
   if (Hq < 1 || Hq > 256) return fail(MC_EINVAL, "Hq=%d outside [1, 256]", Hq);
   if (!q != !q_out) return fail(MC_EINVAL, "q and q_out: both or neither");
@@ -920,7 +934,8 @@ mc_status mc_attn_importance(const uint16_t* q, size_t q_stride, const float* ls
   if (!b) return fail(MC_EINVAL, "batch descriptor is NULL");
   if (b->S != 1 || b->T < 1) return fail(MC_EINVAL, "S=%d, T=%d: one sequence of at least one token", b->S, b->T);
   if (b->T > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "T=%d above %d", b->T, MC_MAX_TOKENS);
-  if (!b->page_table) return fail(MC_EINVAL, "page_table is NULL");
+  s = check_table(b, c);
+  if (s != MC_OK) return s;
   if ((long long)b->max_pages * c->page < b->T)
     return fail(MC_EINVAL, "max_pages=%d do not hold %d tokens", b->max_pages, b->T);
   s = check_attention(a, c);

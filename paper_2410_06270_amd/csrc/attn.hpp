@@ -45,9 +45,8 @@ struct SplitArgs {
 
 // The longest length the tables describe, and a sequence's length within it.
 __device__ __forceinline__ int kv_length(const KvArgs& c, const BatchArgs& b, int s) {
-  const long long most = ((long long)b.max_pages << c.lb) * kKvBlock;
-  const long long n = b.kv_len[s];
-  return (int)(n < 0 ? 0 : n > most ? (most > 0x7fffffff ? 0x7fffffff : most) : n);
+  const int most = (b.max_pages << c.lb) * kKvBlock, n = b.kv_len[s];      // most: 2^30 or less
+  return n < 0 ? 0 : n > most ? most : n;
 }
 
 __device__ __forceinline__ int kv_prefix(const ScoreArgs& a, int s, int len) {

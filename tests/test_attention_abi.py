@@ -168,6 +168,22 @@ def test_importance_refusals(b):
         assert importance(b, **kw) == want, kw
 
 
+def test_sizes_beyond_a_launch_or_a_position(b):
+    """Tables of more than 2^30 positions and launches of 2^32 threads are refused; one
+    less is not (it gets as far as the workspace, which is too small)."""
+    for n, want in [((1 << 26) + 1, EUNSUPPORTED), ((1 << 31) - 1, EUNSUPPORTED), (1 << 26, ENOSPACE)]:
+        for which in ("decode", "prefill"):
+            assert call(b, which, bt=batch(b, max_pages=n), ws_bytes=0) == want, (which, n)
+        assert importance(b, bt=batch(b, S=1, T=50, max_pages=n), ws_bytes=0) == want, n
+    assert append(b, bt=batch(b, max_pages=(1 << 26) + 1)) == EUNSUPPORTED
+    assert call(b, "decode", c=cache(b, page=256), bt=batch(b, max_pages=(1 << 22) + 1)) == EUNSUPPORTED
+    c, a = cache(b, Hkv=256), attention(b, Hq=256)
+    for which, S, T, want in [("decode", 65536, 0, EUNSUPPORTED), ("decode", 65535, 0, ENOSPACE),
+                              ("prefill", 65536, 1, EUNSUPPORTED), ("prefill", 65408, 16384, EUNSUPPORTED),
+                              ("prefill", 65407, 16384, ENOSPACE)]:
+        assert call(b, which, c=c, a=a, bt=batch(b, S=S, T=T), qs=16384, os=16384, ws_bytes=0) == want, (which, S, T)
+
+
 def test_size_queries(b):
     lib, n = b.load(), ctypes.c_size_t()
     assert lib.mc_kv_page_bytes(16, 8, 128, 0, ctypes.byref(n)) == 0 and n.value == 16 * 8 * 128 * 2

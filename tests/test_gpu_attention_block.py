@@ -422,3 +422,57 @@ def test_binding_refusals(mc):
         mc.kv_append(q, q, q, None, b, h.cache, o)          # k and v are 64 wide
     with pytest.raises(AssertionError):
         mc.KVCache(4, 16, 1, 64, dtype=E4M3)                 # no scales
+
+
+def test_descriptors_on_one_gpu(mc):
+    """A descriptor's tensors all lie on the device of the call, and rows are bf16."""
+    h = Heads(mc, [32], 2, 1, 64)
+    b = h.batch([32], [2])
+    q = torch.zeros((2, 128), dtype=BF16, device="cuda")
+    ws, f32 = h.workspace(2), dict(dtype=torch.float32)
+    with pytest.raises(AssertionError):
+        mc.attn_prefill(q.half(), b, h.cache, h.attn, q, ws)
+    for bad in (dict(slopes=torch.zeros(2, **f32)), dict(prefix=torch.zeros(1, dtype=torch.int32)),
+                dict(slopes=torch.zeros(2, device="cuda", **f32), prefix=torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(AssertionError):
+            mc.Attention(2, 1.0, **bad)
+    with pytest.raises(AssertionError):
+        mc.KVBatch(i32([32]), h.table.cpu())
+    with pytest.raises(AssertionError):
+        mc.KVBatch(i32([32]), h.table, q_start=torch.tensor([0, 2], dtype=torch.int32), T=2)
+    with pytest.raises(AssertionError):
+        mc.QKPrep(rope=rope_table(4, 64))
+    with pytest.raises(AssertionError):
+        mc.KVCache(2, 16, 1, 64, dtype=E4M3, k_scale=torch.ones(1), v_scale=torch.ones(1, device="cuda"))
+    with pytest.raises(AssertionError):
+        mc.KVCache(2, 16, 1, 64, k=torch.zeros((2, 1024), dtype=torch.float16, device="cuda"))
+
+
+@pytest.mark.parametrize("window", [500, 1 << 30, (1 << 31) - 1])
+def test_windows_of_everything(mc, window):
+    """A window that hides nothing, up to the largest there is, gives what no window gives
+    (of 500 tokens: but for rounding, as the work may be split otherwise)."""
+    L, Hq, Hkv, D = 333, 4, 2, 64
+    outs = []
+    for w in (0, window):
+        h = Heads(mc, [L], Hq, Hkv, D, seed=3, window=w)
+        qkv = torch.randn((L, (Hq + 2 * Hkv) * D), generator=torch.Generator().manual_seed(4)).to(BF16).cuda()
+        q, o = (torch.empty((L, Hq * D), dtype=BF16, device="cuda") for _ in range(2))
+        od = torch.empty((1, Hq * D), dtype=BF16, device="cuda")
+        lse, imp = torch.empty((L, Hq), device="cuda"), torch.empty(L, device="cuda")
+        mask, b = torch.empty(L, dtype=torch.uint8, device="cuda"), h.batch([L], [L])
+        h.append(qkv, b, q)
+        mc.attn_prefill(q, b, h.cache, h.attn, o, h.workspace(L), lse=lse)
+        mc.attn_decode(q[-1:], b, h.cache, h.attn, od, h.workspace(1))
+        x = torch.ones((L, 64), dtype=BF16, device="cuda")
+        ws = torch.empty(mc.attn_importance_workspace(Hq, L), dtype=torch.uint8, device="cuda")
+        mc.attn_importance(q, lse, b, h.cache, h.attn, x, 0.1, mask, ws, importance=imp)
+        torch.cuda.synchronize()
+        outs.append([t.cpu() for t in (o, od, lse, imp, mask)])
+    if window >= 1 << 30:
+        assert all(torch.equal(x, y) for x, y in zip(*outs))
+    else:
+        # on either side the weights' rounding and the output's, each 2^-8 of the largest value
+        far = 4 * 2.0 ** -8 * float(qkv[:, -Hkv * D:].abs().max())
+        for x, y, tol in zip(outs[0], outs[1], (far, far, 1e-5)):
+            assert bool(((x.double() - y.double()).abs() <= tol).all())
