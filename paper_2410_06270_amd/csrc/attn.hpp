@@ -2,6 +2,8 @@
 // arguments, address arithmetic, visibility and number formats.
 #pragma once
 
+#include <type_traits>
+
 #include "mc_internal.hpp"
 
 namespace mc {
@@ -214,13 +216,21 @@ __device__ __forceinline__ float cap_unit(float qk, const ScoreConsts& c) {
   return __builtin_amdgcn_rcpf(1.0f + exp2_fast(qk * c.cap_in));
 }
 
-// MODE: 0 plain, 1 capped, 2 slopes (capped or not); dist = j - i.
+// MODE: bit 0 capped, bit 1 slopes; dist = j - i, a
+// whole number (callers add small ones to one conversion: exact below 2^24).
 template <int MODE>
-__device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float slope2, int dist) {
-  if (MODE == 0) return qk * c.scale2;
-  float s = qk * c.scale2;
-  if (MODE == 1 || c.cap2 > 0.0f) s = __builtin_fmaf(-2.0f * c.cap2, cap_unit(qk, c), c.cap2);
-  return MODE == 1 ? s : s + slope2 * (float)dist;
+__device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float slope2, float dist) {
+  const float s = MODE & 1 ? __builtin_fmaf(-2.0f * c.cap2, cap_unit(qk, c), c.cap2) : qk * c.scale2;
+  return MODE & 2 ? __builtin_fmaf(slope2, dist, s) : s;
+}
+
+// Calls f(integral constant of the call's MODE).
+template <class F>
+void with_score_mode(const ScoreArgs& a, F&& f) {
+  if (a.softcap > 0.0f)
+    a.slopes ? f(std::integral_constant<int, 3>{}) : f(std::integral_constant<int, 1>{});
+  else
+    a.slopes ? f(std::integral_constant<int, 2>{}) : f(std::integral_constant<int, 0>{});
 }
 
 // Joins the parts of every (row, head); ragged: rows outside its sequences are

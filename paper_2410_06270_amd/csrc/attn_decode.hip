@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   float m = kNegInf, l = 0.0f;       // l: of the lane's own keys
   const float kscale = E4 ? c.k_scale[hk] : 1.0f;
   const ScoreConsts sc = score_consts(a.scale * kscale, a.softcap);
-  const float slope2 = MODE == 2 && a.slopes && n < heads ? a.slopes[head0 + n] * kLog2e : 0.0f;
+  const float slope2 = (MODE & 2) && n < heads ? a.slopes[head0 + n] * kLog2e : 0.0f;
 
   auto compute = [&](Step& st, int i) {
     const int key0 = step_blk(i) << 4;
@@ -151,9 +151,10 @@ __global__ void __launch_bounds__(kDecThreads, 2)
     }
     // lane (n, quarter): score (t, r) is of key key0 + 4 KT quarter + 4 t + r
     const int lane_key = key0 + 4 * KT * quarter;
+    const float dist = (float)(lane_key - pos);
     float x[4 * KT];
 #pragma unroll
-    for (int e = 0; e < 4 * KT; ++e) x[e] = score2<MODE>(sv[e / 4][e % 4], sc, slope2, lane_key + e - pos);
+    for (int e = 0; e < 4 * KT; ++e) x[e] = score2<MODE>(sv[e / 4][e % 4], sc, slope2, dist + (float)e);
     const bool whole = (key0 >= wstart && key0 + KS <= len) || key0 + KS <= pre;
     if (!whole) {
       // keys out of sight: weight 0, and values 0 whatever the cache holds there
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
 // 2^(m - M) for itself; then D/4 threads take a part's row, 16 bytes each, the
 // 256 threads 8 (D = 128) or 16 parts at once, and their sums are joined in LDS in a fixed
 // order.  Parts without a visible key have l = 0 and no o.  (A wave for all parts of a
-// row took 56 us for 64 rows of 128 parts, this 8.)
+// (row, head) took 56 us for 64 of them in 128 parts, this 8.)
 constexpr int kJoinThreads = 256;
 
 template <int D>
@@ -373,8 +374,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, i
   if (lse && d == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
 }
 
-// Few parts: D/4 threads a (row, head), 16 bytes of a part each.  (4096 rows of
-// 16 heads in two parts: 78 us by the kernel above, @JOIN2@ by this.)
+// Few parts: D/4 threads a (row, head), 16 bytes of a part each.  (896 rows of
+// 32 heads in two parts: 34.6 us by the kernel above, 9.6 by this.)
 constexpr int kJoinFew = 8;
 
 template <int D>
@@ -453,15 +454,10 @@ template <int D, bool E4>
 static void decode_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                           const SplitArgs& sp, int head_tiles, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)b.S * c.Hkv * head_tiles * sp.nsplit));
-  if (a.slopes)
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 2>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       head_tiles);
-  else if (a.softcap > 0.0f)
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 1>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       head_tiles);
-  else
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, 0>), grid, dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       head_tiles);
+  with_score_mode(a, [&](auto mode) {
+    hipLaunchKernelGGL((attn_decode_kernel<D, E4, decltype(mode)::value>), grid, dim3(kDecThreads), 0, stream, q, b,
+                       c, a, o, lse, sp, head_tiles);
+  });
 }
 
 hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,

@@ -17,8 +17,6 @@
 // lanes' sums are joined once at the end.  The rows are dealt out to `slices` workgroups.
 // attn_finish_kernel: one wave a key: its partial sums, the norm of x_j, I_j and
 // the selection key that importance_select takes.
-#include <type_traits>
-
 #include "attn.hpp"
 
 namespace mc {
@@ -174,13 +172,14 @@ __global__ void __launch_bounds__(kColThreads, 2)
   auto add = [&](auto masked, const f32x16 (&sv)[2], const Tile& t) {
     constexpr bool MASKED = decltype(masked)::value;
     const int row = t.row0 + n, key = key0 + 4 * half;
+    const float dist = (float)(key - row);
     const int low = (a.window > 0 && row >= a.window ? row - a.window : -1) - key, high = (row < L ? row : -1) - key;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = 32 * h + 8 * (r >> 2) + (r & 3);
-        float p = exp2_fast(MODE ? score2<MODE>(sv[h][r], sc, t.slope2, j + key - row) - t.ls
+        float p = exp2_fast(MODE ? score2<MODE>(sv[h][r], sc, t.slope2, dist + (float)j) - t.ls
                                  : __builtin_fmaf(sv[h][r], sc.scale2, -t.ls));
         if (MASKED) p = ((j <= high) & (j > low)) ? p : 0.0f;
         acc[h][r] += p;
@@ -195,7 +194,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
     if (i + kColRing - 1 < count) fetch(nxt);
     Tile t = {32 * ct, 0.0f, 0.0f, false, false};
     if (i < count) {
-      t.slope2 = MODE == 2 && a.slopes ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
+      t.slope2 = MODE & 2 ? a.slopes[hk * a.g + ch] * kLog2e : 0.0f;
       next(ct, ch);
       t.live = t.row0 + 31 >= key0;
       t.masked = !(t.row0 >= key0 + 63 && t.row0 + 32 <= L && (a.window == 0 || t.row0 + 31 - key0 < a.window));
@@ -308,15 +307,10 @@ template <int D, bool E4>
 static void colsum_launch(RowsIn q, const float* lse, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, int L,
                           int slices, float* partial, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)col_tiles(L) * slices * c.Hkv));
-  if (a.slopes)
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 2>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
-                       partial);
-  else if (a.softcap > 0.0f)
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 1>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
-                       partial);
-  else
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, 0>), grid, dim3(kColThreads), 0, stream, q, lse, b, c, a, L, slices,
-                       partial);
+  with_score_mode(a, [&](auto mode) {
+    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, decltype(mode)::value>), grid, dim3(kColThreads), 0, stream, q,
+                       lse, b, c, a, L, slices, partial);
+  });
 }
 
 hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const BatchArgs& b, const KvArgs& c,

@@ -19,8 +19,6 @@
 // row's maximum and sum are in-lane but for one exchange between the half waves,
 // and the score rows are dealt so that the lane's keys are the ones that it
 // supplies to O^T = V^T P^T: the weights never leave their registers.
-#include <type_traits>
-
 #include "attn.hpp"
 
 namespace mc {
@@ -101,7 +99,7 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-// MODE: 0 plain scores, 1 capped ones, 2 slopes (capped or not).
+// MODE: bit 0 capped scores, bit 1 slopes.
 template <int D, bool E4, int MODE>
 __global__ void __launch_bounds__(kPreThreads, 2)
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
@@ -211,7 +209,7 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   float m = kNegInf, l = 0.0f;       // l: of the lane's own keys
   const float kscale = E4 ? c.k_scale[hk] : 1.0f, scale = fabsf(a.scale) * kscale;
   const ScoreConsts sc = score_consts(scale, a.softcap);
-  const float slope2 = MODE == 2 && a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+  const float slope2 = MODE & 2 ? a.slopes[head] * kLog2e : 0.0f;
   // keys of a score tile: row m of the tile is key (m with bits 2 and 3 swapped)
   const int krow = (n & 16) | ((n & 4) << 1) | ((n & 8) >> 1) | (n & 3);
   const int koff = (krow >> 4) * kBlk + (krow & 15) * 16 + half * 256;
@@ -277,10 +275,11 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     if (masked || MODE) {
       const int hkey = key0 + 8 * half;
       const Mask k = {pos - hkey, rlow - hkey, rpre - hkey};
+      const float dist = (float)-k.pos;
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
         const int j = 32 * (e >> 4) + 16 * ((e >> 3) & 1) + (e & 7);
-        sv[e >> 4][e & 15] = score2<MODE>(sv[e >> 4][e & 15], sc, slope2, j - k.pos);
+        sv[e >> 4][e & 15] = score2<MODE>(sv[e >> 4][e & 15], sc, slope2, dist + (float)j);
       }
       if (masked) {
 #pragma unroll
@@ -289,7 +288,7 @@ __global__ void __launch_bounds__(kPreThreads, 2)
           sv[e >> 4][e & 15] = visible(k, j) ? sv[e >> 4][e & 15] : kNegInf;
         }
       }
-      mx = MODE == 1 && !masked ? score2<1>(mx, sc, 0.0f, 0) : largest(sv);
+      mx = MODE == 1 && !masked ? score2<1>(mx, sc, 0.0f, 0.0f) : largest(sv);
     } else {
       mx *= sc.scale2;
     }
@@ -480,15 +479,10 @@ template <int D, bool E4>
 static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                            const SplitArgs& sp, int slots, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)slots * c.Hkv * sp.nsplit));
-  if (a.slopes)
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 2>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       slots);
-  else if (a.softcap > 0.0f)
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 1>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       slots);
-  else
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, 0>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
-                       slots);
+  with_score_mode(a, [&](auto mode) {
+    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, decltype(mode)::value>), grid, dim3(kPreThreads), 0, stream, q, b,
+                       c, a, o, lse, sp, slots);
+  });
 }
 
 hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
