@@ -196,6 +196,16 @@ __device__ __forceinline__ float half_wave_sum(float x) {
   return rows_sum(x);
 }
 
+// The largest over the wave's lanes, and the sum.
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, dpp<0xb1>(x));
+  x = fmaxf(x, dpp<0x4e>(x));
+  x = fmaxf(x, dpp<0x141>(x));
+  x = fmaxf(x, dpp<0x140>(x));
+  return halves_max(rows_max(x));
+}
+__device__ __forceinline__ float wave_sum(float x) { return halves_sum(half_wave_sum(x)); }
+
 // ------------------------------------------------------------------ scores --
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -303,8 +303,9 @@ __global__ void __launch_bounds__(kDecThreads, 2)
 // One workgroup a (row, head).  Every wave finds the parts' factors
 // 2^(m - M) for itself; then D/4 threads take a part's row, 16 bytes each, the
 // 256 threads 8 (D = 128) or 16 parts at once, and their sums are joined in LDS in a fixed
-// order.  Parts without a visible key have l = 0 and no o.  (A wave for all parts of a
-// (row, head) took 56 us for 64 of them in 128 parts, this 8.)
+// order.  Parts without a visible key have l = 0 and no o: what lies in its place is
+// read, so that no load waits for another, and left out.  (A wave for all parts of a
+// (row, head) took 56 us for 64 of them in 128 parts, this 4.7.)
 constexpr int kJoinThreads = 256;
 
 template <int D>
@@ -332,28 +333,27 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, i
     }
     M = fmaxf(M, mv[i]);
   }
-  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  M = wave_max(M);
   const float M0 = M == kNegInf ? 0.0f : M;
   float L = 0.0f;
 #pragma unroll
   for (int i = 0; i < kMaxSplit / 64; ++i) {
     const float f = lv[i] == 0.0f ? 0.0f : exp2_fast(mv[i] - M0);
     L += lv[i] == 0.0f ? 0.0f : lv[i] * f;
-    // -1: no o to read (a factor may itself be 0)
+    // -1: no o (a factor may itself be 0)
     if (threadIdx.x < 64) s_f[lane + 64 * i] = lv[i] == 0.0f ? -1.0f : f;
   }
-  for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
+  L = wave_sum(L);
   __syncthreads();
   const int grp = threadIdx.x / kGroup, d = threadIdx.x % kGroup;
   const float* po = sp.o + (size_t)w * sp.nsplit * D + 4 * d;
   f32x4 r = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
   for (int part = grp; part < sp.nsplit; part += kGroups) {
     const float f = s_f[part];
-    if (f == -1.0f) continue;
     const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)part * D);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+    for (int e = 0; e < 4; ++e) r[e] += f == -1.0f ? 0.0f : v[e] * f;
   }
   s_o[grp][d] = r;
   __syncthreads();
@@ -374,11 +374,13 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, i
   if (lse && d == 0) lse[(size_t)row * Hq + h] = L == 0.0f ? kNegInf : (M0 + __log2f(L)) * kLn2;
 }
 
-// Few parts: D/4 threads a (row, head), 16 bytes of a part each.  (896 rows of
-// 32 heads in two parts: 34.6 us by the kernel above, 9.6 by this.)
+// Few parts, FEW at most: D/4 threads a (row, head), 16 bytes of a part each, all
+// loads at once.  896 rows of 32 heads in two parts: 34.6 us by the kernel above, 11.8 by
+// this for up to 8, 7.9 for 2 (fewer registers, more waves).  One row of 16 heads in 7
+// parts: 6.4 us one part after the other, 2.9 so.
 constexpr int kJoinFew = 8;
 
-template <int D>
+template <int D, int FEW>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(SplitArgs sp, int all, int Hq, int g,
                                                                      const float* __restrict__ v_scale, RowsOut o,
                                                                      float* __restrict__ lse,
@@ -389,21 +391,28 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(SplitArgs s
   const int row = w / Hq, h = w - row * Hq;
   if (q_start && (row < q_start[0] || row >= q_start[S])) return;   // padding
   const float* ml = sp.ml + (size_t)w * sp.nsplit * 2;
-  float M = kNegInf;
-  for (int part = 0; part < sp.nsplit; ++part)
-    if (ml[2 * part + 1] != 0.0f) M = fmaxf(M, ml[2 * part]);
-  const float M0 = M == kNegInf ? 0.0f : M;
   const float* po = sp.o + (size_t)w * sp.nsplit * D + 4 * d;
-  f32x4 r = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.0f;
-  for (int part = 0; part < sp.nsplit; ++part) {
-    const float l = ml[2 * part + 1];
-    if (l == 0.0f) continue;
-    const float f = exp2_fast(ml[2 * part] - M0);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (size_t)part * D);
-    L += l * f;
+  float mv[FEW], lv[FEW], M = kNegInf, L = 0.0f;
+  f32x4 v[FEW], r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] += v[e] * f;
+  for (int i = 0; i < FEW; ++i) {           // all loads first
+    const int part = min(i, sp.nsplit - 1);
+    mv[i] = ml[2 * part];
+    lv[i] = ml[2 * part + 1];
+    if (i < sp.nsplit) v[i] = *reinterpret_cast<const f32x4*>(po + (size_t)part * D);
+  }
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    if (i >= sp.nsplit) lv[i] = 0.0f;
+    M = fmaxf(M, lv[i] == 0.0f ? kNegInf : mv[i]);
+  }
+  const float M0 = M == kNegInf ? 0.0f : M;
+#pragma unroll
+  for (int i = 0; i < FEW; ++i) {
+    const float f = exp2_fast(mv[i] - M0);
+    L += lv[i] == 0.0f ? 0.0f : lv[i] * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] += lv[i] == 0.0f ? 0.0f : v[i][e] * f;
   }
   const float f = L == 0.0f ? 0.0f : (v_scale ? v_scale[h / g] : 1.0f) / L;
   u32x2 out = {0u, 0u};
@@ -423,12 +432,13 @@ hipError_t launch_attn_join(const SplitArgs& sp, int rows, int Hq, int g, int D,
   timing_begin(stream, kSiteAttnJoin);
   if (sp.nsplit <= kJoinFew) {
     const dim3 grid((all + per - 1) / per);
-    if (D == 64)
-      hipLaunchKernelGGL(attn_join_few_kernel<64>, grid, dim3(kJoinThreads), 0, stream, sp, all, Hq, g, v_scale, o, lse,
-                         q_start, S);
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kJoinThreads), 0, stream, sp, all, Hq, g, v_scale, o, lse, q_start, S);
+    };
+    if (sp.nsplit == 2)
+      D == 64 ? launch(attn_join_few_kernel<64, 2>) : launch(attn_join_few_kernel<128, 2>);
     else
-      hipLaunchKernelGGL(attn_join_few_kernel<128>, grid, dim3(kJoinThreads), 0, stream, sp, all, Hq, g, v_scale, o,
-                         lse, q_start, S);
+      D == 64 ? launch(attn_join_few_kernel<64, kJoinFew>) : launch(attn_join_few_kernel<128, kJoinFew>);
   } else if (D == 64) {
     hipLaunchKernelGGL(attn_join_kernel<64>, dim3(all), dim3(kJoinThreads), 0, stream, sp, Hq, g, v_scale, o, lse,
                        q_start, S);

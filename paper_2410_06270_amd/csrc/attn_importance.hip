@@ -291,10 +291,8 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const float
   } else {
     for (int i = lane; i < d; i += 64) n1 += fabsf(bf16_bits_to_float(xr[i]));
   }
-  for (int off = 32; off >= 1; off >>= 1) {
-    cs += __shfl_xor(cs, off);
-    n1 += __shfl_xor(n1, off);
-  }
+  cs = wave_sum(cs);
+  n1 = wave_sum(n1);
   if (lane == 0) {
     const float I = n1 * (cs / (float)Hq) / (float)(L - j);
     if (importance) importance[j] = I;
