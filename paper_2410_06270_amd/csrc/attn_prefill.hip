@@ -30,20 +30,34 @@ constexpr int kPreKeys = 64;                  // keys of a tile
 
 // Row tiles: sequence s owns slots floor(q_start[s] g / 128) + s and on, at
 // least ceil(rows / 128) of them.
-static int prefill_slots(int T, int S, int g) { return (int)((long long)T * g / kPreRows) + S; }
+static int prefill_slots(int T, int S, int g) {
+  return (int)(((long long)T * g + kPreRows - 1) / kPreRows) + S - 1;
+}
 
-// Few row tiles are split over the keys, up to kPreTarget workgroups (two a
-// CU), each with 512 keys at least.
+// Few row tiles are split over the keys, below kPreTarget workgroups (two a
+// CU), each with 512 keys at least.  (Not at one a CU: a wave alone on its SIMD gets 90 %
+// of what two get for heads of 128, and the join would cost more.)
 constexpr int kPreTarget = 512, kPreMaxSplit = 32;
 
 static int prefill_splits(int slots, int Hkv, int max_len) {
-  long long n = kPreTarget / ((long long)slots * Hkv);
+  long long n = (kPreTarget - 1) / ((long long)slots * Hkv);
   const int most = (max_len + 511) / 512;
   n = n > most ? most : n;
   return (int)(n < 1 ? 1 : n > kPreMaxSplit ? kPreMaxSplit : n);
 }
 
-// T g / 128 <= slots and nsplit slots Hkv <= kPreTarget, so a split call has at
+// Heads of 64, whose products are half as long, leave a lone wave waiting for 30 % of its
+// time, and a row tile is as long as its keys are many.  Up to two workgroups a CU that
+// are not split take two teams of waves, each half of the keys, joined in LDS (32 query
+// heads over 8 key-value heads, one prompt of 1024 tokens: 23.1 -> 19.5 us, of 2048: 41.9
+// -> 39.2; chunks of 2048 over 14000 tokens, 16 heads: 272 -> 196); more keep one (4096
+// tokens of 32 heads: 101, with two 128), and so do short ones (256 tokens: 9.7, with two
+// 9.9).  Heads of 128: 4096 tokens of 16 heads 89, with two 93.
+static bool prefill_two_teams(int slots, int Hkv, int nsplit, int max_len) {
+  return nsplit == 1 && (long long)slots * Hkv <= kPreTarget && max_len >= 512;
+}
+
+// T g / 128 <= slots and nsplit slots Hkv < kPreTarget where nsplit > 1, so a split call has at
 // most 128 kPreTarget partial rows.
 size_t attn_prefill_split_rows(int T, int Hq) {
   const size_t all = (size_t)T * Hq * kPreMaxSplit, most = (size_t)kPreRows * kPreTarget;
@@ -63,7 +77,7 @@ template <int D>
 __device__ __forceinline__ bool clean_values(char* vt, int n) {
   uint32_t odd = 0;
 #pragma unroll 1
-  for (int i = threadIdx.x; i < kPreKeys * D / 8; i += kPreThreads) {
+  for (int i = threadIdx.x % kPreThreads; i < kPreKeys * D / 8; i += kPreThreads) {
     // unit i of the tile: block i / (2D), token group (i / D) % 2
     const int over = 16 * (i / (2 * D)) + 8 * ((i / D) & 1) + 8 - n;      // hidden tokens of the unit
     u32x4 w = *reinterpret_cast<u32x4*>(vt + 16 * i);
@@ -100,8 +114,8 @@ __device__ __forceinline__ void interleave() {
 }
 
 // MODE: bit 0 capped scores, bit 1 slopes.
-template <int D, bool E4, int MODE>
-__global__ void __launch_bounds__(kPreThreads, 2)
+template <int D, bool E4, int MODE, int G>
+__global__ void __launch_bounds__(G * kPreThreads, 2)
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                         int slots) {
   constexpr int DT = D / 32, DK = D / 16;      // value tiles; score steps
@@ -110,20 +124,24 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   constexpr int kPieces = kBlockBytes / 1024, kUnit = E4 ? 16 : 8;
   // one array: for several the compiler keeps marks of its own that replace those
   // of the parameters of round() below, and then waits for every load before a read
-  __shared__ __attribute__((aligned(16))) char s_lds[4 * kTileBytes + (E4 ? kPreWaves * 2 * kBlockBytes : 0)];
+  constexpr int kTeamBytes = 4 * kTileBytes + (E4 ? kPreWaves * 2 * kBlockBytes : 0);
+  __shared__ __attribute__((aligned(16))) char s_all[G * kTeamBytes];
+  const int team = G == 1 ? 0 : wave_id() / kPreWaves, wave = wave_id() % kPreWaves;
+  char* const s_lds = s_all + team * kTeamBytes;
   char* const s_k[2] = {s_lds, s_lds + kTileBytes};
   char* const s_v[2] = {s_lds + 2 * kTileBytes, s_lds + 3 * kTileBytes};
-  const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 31, half = lane >> 5;
+  const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   int id = blockIdx.x;
   const int hk = id % c.Hkv;
   id /= c.Hkv;
   const int split = id % sp.nsplit;
   // Later rows see more keys: the later half of the row tiles goes first, from the
   // last on, then the other from the first on, so that where all workgroups are on the chip
-  // at once a CU has a long and a short one (4096 tokens of 16 heads, 528
-  // workgroups: 108 us from the last to the first, 105 so).
+  // at once a CU has a long and a short one (4096 tokens of 16 heads, 512 workgroups: 108
+  // us from the last to the first, 105 so).  Of two teams a CU holds one workgroup, and the
+  // first to end takes the next: from the last to the first (80 us by halves, 68 so).
   const int turn = id / sp.nsplit, later = (slots + 1) / 2;
-  const int slot = turn < later ? slots - 1 - turn : turn - later;
+  const int slot = G > 1 || turn < later ? slots - 1 - turn : turn - later;
   const int s = find_sequence(b.q_start, b.S, slot, kPreRows, 1, a.g);
   int first, count;
   sequence_rows(b, s, first, count);
@@ -171,8 +189,10 @@ __global__ void __launch_bounds__(kPreThreads, 2)
   const int wstart = a.window > 0 && pos_first >= a.window ? pos_first - a.window + 1 : 0;
   int ia = (pre + kPreKeys - 1) / kPreKeys, ib = wstart / kPreKeys;
   if (ib <= ia) ia = ib = 0;
-  const int tiles = max(0, ia + end - ib), per = (tiles + sp.nsplit - 1) / sp.nsplit;
-  const int t_end = min(tiles, (split + 1) * per), t_begin = min(split * per, t_end);
+  const int tiles = max(0, ia + end - ib), per = (tiles + G * sp.nsplit - 1) / (G * sp.nsplit);
+  auto end_of = [&](int tm) { return min(tiles, (split * G + tm + 1) * per); };
+  const int t_end = end_of(team), t_begin = min((split * G + team) * per, t_end);
+  const int rounds = end_of(0) - min(split * G * per, tiles);          // the first team's, no fewer than another's
   const int32_t* pages = b.page_table + (size_t)s * b.max_pages;
   const int last_blk = len > 0 ? (len - 1) >> 4 : 0;
   auto tile_key = [&](int t) { return (t < ia ? t : t - ia + ib) * kPreKeys; };
@@ -346,7 +366,7 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     } else {
       load(t + 2, knext, vnext);
     }
-    if (wave_live) {
+    if (wave_live && (G == 1 || t < t_end)) {
       // (the last round's next tile is whatever its buffer holds, and not used)
       // Where the scores need vector work of their own (settle), the wave with matrix
       // work goes first: chunks of capped scores 416 -> 366 us; plain ones gain nothing.
@@ -370,12 +390,18 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     if constexpr (!E4) wait_vmcnt<0>();
     lds_barrier();
     if constexpr (E4) wait_vmcnt<0>();
-    if (edge(tile_key(t))) {
-      odd = clean_values<D>(vt, len - tile_key(t)) || odd;
+    bool any = false;                                  // a tile of some team
+#pragma unroll
+    for (int tm = 0; tm < G; ++tm) {
+      const int tt = (split * G + tm) * per + t - t_begin;
+      any |= (G == 1 || tt < end_of(tm)) && edge(tile_key(tt));
+    }
+    if (any) {
+      if (G == 1 || (t < t_end && edge(tile_key(t)))) odd = clean_values<D>(vt, len - tile_key(t)) || odd;
       lds_barrier();
     }
   };
-  if (t_begin < t_end) {
+  if (rounds > 0) {
     f32x16 sa[2], sb[2];
     page = page_of(t_begin);
     load(t_begin, s_k[0], s_v[1]);
@@ -398,21 +424,21 @@ __global__ void __launch_bounds__(kPreThreads, 2)
       wait_vmcnt<0>();
     }
     lds_barrier();
-    if (wave_live) {
+    if (wave_live && (G == 1 || t_begin < t_end)) {
       qk(s_k[0], sa);
       mul = settle(sa, largest(sa), tile_key(t_begin));
     }
-    for (int t = t_begin; t < t_end; t += 2) {
+    for (int t = t_begin; t < t_begin + rounds; t += 2) {
       begin_round(s_v[0], t);
       round(s_k[1], s_v[0], s_k[0], s_v[1], sa, sb, t);
-      if (t + 1 == t_end) break;
+      if (t + 1 == t_begin + rounds) break;
       begin_round(s_v[1], t + 1);
       round(s_k[0], s_v[1], s_k[1], s_v[0], sb, sa, t + 1);
     }
     // whether any wave met values that clean_values left out
     lds_barrier();
     const int any_odd = __any(odd) ? 1 : 0;
-    int* flags = reinterpret_cast<int*>(s_k[0]);
+    int* flags = reinterpret_cast<int*>(s_k[0]);       // of the team
     if (lane == 0) flags[wave] = any_odd;
     lds_barrier();
     if (flags[0] | flags[1] | flags[2] | flags[3]) {
@@ -439,6 +465,33 @@ __global__ void __launch_bounds__(kPreThreads, 2)
     }
   }
 
+  if constexpr (G > 1) {
+    // join the teams: a lane of one holds the same row and dimensions as the lane of
+    // the other, whose part comes by way of LDS
+    f32x4* part = reinterpret_cast<f32x4*>(s_all) + wave * (16 * DT / 4 + 1) * 64 + lane;
+    lds_barrier();
+    if (team == 1) {
+      part[0] = f32x4{m, l, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i)
+        part[64 * (i + 1)] = f32x4{acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2],
+                                   acc[i / 4][4 * (i % 4) + 3]};
+    }
+    lds_barrier();
+    if (team == 1) return;
+    const f32x4 ml = part[0];
+    const float M = fmaxf(m, ml[0]);
+    // (a part without a maximum joins one with it at factor 0, and its equal at 1)
+    const float f0 = m == M ? 1.0f : exp2_fast(m - M), f1 = ml[0] == M ? 1.0f : exp2_fast(ml[0] - M);
+    m = M;
+    l = l * f0 + ml[1] * f1;
+#pragma unroll
+    for (int i = 0; i < 4 * DT; ++i) {
+      const f32x4 w = part[64 * (i + 1)];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i / 4][4 * (i % 4) + e] = acc[i / 4][4 * (i % 4) + e] * f0 + w[e] * f1;
+    }
+  }
   l = halves_sum(l);
   if (!live) return;
   const float m0 = m == kNegInf ? 0.0f : m;
@@ -477,11 +530,19 @@ __global__ void __launch_bounds__(kPreThreads, 2)
 
 template <int D, bool E4>
 static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
-                           const SplitArgs& sp, int slots, hipStream_t stream) {
+                           const SplitArgs& sp, int slots, int max_len, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)slots * c.Hkv * sp.nsplit));
   with_score_mode(a, [&](auto mode) {
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, decltype(mode)::value>), grid, dim3(kPreThreads), 0, stream, q, b,
-                       c, a, o, lse, sp, slots);
+    constexpr int MODE = decltype(mode)::value;
+    if constexpr (D == 64) {
+      if (prefill_two_teams(slots, c.Hkv, sp.nsplit, max_len)) {
+        hipLaunchKernelGGL((attn_prefill_kernel<D, E4, MODE, 2>), grid, dim3(2 * kPreThreads), 0, stream, q, b, c, a, o,
+                           lse, sp, slots);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, MODE, 1>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse, sp,
+                       slots);
   });
 }
 
@@ -496,11 +557,11 @@ hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs
   sp.ml = sp.o + (size_t)b.T * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnPrefill);
   if (D == 64)
-    e4 ? prefill_launch<64, true>(q, b, c, a, o, lse, sp, slots, stream)
-       : prefill_launch<64, false>(q, b, c, a, o, lse, sp, slots, stream);
+    e4 ? prefill_launch<64, true>(q, b, c, a, o, lse, sp, slots, max_len, stream)
+       : prefill_launch<64, false>(q, b, c, a, o, lse, sp, slots, max_len, stream);
   else
-    e4 ? prefill_launch<128, true>(q, b, c, a, o, lse, sp, slots, stream)
-       : prefill_launch<128, false>(q, b, c, a, o, lse, sp, slots, stream);
+    e4 ? prefill_launch<128, true>(q, b, c, a, o, lse, sp, slots, max_len, stream)
+       : prefill_launch<128, false>(q, b, c, a, o, lse, sp, slots, max_len, stream);
   timing_end(stream, kSiteAttnPrefill);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;

@@ -358,6 +358,32 @@ def test_prefill_hides_what_it_masks(mc, D, dtype):
         run_attention(mc, w, [140, 100], 4, False, window=window, what="prefill odd")
 
 
+@pytest.mark.parametrize("window,cap,slopes,prefix", [
+    (0, 0.0, False, None), (390, 0.0, False, None), (400, 15.0, True, None), (0, 5.0, False, None),
+    (0, 0.0, True, None), (40, 0.0, False, [0, 1, 7, 64, 900, -3, 5]),
+])
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_prefill_by_teams(mc, window, cap, slopes, prefix, dtype):
+    """Heads of 64 whose lengths are said to be long and that are not split over the keys
+    (512 is one part's): halves of the keys go to two teams, one of which may have none."""
+    lens = [1, 40, 77, 300, 700, 640, 0]
+    new = [1, 40, 30, 300, 150, 3, 2]
+    w = World(mc, lens, Hkv=2, D=64, page=32, dtype=dtype, seed=window)
+    sl = torch.exp2(-torch.arange(1, 7, dtype=torch.float32)) if slopes else None
+    run_attention(mc, w, new, 6, False, window=window, cap=cap, slopes=sl, prefix=prefix, max_len=512, wide=8,
+                  what="prefill by teams")
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_prefill_by_teams_hides_what_it_masks(mc, dtype):
+    inf = math.nan if dtype == E4M3 else math.inf
+    odd = [(0, 3, 0, 5, "v", math.nan), (0, 40, 0, 6, "v", inf), (0, 41, 0, 6, "v", -inf), (0, 90, 1, 33, "v", -inf),
+           (0, 100, 1, 20, "v", inf), (1, 129, 0, 0, "v", inf), (1, 10, 1, 63, "v", math.nan), (1, 128, 1, 3, "k", math.nan)]
+    w = World(mc, [140, 130], Hkv=2, D=64, dtype=dtype, seed=6, odd=odd)
+    for window in (0, 30):
+        run_attention(mc, w, [140, 100], 4, False, window=window, max_len=512, what="prefill by teams, odd")
+
+
 def test_rows_without_keys(mc):
     """More new tokens than the cache holds: rows at negative positions see no key,
     with a prefix too; scores of -infinity alone give no weight either."""
