@@ -17,6 +17,9 @@
  *   mc_moe_route_forward  routing and Eq. 1 in one call
  *   mc_moe_stack_forward  a stack of MoE layers with residual connections
  *   mc_token_importance   Eq. 6 token importance -> the protected set
+ *   mc_kv_append, mc_attn_decode, mc_attn_prefill
+ *                      the blocks' attention over a paged key-value cache
+ *   mc_attn_importance the protected set without an attention map
  *   mc_odp_threshold, mc_pmq_significance, mc_pmq_allocate
  *                      host helpers: the pruning threshold, expert
  *                      significance and the Eq. 4 width allocation

@@ -9,7 +9,9 @@
 // Bound by HBM: every key and value is read once, 4 g operations an element
 // (g query heads share it).  The products are 16x16x32 matrix instructions with up
 // to 16 query heads as their columns; that most columns are empty costs nothing
-// that counts (5 % of the matrix rate at 8 TB/s).
+// that counts (5 % of the matrix rate at 8 TB/s).  48 sequences of 300 to 8191 tokens,
+// 813 MB of bf16: 141 us, 5.8 TB/s; 2 of 50000 to 131071, 380 MB of e4m3: 70 us, 5.4 TB/s.
+// One of 777: 8 us, two launches of three memory latencies each.
 //
 // A wave takes KS keys a step (32 of bf16, 64 of e4m3: 16 KB for D = 128), all
 // of it in registers straight from memory, the next step's loads issued before this
