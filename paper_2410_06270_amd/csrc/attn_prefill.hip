@@ -203,14 +203,23 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   auto tile_key = [&](int t) { return (t < ia ? t : t - ia + ib) * kPreKeys; };
 
   // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each, both
-  // at the same offset.  A page number comes a round before the loads that it is for.
-  auto tile_blk = [&](int t) { return min((tile_key(t) >> 4) + wave, last_blk); };
-  auto page_of = [&](int t) { return uniform_entry(pages, tile_blk(min(t, t_end - 1)) >> c.lb); };
-  auto offset_of = [&](int t, int page) { return kv_block_offset<kBlockBytes>(c, kv_page(c, page), hk, tile_blk(t)); };
+  // at the same offset.  The lanes find the offsets of 64 tiles together, from `known` on.
+  int known = t_begin;
+  uint32_t off_lo = 0, off_hi = 0;
+  auto find_offsets = [&]() {
+    const int blk = min((tile_key(min(known + lane, max(t_end - 1, 0))) >> 4) + wave, last_blk);
+    const size_t off = kv_block_offset<kBlockBytes>(c, kv_page(c, pages[blk >> c.lb]), hk, blk);
+    off_lo = (uint32_t)off;
+    off_hi = (uint32_t)(off >> 32);
+  };
   auto fetch = [&](const char* from, size_t off, char* to) {
-    const char* src = from + off + 16 * lane;
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) lds_dma16(src + 1024 * i, to + 1024 * i);
+    const Buffer src = buffer_of(from + off, kBlockBytes);
+    lds_dma16<0>(src, 16 * lane, to);
+    if constexpr (kPieces > 1) lds_dma16<1024>(src, 16 * lane, to);
+    if constexpr (kPieces > 2) {
+      lds_dma16<2048>(src, 16 * lane, to);
+      lds_dma16<3072>(src, 16 * lane, to);
+    }
   };
   // e4m3: a fetched block's units, widened to bf16 units.  Unit x of the keys is
   // (16 dimensions, token): two bf16 units, 256 bytes apart; of the values (dimension,
@@ -289,16 +298,17 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
             0);
   };
   auto largest = [&](const f32x16 (&sv)[2]) {
-    float mx = kNegInf;
+    float mx[2] = {kNegInf, kNegInf};
 #pragma unroll
-    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, sv[e >> 4][e & 15]);
-    return mx;
+    for (int e = 0; e < 32; ++e) mx[e >> 4] = fmaxf(mx[e >> 4], sv[e >> 4][e & 15]);
+    return fmaxf(mx[0], mx[1]);
   };
   // A tile's scores in place of its products, where it is masked or the score is not
   // a multiple of the product, and the running maximum.  Returns what weigh multiplies by.
-  auto settle = [&](f32x16 (&sv)[2], float mx, int key0) {
-    const bool masked = !((wpos_first >= 0 && key0 + kPreKeys <= pre) ||
-                          (key0 + kPreKeys - 1 <= wpos_first && (a.window == 0 || key0 > wpos_last - a.window)));
+  auto settle = [&](f32x16 (&sv)[2], float mx, int t) {
+    const int key0 = tile_key(t);
+    const bool masked = !(((wpos_first >= 0) & (key0 + kPreKeys <= pre)) |
+                          ((key0 + kPreKeys - 1 <= wpos_first) & ((a.window == 0) | (key0 > wpos_last - a.window))));
     if (masked || MODE) {
       const int hkey = key0 + 8 * half;
       const Mask k = {pos - hkey, rlow - hkey, rpre - hkey};
@@ -333,9 +343,10 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     return mul;
   };
   // a tile with a key that some row of the workgroup does not see
-  auto edge = [&](int key0) {
-    return !((pos_first >= 0 && key0 + kPreKeys <= pre) ||
-             (key0 + kPreKeys - 1 <= pos_first && (a.window == 0 || key0 > pos_last - a.window)));
+  auto edge = [&](int t) {
+    const int key0 = tile_key(t);
+    return !(((pos_first >= 0) & (key0 + kPreKeys <= pre)) |
+             ((key0 + kPreKeys - 1 <= pos_first) & ((a.window == 0) | (key0 > pos_last - a.window))));
   };
 
   // Round t: the scores of tile t + 1 beside the weights of tile t, whose values
@@ -343,7 +354,6 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // work on the other.  Loads: keys of tile t + 2 and values of t + 1 (e4m3: of one
   // more, those of this round being widened).  The buffers are distinct and passed as
   // such: reads of one do not wait for the loads into another.
-  int page = 0, page_tile = 0;                         // of the next tile of keys, and which
   size_t off_v = 0;                                    // of the next tile of values
   float mul = 1.0f;
   bool odd = false;
@@ -353,10 +363,13 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   auto load = [&](int t, char* kt, char* vt) {
     if (t > t_begin && t <= t_end) fetch(c.v, off_v, E4 ? raw_v : vt + wave * kBlk);
     if (t >= t_end) return;
-    const size_t off = offset_of(t, page);
-    page_tile = t + 1;
-    fetch(c.k, off, E4 ? raw_k : kt + wave * kBlk);
-    off_v = off;
+    if (t == known + 64) {
+      known = t;
+      find_offsets();
+    }
+    off_v = (size_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, t - known) << 32 |
+            (uint32_t)__builtin_amdgcn_readlane(off_lo, t - known);
+    fetch(c.k, off_v, E4 ? raw_k : kt + wave * kBlk);
   };
   auto lds_done = [&]() {                              // what was read may be overwritten
     asm volatile("" ::: "memory");
@@ -382,14 +395,12 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
       qk(kt, nxt);
       weigh(cur, mul, p);
       pv(vt, p);
-      const float mx = largest(nxt);
+      float mx = largest(nxt);
+      asm volatile("" : "+v"(mx));                     // here, beside the products, not where it is used
       interleave<DK, DT>();
       if (MODE) __builtin_amdgcn_s_setprio(0);
-      if (t + 1 < t_end) mul = settle(nxt, mx, tile_key(t + 1));
+      if (t + 1 < t_end) mul = settle(nxt, mx, t + 1);
     }
-    // here, and not with the loads: a scalar load under way makes the wait for an
-    // LDS read a wait for all of them
-    page = page_of(page_tile);
   };
   // what the last round loaded is in LDS once every wave's loads are; the barrier
   // also ends every wave's reads of the buffers that this round fills
@@ -401,39 +412,36 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
 #pragma unroll
     for (int tm = 0; tm < G; ++tm) {
       const int tt = (split * G + tm) * per + t - t_begin;
-      any |= (G == 1 || tt < end_of(tm)) && edge(tile_key(tt));
+      any |= (G == 1 || tt < end_of(tm)) && edge(tt);
     }
     if (any) {
-      if (G == 1 || (t < t_end && edge(tile_key(t)))) odd = clean_values<D>(vt, len - tile_key(t)) || odd;
+      if (G == 1 || (t < t_end && edge(t))) odd = clean_values<D>(vt, len - tile_key(t)) || odd;
       lds_barrier();
     }
   };
   if (rounds > 0) {
     f32x16 sa[2], sb[2];
-    page = page_of(t_begin);
+    find_offsets();
     load(t_begin, s_k[0], s_v[1]);
-    page = page_of(page_tile);
     if constexpr (E4) {
       wait_vmcnt<0>();
       widen(raw_k, true, s_k[0] + wave * kBlk);
       lds_done();
     }
     load(t_begin + 1, s_k[1], s_v[0]);
-    page = page_of(page_tile);
     if constexpr (E4) {
       wait_vmcnt<0>();
       if (t_begin + 1 < t_end) widen(raw_k, true, s_k[1] + wave * kBlk);
       widen(raw_v, false, s_v[0] + wave * kBlk);
       lds_done();
       load(t_begin + 2, s_k[0], s_v[1]);
-      page = page_of(page_tile);
     } else {
       wait_vmcnt<0>();
     }
     lds_barrier();
     if (wave_live && (G == 1 || t_begin < t_end)) {
       qk(s_k[0], sa);
-      mul = settle(sa, largest(sa), tile_key(t_begin));
+      mul = settle(sa, largest(sa), t_begin);
     }
     for (int t = t_begin; t < t_begin + rounds; t += 2) {
       begin_round(s_v[0], t);
@@ -454,7 +462,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
 #pragma unroll 1
       for (int i = 0; i < (t_end - t_begin) * kPreKeys; ++i) {
         const int t = t_begin + i / kPreKeys, j = tile_key(t) + i % kPreKeys;
-        if (j >= len || !edge(tile_key(t))) continue;
+        if (j >= len || !edge(t)) continue;
         const int blk = j >> 4, page = kv_page(c, pages[blk >> c.lb]), u = (j & 15) / kUnit;
         const char* vj = c.v + kv_block_offset<kBlockBytes>(c, page, hk, blk) + u * D * 16 + 64 * half +
                          (j % kUnit) * (E4 ? 1 : 2);
