@@ -528,7 +528,8 @@ mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch 
  * q and lse).  a->prefix must be NULL (Eq. 6 is of causal attention).  x [L][d]
  * bf16; importance [L] fp32 may be NULL.  Workspace: mc_attn_importance_workspace.
  * Errors: MC_EINVAL (shape, rho outside [0, 1], NULL or misaligned pointer),
- * MC_ENOSPACE, MC_EUNSUPPORTED (prefix, L above MC_MAX_TOKENS), MC_EHIP. */
+ * MC_ENOSPACE, MC_EUNSUPPORTED (prefix, L above MC_MAX_TOKENS, q_stride above
+ * 2^24), MC_EHIP. */
 mc_status mc_attn_importance_workspace(int Hq, int L, size_t *bytes);
 mc_status mc_attn_importance(const uint16_t *q, size_t q_stride, const float *lse, const mc_kv_batch *b,
                              const mc_kv_cache *c, const mc_attention *a, const uint16_t *x_bf16, int d,

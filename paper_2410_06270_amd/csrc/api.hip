@@ -942,6 +942,8 @@ mc_status mc_attn_importance(const uint16_t* q, size_t q_stride, const float* ls
   if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
   if (s != MC_OK) return s;
   if (a->prefix) return fail(MC_EUNSUPPORTED, "a prefix: Eq. 6 is of causal attention");
+  // 32 rows lie within 31 bits
+  if (q_stride > (size_t)1 << 24) return fail(MC_EUNSUPPORTED, "q: %zu elements between rows, above 2^24", q_stride);
   if (d < 1) return fail(MC_EINVAL, "d=%d must be >= 1", d);
   if (!(rho >= 0.0f && rho <= 1.0f)) return fail(MC_EINVAL, "rho %g outside [0, 1]", (double)rho);
   if (!lse || !x_bf16 || !important || !workspace)

@@ -108,14 +108,15 @@ __global__ void __launch_bounds__(kColThreads, 2)
   int ft = t0 + slice / a.g, fh = slice % a.g;           // the next pair to fetch
   int ct = ft, ch = fh;                                  // the next to work on
   auto fetch = [&](char* slot) {
-    const int row = min(32 * ft + n, L - 1), head = hk * a.g + fh;
-    const uint16_t* src = q.p + (size_t)row * q.stride + (size_t)head * D;
+    const int head = hk * a.g + fh, row = min(n, L - 1 - 32 * ft);      // of the tile
+    const Buffer src = buffer_of(q.p + (size_t)(32 * ft) * q.stride + (size_t)head * D, 0x7fffffff);
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
       const int u = 2 * (D / 64 * wave + i);
-      lds_dma16(src + 8 * (u + half), slot + u * 512);
+      lds_dma16<0>(src, row * (2 * (int)q.stride) + 16 * half, 16 * u, slot + u * 512);
     }
-    lds_dma4(lse + (size_t)row * a.Hq + head, slot + kRowBytes + 256 * wave);
+    lds_dma4(buffer_of(lse + (size_t)(32 * ft) * a.Hq + head, 0x7fffffff), row * (4 * a.Hq),
+             slot + kRowBytes + 256 * wave);
     next(ft, fh);
   };
 

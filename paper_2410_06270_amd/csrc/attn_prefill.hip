@@ -214,11 +214,11 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   };
   auto fetch = [&](const char* from, size_t off, char* to) {
     const Buffer src = buffer_of(from + off, kBlockBytes);
-    lds_dma16<0>(src, 16 * lane, to);
-    if constexpr (kPieces > 1) lds_dma16<1024>(src, 16 * lane, to);
+    lds_dma16<0>(src, 16 * lane, 0, to);
+    if constexpr (kPieces > 1) lds_dma16<1024>(src, 16 * lane, 0, to);
     if constexpr (kPieces > 2) {
-      lds_dma16<2048>(src, 16 * lane, to);
-      lds_dma16<3072>(src, 16 * lane, to);
+      lds_dma16<2048>(src, 16 * lane, 0, to);
+      lds_dma16<3072>(src, 16 * lane, 0, to);
     }
   };
   // e4m3: a fetched block's units, widened to bf16 units.  Unit x of the keys is

@@ -108,7 +108,7 @@ __device__ __forceinline__ void lds_dma4(const void* src, void* dst) {
 }
 
 // The same from a buffer: `bytes` at a wave-uniform address, read at OFF (below 4096)
-// plus each lane's own offset, to dst + OFF + 16*l.  Global direct loads make the compiler
+// plus each lane's own offset and a uniform one, to dst + OFF + 16*l (or 4*l).  Global direct loads make the compiler
 // wait for every LDS read under way wherever it waits for one; these do not.
 typedef __amdgpu_buffer_rsrc_t Buffer;
 
@@ -117,8 +117,13 @@ __device__ __forceinline__ Buffer buffer_of(const void* p, int bytes) {
 }
 
 template <int OFF>
-__device__ __forceinline__ void lds_dma16(Buffer src, int offset, void* dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, offset, 0, OFF, 0);
+__device__ __forceinline__ void lds_dma16(Buffer src, int offset, int uniform, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, offset, uniform, OFF,
+                                           0);
+}
+
+__device__ __forceinline__ void lds_dma4(Buffer src, int offset, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, offset, 0, 0, 0);
 }
 
 // ------------------------------------------------------------------ layout --

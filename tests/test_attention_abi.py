@@ -184,6 +184,11 @@ def test_sizes_beyond_a_launch_or_a_position(b):
         assert call(b, which, c=c, a=a, bt=batch(b, S=S, T=T), qs=16384, os=16384, ws_bytes=0) == want, (which, S, T)
 
 
+def test_importance_row_stride(b):
+    for qs, want in [((1 << 24) + 8, EUNSUPPORTED), (1 << 24, ENOSPACE)]:
+        assert importance(b, qs=qs, ws_bytes=0) == want, qs
+
+
 def test_size_queries(b):
     lib, n = b.load(), ctypes.c_size_t()
     assert lib.mc_kv_page_bytes(16, 8, 128, 0, ctypes.byref(n)) == 0 and n.value == 16 * 8 * 128 * 2
