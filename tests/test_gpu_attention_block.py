@@ -476,3 +476,33 @@ def test_windows_of_everything(mc, window):
         far = 4 * 2.0 ** -8 * float(qkv[:, -Hkv * D:].abs().max())
         for x, y, tol in zip(outs[0], outs[1], (far, far, 1e-5)):
             assert bool(((x.double() - y.double()).abs() <= tol).all())
+
+
+def test_capped_products_past_fp32(mc):
+    """A product that overflows fp32 scores at the cap, below as above, in tiles that
+    every row sees and in masked ones, and hidden keys stay hidden."""
+    D, page, L, cap = 64, 16, 200, 4.0
+    gen = torch.Generator().manual_seed(12)
+    k, v = (torch.randn((13, page * D), generator=gen).to(BF16) for _ in range(2))
+    table = torch.arange(13, dtype=torch.int32).view(1, -1)
+    flat = k.view(-1)
+    for pos, sign in ((3, 1.0), (20, -1.0), (100, -1.0), (150, 1.0), (190, -1.0), (199, -1.0)):
+        for i in range(D):
+            flat[oa.offset("k", pos // page, 0, pos % page, i, page, 1, D, 8)] = sign * 2.0 ** 126
+    kk = oa.read("k", flat, table[0], L, 0, page, 1, D, 8)
+    vv = oa.read("v", v.reshape(-1), table[0], L, 0, page, 1, D, 8)
+    q = (4 + torch.rand((L, D), generator=gen)).to(BF16)
+    cache = mc.KVCache(13, page, 1, D, k=k.cuda(), v=v.cuda())
+    at = mc.Attention(1, 1.0, softcap=cap)
+    b = mc.KVBatch(i32([L]), table.cuda(), q_start=i32([0, L]), T=L)
+    o, od = (torch.empty((n, D), dtype=BF16, device="cuda") for n in (L, 1))
+    ws = torch.empty(mc.attn_workspace(L, 1, 1, D), dtype=torch.uint8, device="cuda")
+    mc.attn_prefill(q.cuda(), b, cache, at, o, ws)
+    mc.attn_decode(q[-1:].cuda(), b, cache, at, od, ws)
+    torch.cuda.synchronize()
+    ro, _, _, _ = oa.attend(q.double(), kk, vv, torch.arange(L), scale=1.0, cap=cap)
+    # the weights' rounding and the output's, 2^-8 of the largest value each; the scores,
+    # of which a product past 100 caps moves none, add less than a third such part
+    tol = 3 * 2.0 ** -8 * float(v.float().abs().max())
+    assert bool(((o.cpu().double() - ro).abs() <= tol).all())
+    assert bool(((od.cpu().double() - ro[-1:]).abs() <= tol).all())
