@@ -101,20 +101,21 @@ __device__ __forceinline__ bool clean_values(char* vt, int n) {
   return odd != 0;
 }
 
-// The order of a round's instructions: LDS reads kReadAhead matrix instructions
-// before their use, and the vector work spread over the spaces between all of them: the
-// first products with the values need only the first weights.
-constexpr int kReadAhead = 5;
-
+// The order of a round's instructions: LDS reads some matrix instructions before their
+// use, and the vector work (some 135 instructions) spread over the spaces between all of
+// them: the first products with the values need only the first weights.  Heads of 128, 32
+// products: 3 instructions a space (8192 tokens of 32 heads over 8: 551 us, with 4 559 and
+// with 5 567); of 64, 16 products: 10 and reads 3 ahead (2048 tokens over 14000 187 us,
+// with 8 and 5 ahead 192).
 template <int DK, int DT>
 __device__ __forceinline__ void interleave() {
-  constexpr int kMfmas = 2 * DK + 4 * DT;
+  constexpr int kMfmas = 2 * DK + 4 * DT, kReadAhead = DT == 2 ? 3 : 5, kVector = DT == 2 ? 10 : 3;
   __builtin_amdgcn_sched_group_barrier(0x100, kReadAhead, 0);      // LDS reads
 #pragma unroll
   for (int i = 0; i < kMfmas; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);             // matrix
     if (i + kReadAhead < kMfmas) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, 128 / kMfmas, 0);  // vector
+    __builtin_amdgcn_sched_group_barrier(0x002, kVector, 0);  // vector
   }
 }
 
@@ -388,9 +389,10 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     }
     if (wave_live && (G == 1 || t < t_end)) {
       // (the last round's next tile is whatever its buffer holds, and not used)
-      // Where the scores need vector work of their own (settle), the wave with matrix
-      // work goes first: chunks of capped scores 416 -> 366 us; plain ones gain nothing.
-      if (MODE) __builtin_amdgcn_s_setprio(1);
+      // The wave with matrix work goes first: chunks of capped scores 416 -> 366 us, 8192
+      // tokens of e4m3 576 -> 558; plain scores of heads of 64 gain nothing.
+      constexpr bool kFirst = MODE || D == 128;
+      if (kFirst) __builtin_amdgcn_s_setprio(1);
       u32x4 p[4];
       qk(kt, nxt);
       weigh(cur, mul, p);
@@ -398,7 +400,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
       float mx = largest(nxt);
       asm volatile("" : "+v"(mx));                     // here, beside the products, not where it is used
       interleave<DK, DT>();
-      if (MODE) __builtin_amdgcn_s_setprio(0);
+      if (kFirst) __builtin_amdgcn_s_setprio(0);
       if (t + 1 < t_end) mul = settle(nxt, mx, t + 1);
     }
   };
