@@ -205,6 +205,8 @@ __global__ void __launch_bounds__(kColThreads, 2)
       t.ls = v == kNegInf ? -kNegInf : v * kLog2e;       // a row without keys: every probability 0
     }
     if (t.live && prev.live && !prev.masked) {
+      // the wave with matrix work goes first (4096 tokens of 32 heads over 8: 109 -> 102 us)
+      __builtin_amdgcn_s_setprio(1);
       qk(cur, sv);
       add(std::false_type{}, sp, prev);
       // LDS reads ahead of their products, and between the products the vector work
@@ -215,6 +217,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
         if (m & 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, 96 / (2 * DK), 0);
       }
+      __builtin_amdgcn_s_setprio(0);
     } else {
       if (t.live) qk(cur, sv);
       if (prev.live) {
