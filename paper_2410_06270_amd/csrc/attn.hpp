@@ -62,12 +62,6 @@ __device__ __forceinline__ int kv_page(const KvArgs& c, int p) {
   return p < 0 ? 0 : p >= c.n_pages ? c.n_pages - 1 : p;
 }
 
-// An entry of a device array that no kernel in flight writes, at a wave-uniform
-// index: a scalar load, which waits for no vector load before it.
-__device__ __forceinline__ int32_t uniform_entry(const int32_t* p, int i) {
-  return ((const __attribute__((address_space(4))) int32_t*)p)[__builtin_amdgcn_readfirstlane(i)];
-}
-
 // Byte offset of block `blk` (a position / 16) of head h, on page p, the block
 // being BYTES long.
 template <int BYTES>
@@ -115,6 +109,27 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));     // lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// ----------------------------------------------------------- direct loads --
+// 16 or 4 bytes a lane to LDS from a buffer, `bytes` at a wave-uniform address: read at
+// OFF (below 4096) plus the lane's own offset and a uniform one, to dst + OFF + 16 l (or dst
+// + 4 l), counted by vmcnt.  Global direct loads (lds_dma16 of an address) make the
+// compiler wait for every LDS read under way wherever it waits for one; these do not.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+
+__device__ __forceinline__ Buffer buffer_of(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+
+template <int OFF>
+__device__ __forceinline__ void lds_dma16(Buffer src, int offset, int uniform, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, offset, uniform, OFF,
+                                           0);
+}
+
+__device__ __forceinline__ void lds_dma4(Buffer src, int offset, void* dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, offset, 0, 0, 0);
 }
 
 // ----------------------------------------------------------------- formats --

@@ -9,8 +9,8 @@
 // and one exponential a pair.  Bound by the vector units: 16 pairs a lane of a 32 x 32
 // tile cost 8 matrix instructions (256 cycles of a SIMD for D = 128) and 16 x (an
 // exponential, a multiply-add and an add: 24 cycles).  4096 tokens of 32 query heads over
-// 8: 104 us in all, what reading the lower half of a map takes alone (0.54 GB); 0.76
-// PFLOP/s in the sums' kernel; 16384 tokens: 0.95 PFLOP/s.
+// 8: 97 us in all, what reading the lower half of a map takes alone (0.54 GB); 0.82
+// PFLOP/s in the sums' kernel; 16384 tokens: 0.99 PFLOP/s.
 //
 // attn_colsum_kernel: a workgroup keeps 256 keys of one key-value head in
 // registers (64 a wave) and walks the rows below the diagonal, 32 at a time, of each of

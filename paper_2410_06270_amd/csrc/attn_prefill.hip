@@ -4,18 +4,18 @@
 //   o_i = sum_j p_ij v_j / l_i,  p_ij = exp2(s_ij - m_i),  l_i = sum_j p_ij
 // in one pass over the keys with a running maximum m_i for each row.
 //
-// Bound by the matrix units and the vector units together: a wave's 32 rows x 64 keys
-// cost 32 matrix instructions of 32x32x16 for D = 128 (1024 cycles of a SIMD), and 32
-// exponentials and some 140 other vector instructions a lane (1070 cycles).  Each wave
-// has both in every round, the vector work of one tile beside the products of the next;
-// the two waves of a SIMD overlap no better than that: products take 0.43 of the time,
-// vector work as much.  8192 tokens of 32 query heads over 8: 540 us, 1.02 PFLOP/s (the
-// library's product of two 8192 x 8192 matrices reaches 1.19); 4096 of 16 heads: 88 us,
-// 0.78, where late row tiles end alone.
+// Bound by the matrix units, and by the vector units beside them: a wave's 32 rows x 64
+// keys cost 32 matrix instructions of 32x32x16 for D = 128 (1024 cycles of a SIMD), and 32
+// exponentials and some 105 other vector instructions (800 cycles).  Each wave has both in
+// every round, the vector work of one tile beside the products of the next.  8192 tokens
+// of 32 query heads over 8: 535 us, 1.03 PFLOP/s (the library's product of two 8192 x
+// 8192 matrices reaches 1.19, and this loop with nothing but its products 1.33: the
+// clock falls under matrix load); 4096 of 16 heads: 84 us, 0.82, matrix units busy half of
+// the time, as late row tiles end alone.
 //
-// A workgroup of four waves (or two teams of four, each half of the keys) takes 128 rows of one sequence and key-value head;
-// the g query heads that share it are packed into the rows (row = token * g +
-// head), so a short chunk fills a tile with heads and a tile's rows span few
+// A workgroup of four waves (or two teams of four, each half of the keys) takes 128
+// rows of one sequence and key-value head; the g query heads that share it are packed into
+// the rows (row = token * g + head), so a short chunk fills a tile with heads and a tile's rows span few
 // positions.  Keys and values come through LDS in tiles of 64, two buffers;
 // the cache's 16-byte units are already the order in which the matrix
 // instructions read them, so a bf16 tile is copied straight to LDS by direct

@@ -101,31 +101,6 @@ __device__ __forceinline__ void lds_dma16(const void* src, void* dst) {
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// The same with 4 bytes a lane, to dst + 4*l.
-__device__ __forceinline__ void lds_dma4(const void* src, void* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
-}
-
-// The same from a buffer: `bytes` at a wave-uniform address, read at OFF (below 4096)
-// plus each lane's own offset and a uniform one, to dst + OFF + 16*l (or 4*l).  Global direct loads make the compiler
-// wait for every LDS read under way wherever it waits for one; these do not.
-typedef __amdgpu_buffer_rsrc_t Buffer;
-
-__device__ __forceinline__ Buffer buffer_of(const void* p, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
-}
-
-template <int OFF>
-__device__ __forceinline__ void lds_dma16(Buffer src, int offset, int uniform, void* dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, offset, uniform, OFF,
-                                           0);
-}
-
-__device__ __forceinline__ void lds_dma4(Buffer src, int offset, void* dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, offset, 0, 0, 0);
-}
-
 // ------------------------------------------------------------------ layout --
 // Lane l of a 16x128 tile holds, for MFMA step u (32 columns) and register v
 // (0..3), the codes of columns 32u + 8*(l/16) + 2v (low half) and +1 (high
