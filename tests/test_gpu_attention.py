@@ -358,6 +358,15 @@ def test_prefill_hides_what_it_masks(mc, D, dtype):
         run_attention(mc, w, [140, 100], 4, False, window=window, what="prefill odd")
 
 
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (64, E4M3), (128, BF16), (128, E4M3)])
+@pytest.mark.parametrize("max_len,window", [(1, 0), (512, 0), (1, 5000), (0, 0)])
+def test_prefill_long(mc, D, dtype, max_len, window):
+    """More than 64 and more than 128 tiles of keys for one workgroup, of two sequences."""
+    lens, new = [9001, 4160], [33, 1]
+    w = World(mc, lens, Hkv=1, D=D, page=16, dtype=dtype, seed=D)
+    run_attention(mc, w, new, 2, False, window=window, max_len=max_len, what="prefill long")
+
+
 @pytest.mark.parametrize("window,cap,slopes,prefix", [
     (0, 0.0, False, None), (390, 0.0, False, None), (400, 15.0, True, None), (0, 5.0, False, None),
     (0, 0.0, True, None), (40, 0.0, False, [0, 1, 7, 64, 900, -3, 5]),
