@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     lds_dma16<0>(src, 16 * lane, 0, to);
     if constexpr (kPieces > 1) lds_dma16<1024>(src, 16 * lane, 0, to);
     if constexpr (kPieces > 2) {
-      lds_dma16<2048>(src, 16 * lane, 0, to);
-      lds_dma16<3072>(src, 16 * lane, 0, to);
+      lds_dma16<2 * 1024>(src, 16 * lane, 0, to);
+      lds_dma16<3 * 1024>(src, 16 * lane, 0, to);
     }
   };
   // e4m3: a fetched block's units, widened to bf16 units.  Unit x of the keys is
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // Round t: the scores of tile t + 1 beside the weights of tile t, whose values
   // then are added up: the matrix units work on one tile while the vector units
   // work on the other.  Loads: keys of tile t + 2 and values of t + 1 (e4m3: of one
-  // more, those of this round being widened).  The buffers are distinct and passed as
+  // more, the ones before being widened).  The buffers are distinct and passed as
   // such: reads of one do not wait for the loads into another.
   size_t off_v = 0;                                    // of the next tile of values
   float mul = 1.0f;
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     }
   };
   // what the last round loaded is in LDS once every wave's loads are; the barrier
-  // also ends every wave's reads of the buffers that this round fills
+  // also ends every wave's reads of the buffers that are filled next
   auto begin_round = [&](char* vt, int t) {
     if constexpr (!E4) wait_vmcnt<0>();
     lds_barrier();
