@@ -234,7 +234,9 @@ struct ScoreConsts {
 };
 
 __device__ __forceinline__ ScoreConsts score_consts(float scale, float softcap) {
-  return {scale * kLog2e, softcap * kLog2e, softcap > 0.0f ? 2.0f * kLog2e * (scale / softcap) : 0.0f};
+  // (kept finite, so that a product of 0 stays 0 however small the cap)
+  const float in = softcap > 0.0f ? 2.0f * kLog2e * (scale / softcap) : 0.0f;
+  return {scale * kLog2e, softcap * kLog2e, fminf(fmaxf(in, -3.0e38f), 3.0e38f)};
 }
 
 __device__ __forceinline__ float cap_unit(float qk, const ScoreConsts& c) {

@@ -506,3 +506,33 @@ def test_capped_products_past_fp32(mc):
     tol = 3 * 2.0 ** -8 * float(v.float().abs().max())
     assert bool(((o.cpu().double() - ro).abs() <= tol).all())
     assert bool(((od.cpu().double() - ro[-1:]).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("cap", [1e-30, 1e-42])
+def test_smallest_caps(mc, cap):
+    """Scores within a cap that is next to nothing are next to nothing, a product of 0
+    among them: every row is the mean of the values it sees."""
+    D, page, L = 64, 16, 100
+    gen = torch.Generator().manual_seed(13)
+    k, v = (torch.randn((7, page * D), generator=gen).to(BF16) for _ in range(2))
+    vv = oa.read("v", v.reshape(-1), torch.arange(7, dtype=torch.int32), L, 0, page, 1, D, 8)
+    q = torch.randn((L, D), generator=gen).to(BF16)
+    q[50] = 0
+    q[-1] = 0
+    cache = mc.KVCache(7, page, 1, D, k=k.cuda(), v=v.cuda())
+    at = mc.Attention(1, 1.0, softcap=cap)
+    b = mc.KVBatch(i32([L]), torch.arange(7, dtype=torch.int32).view(1, -1).cuda(), q_start=i32([0, L]), T=L)
+    o, od = (torch.empty((n, D), dtype=BF16, device="cuda") for n in (L, 1))
+    lse = torch.empty((L, 1), device="cuda")
+    ws = torch.empty(mc.attn_workspace(L, 1, 1, D), dtype=torch.uint8, device="cuda")
+    mc.attn_prefill(q.cuda(), b, cache, at, o, ws, lse=lse)
+    mc.attn_decode(q[-1:].cuda(), b, cache, at, od, ws)
+    torch.cuda.synchronize()
+    n = torch.arange(1, L + 1, dtype=torch.float64)[:, None]
+    want = vv.cumsum(0) / n
+    # weights of 1 are exact in bf16: the sums (100 terms) and the output's rounding
+    tol = 2.0 ** -8 * want.abs() + 200 * 2.0 ** -24 * vv.abs().amax()
+    assert bool(((o.cpu().double() - want).abs() <= tol).all())
+    assert bool(((od.cpu().double() - want[-1:]).abs() <= tol[-1:]).all())
+    # exp, sum and logarithm in fp32: some roundings of a value below 5
+    assert bool(((lse.cpu().double() - n.log()).abs() <= 8 * 2.0 ** -24 * 5).all())
