@@ -480,7 +480,9 @@ mc_status mc_kv_append(const uint16_t *q, size_t q_stride, const uint16_t *k, si
 typedef struct mc_attention {
   int Hq;                    /* query heads, a multiple of Hkv, up to 256 */
   float scale;               /* finite */
-  float softcap;             /* 0: none; else positive */
+  float softcap;             /* 0: none; else positive, up to 2^126.  Capped scores are
+                                off by some 2^-22 softcap at most up to 64, above that by
+                                some 2^-19 of themselves */
   int window;                /* 0: none; else positive (2^30 and more: none) */
   const float *slopes;       /* device [Hq] or NULL */
   const int32_t *prefix;     /* device [S] or NULL */

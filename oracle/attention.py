@@ -50,6 +50,16 @@ def write(which, flat, pages, pos, h, rows, page, Hkv, D, U):
     flat.view(raw)[at.reshape(-1)] = rows.contiguous().view(raw).reshape(-1)
 
 
+def cap_error(s, cap):
+    """What fp32 may add to capped scores s.  Caps to 64: cap - 2 cap u with u = 1 / (1 + e), e =
+    exp(2 x / cap), is off by some 2^-23 cap whatever the score.  Above, the error is relative:
+    from |x| = cap / 4 on cap (1 - 2 u), where e is off by 2 + 8 |x / cap| half steps (one step
+    of exp2, 4 roundings in its argument), u by 1 - u of that and 3 (the sum, one step of the
+    reciprocal), which is 5.6 of 1 - 2 u = 0.245 at x = -cap / 4, 23 half steps, and falls
+    from there; 4 more are 1 - 2 u, the cap in the log2 domain and their product."""
+    return 8 * U24 * cap if cap <= 64 else 28 * U24 * s.abs()
+
+
 def scores(q, k, pos, scale, cap=0.0, window=0, slope=0.0, prefix=0):
     """(s [R][n] with -inf where a key is hidden, bound [R] on the fp32 error of a
     visible score).  The product's D terms, the scaling to the log2 domain, a
@@ -60,7 +70,7 @@ def scores(q, k, pos, scale, cap=0.0, window=0, slope=0.0, prefix=0):
     err = (D + 6) * U24 * mag
     if cap:
         z = cap * torch.tanh(z / cap)
-        err = err + 8 * U24 * cap
+        err = err + cap_error(z, cap)
     j = torch.arange(n)[None]
     i = torch.as_tensor(pos)[:, None]
     if slope:

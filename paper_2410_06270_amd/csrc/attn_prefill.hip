@@ -119,7 +119,7 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-// MODE: bit 0 capped scores, bit 1 slopes.
+// MODE: as score2 (attn.hpp).
 template <int D, bool E4, int MODE, int G>
 __global__ void __launch_bounds__(G * kPreThreads, 2)
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
           sv[e >> 4][e & 15] = visible(k, j) ? sv[e >> 4][e & 15] : kNegInf;
         }
       }
-      mx = MODE == 1 && !masked ? score2<1>(mx, sc, 0.0f, 0.0f) : largest(sv);
+      mx = (MODE & 1) && !(MODE & 2) && !masked ? score2<MODE>(mx, sc, 0.0f, 0.0f) : largest(sv);
     } else {
       mx *= sc.scale2;
     }
