@@ -479,7 +479,8 @@ mc_status mc_kv_append(const uint16_t *q, size_t q_stride, const uint16_t *k, si
  * h / (Hq / Hkv). */
 typedef struct mc_attention {
   int Hq;                    /* query heads, a multiple of Hkv, up to 256 */
-  float scale;               /* finite */
+  float scale;               /* finite, of at most 2^126 (and so with an e4m3 cache's
+                                k_scale[h] times it) */
   float softcap;             /* 0: none; else positive, up to 2^126.  Capped scores are
                                 off by some 2^-22 softcap at most up to 64, above that by
                                 some 2^-19 of themselves */

@@ -782,8 +782,9 @@ mc_status check_attention(const mc_attention* a, const mc_kv_cache* c) {
     return fail(MC_EINVAL, "Hq=%d: a multiple of Hkv=%d up to 256", a->Hq, c->Hkv);
   if (!std::isfinite(a->scale) || !(a->softcap >= 0.0f) || !std::isfinite(a->softcap))
     return fail(MC_EINVAL, "scale %g and softcap %g: finite, softcap >= 0", (double)a->scale, (double)a->softcap);
-  // the kernels hold it times log2(e)
-  if (a->softcap > mc::kScoreMost) return fail(MC_EUNSUPPORTED, "softcap %g above 2^126", (double)a->softcap);
+  // the kernels hold both times log2(e)
+  if (a->softcap > mc::kScoreMost || std::fabs(a->scale) > mc::kScoreMost)
+    return fail(MC_EUNSUPPORTED, "scale %g or softcap %g beyond 2^126", (double)a->scale, (double)a->softcap);
   if (a->window < 0) return fail(MC_EINVAL, "window=%d must be >= 0", a->window);
   return MC_OK;
 }

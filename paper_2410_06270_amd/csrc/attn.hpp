@@ -232,7 +232,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // (x / cap)^2, up to x = cap / 4 (the next term, below 2^-26), and cap (1 - 2 u) from there
 // (prefill of 8192 tokens, 32 heads over 8: 803 us, by the first form 651).
 constexpr float kCapPlain = 64.0f;
-// Larger caps are refused: in the log2 domain they would not be finite.
+// Larger caps and scales are refused: theirs are finite in the log2 domain.
 constexpr float kScoreMost = 0x1p126f;
 
 struct ScoreConsts {

@@ -1,4 +1,4 @@
-"""Caps that the attention calls take: up to 2^126, on the host (no GPU)."""
+"""Scales and caps that the attention calls take: up to 2^126, on the host (no GPU)."""
 import ctypes
 
 import pytest
@@ -13,8 +13,10 @@ ABOVE = MOST * (1 + 2.0 ** -23)
 
 @pytest.mark.parametrize("kw,want", [
     (dict(softcap=MOST), ENOSPACE), (dict(softcap=ABOVE), EUNSUPPORTED), (dict(softcap=3.4e38), EUNSUPPORTED),
+    (dict(scale=MOST), ENOSPACE), (dict(scale=-MOST), ENOSPACE), (dict(scale=ABOVE), EUNSUPPORTED),
+    (dict(scale=-3.4e38), EUNSUPPORTED),
 ])
-def test_caps_beyond_the_log2_domain(b, kw, want):
+def test_scales_and_caps_beyond_the_log2_domain(b, kw, want):
     """What is accepted gets as far as the workspace, which is too small."""
     assert ctypes.c_float(ABOVE).value == ABOVE
     for which in ("decode", "prefill"):

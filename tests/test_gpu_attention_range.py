@@ -1,4 +1,5 @@
-"""Caps over the whole range that the attention calls take, against the 64-bit oracle."""
+"""Caps and scales over the whole range that the attention calls take, against the
+64-bit oracle."""
 import math
 
 import pytest
@@ -79,3 +80,29 @@ def test_large_caps(mc, cap, D, dtype, slopes):
     want, rel = oa.importance(q[:L].double(), lse.double().cpu(), [w.rows("k", 0, h) for h in range(2)], x.double(), L,
                               2, 2, D, scale=D ** -0.5, cap=cap, slopes=sl)
     assert bool(((imp.cpu().double() - want).abs() <= rel * want).all())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 126, -2.0 ** 126, 2.0 ** -126])
+@pytest.mark.parametrize("which", ["decode", "prefill"])
+def test_scales_at_the_limit(mc, scale, which):
+    """One key and products of 2^-scale's exponent: lse is the score, an ordinary one."""
+    Hq, D, page = 4, 64, 16
+    k = torch.zeros((1, D), dtype=BF16)
+    k[0, 5] = math.copysign(math.ldexp(1.25, -63 if abs(scale) > 1 else 63), scale)
+    flat = torch.zeros((page * D,), dtype=BF16)
+    table = torch.zeros((1, 1), dtype=torch.int32)
+    oa.write("k", flat, table[0], torch.arange(1), 0, k, page, 1, D, 8)
+    q = torch.zeros((1, Hq, D), dtype=BF16)
+    q[0, :, 5] = torch.tensor([1.0, 1.5, -1.75, 0.0]) * 2.0 ** (-61 if abs(scale) > 1 else 63)
+    cache = mc.KVCache(1, page, 1, D, k=flat.view(1, -1).cuda(), v=torch.ones((1, page * D), dtype=BF16, device="cuda"))
+    kw = {} if which == "decode" else dict(q_start=starts([1]), T=1)
+    batch = mc.KVBatch(torch.ones(1, dtype=torch.int32, device="cuda"), table.cuda(), **kw)
+    o, lse = torch.empty((1, Hq * D), dtype=BF16, device="cuda"), torch.empty((1, Hq), device="cuda")
+    ws = torch.empty(mc.attn_workspace(1, Hq, 1, D), dtype=torch.uint8, device="cuda")
+    call = mc.attn_decode if which == "decode" else mc.attn_prefill
+    call(q.view(1, -1).cuda(), batch, cache, mc.Attention(Hq, scale), o, ws, lse=lse)
+    torch.cuda.synchronize()
+    want = q[0, :, 5].double() * k[0, 5].double() * scale
+    # log2(e), the scale and the score in the log2 domain, ln 2 and lse rounded
+    assert bool(((lse[0].cpu().double() - want).abs() <= 6 * oa.U24 * want.abs()).all())
+    assert bool((o == 1).all())
