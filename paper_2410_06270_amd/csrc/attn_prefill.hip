@@ -74,6 +74,14 @@ size_t attn_prefill_split_rows(int T, int Hq) {
 // tiles need no scaling and no exchange between the half waves.
 constexpr float kMaxSlack = 8.0f;
 
+// Plain scores are multiplied out with the maximum's subtraction, unrounded, while the
+// maximum is a rounded product: the largest weight is then 2^(2^-24 |m|) either way.  From this
+// maximum on (log2), where that passes 2^-11 and nears a weight's rounding, a wave takes every
+// tile the way of masked ones, whose scores are rounded first, as decode's are.  (It is looked at
+// where the maximum moves.  2048 tokens over 14000, two teams: 172 us, tested at every tile 175,
+// without 170.)
+constexpr float kFarScore = 8192.0f;
+
 // A tile of values that some row does not see whole.  Those behind its first n
 // keys may be anything and become 0; so do infinities and NaN, which a weight of 0
 // would not keep from the rows that do not see them.  Returns whether the thread met
@@ -170,7 +178,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // of the wave's live rows
   const int wrow = row0 + 32 * wave;
   const bool wave_live = wrow < count * a.g;
-  const int wpos_first = pos0 + wrow / a.g, wpos_last = pos0 + min(wrow + 31, count * a.g - 1) / a.g;
+  int wpos_first = pos0 + wrow / a.g;
+  const int wpos_last = pos0 + min(wrow + 31, count * a.g - 1) / a.g;
 
   // queries: lane (row n, half) holds units half, half + 2, ... of its row (a row
   // that is not live takes another's).  A negative scale turns their signs, so that
@@ -207,6 +216,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
       max(ia, (a.window > 0 && pos_last >= a.window ? (pos_last - a.window) / kPreKeys + 1 : 0) + ia - ib);
   const int in_count = max(0, (pos_first >= 0 ? (pos_first + 1) / kPreKeys : 0) + ia - ib - in_first);
   auto inside = [&](int t) { return (unsigned)(t - in_first) < (unsigned)in_count; };
+  int wave_inside = in_count;                          // the wave's: 0 from far scores on
 
   // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each, both
   // at the same offset.  The lanes find the offsets of 64 tiles together, from `known` on.
@@ -313,11 +323,12 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // a multiple of the product, and the running maximum.  Returns what weigh multiplies by.
   auto settle = [&](f32x16 (&sv)[2], float mx, int t) {
     const int key0 = tile_key(t);
-    // (inside() first: two teams, 2048 tokens over 14000, 173 -> 168 us; one team, 8192
+    // (those inside first: two teams, 2048 tokens over 14000, 173 -> 168 us; one team, 8192
     // tokens of heads of 64, 333 -> 342)
-    const bool masked = (G == 1 || !inside(t)) && !(((wpos_first >= 0) & (key0 + kPreKeys <= pre)) |
-                                                    ((key0 + kPreKeys - 1 <= wpos_first) &
-                                                     ((a.window == 0) | (key0 > wpos_last - a.window))));
+    const bool masked =
+        (G == 1 || (unsigned)(t - in_first) >= (unsigned)wave_inside) &&
+        !(((wpos_first >= 0) & (key0 + kPreKeys <= pre)) |
+          ((key0 + kPreKeys - 1 <= wpos_first) & ((a.window == 0) | (key0 > wpos_last - a.window))));
     if (masked || MODE) {
       const int hkey = key0 + 8 * half;
       const Mask k = {pos - hkey, rlow - hkey, rpre - hkey};
@@ -338,7 +349,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     } else {
       mx *= sc.scale2;
     }
-    const float mul = masked || MODE ? 1.0f : sc.scale2;
+    float mul = masked || MODE ? 1.0f : sc.scale2;
     if (__any(mx > m + kMaxSlack)) {
       const float m_new = fmaxf(m, halves_max(mx));
       const float alpha = m_new == kNegInf ? 1.0f : exp2_fast(m - m_new);
@@ -348,6 +359,17 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
       m = m_new;
+      if constexpr (!MODE) {
+        if (__any(fabsf(m) > kFarScore && m != kNegInf)) {
+          if (!masked) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sv[e >> 4][e & 15] *= mul;
+            mul = 1.0f;
+          }
+          wave_inside = 0;                             // every tile is masked
+          wpos_first = -1;
+        }
+      }
     }
     return mul;
   };

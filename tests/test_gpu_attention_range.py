@@ -1,5 +1,5 @@
-"""Caps and scales over the whole range that the attention calls take, against the
-64-bit oracle."""
+"""Caps, scales and scores over the whole range that the attention calls take, against
+the 64-bit oracle."""
 import math
 
 import pytest
@@ -106,3 +106,95 @@ def test_scales_at_the_limit(mc, scale, which):
     # log2(e), the scale and the score in the log2 domain, ln 2 and lse rounded
     assert bool(((lse[0].cpu().double() - want).abs() <= 6 * oa.U24 * want.abs()).all())
     assert bool((o == 1).all())
+
+
+def _far_scores(mc, D, dtype, e, scale, Hq=2, L=1100, seed=22):
+    """A world of one sequence whose scores are scale 2^e times one dimension of the keys,
+    queries for it and the scores in units of 2^e (and of an e4m3 head's scale)."""
+    gen = torch.Generator().manual_seed(seed)
+    e4 = dtype == E4M3
+    steps = torch.arange(0x20, 0x78, dtype=torch.uint8) if e4 else torch.arange(0x3f80, 0x3f80 + 1200, dtype=torch.int16)
+    if e4:
+        kv = steps.view(E4M3)[torch.randint(len(steps), (L,), generator=gen)].double()
+    else:
+        kv = steps.view(BF16)[torch.randperm(len(steps), generator=gen)[:L]].double()
+    odd = [(0, slice(None), 0, 0, "k", kv.float().to(dtype))]
+    w = World(mc, [L], Hkv=1, D=D, page=64, dtype=dtype, seed=seed, odd=odd)
+    q = torch.zeros((L, Hq * D), dtype=BF16)
+    q[:, ::D] = 2.0 ** e
+    return w, q, kv if scale > 0 else -kv
+
+
+def _best(kv, v, pos):
+    """The mean of the values at the largest score that each position sees."""
+    rows = []
+    for i in pos.tolist():
+        seen = kv[:i + 1]
+        rows.append(v[:i + 1][seen == seen.max()].mean(0))
+    return torch.stack(rows)
+
+
+@pytest.mark.parametrize("e", [20, 27, 31, 33, 40, 100])
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (128, BF16), (64, E4M3), (128, E4M3)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_far_scores(mc, e, D, dtype, sign):
+    """Finite scores of any size choose the keys that have the largest: prefill in one
+    part, two teams and several parts, and decode."""
+    Hq, L, new = 2, 1100, 400
+    w, q, kv = _far_scores(mc, D, dtype, e, sign)
+    v = w.rows("v", 0, 0)
+    pos = torch.arange(L - new, L)
+    want = _best(kv, v, pos)
+    top = torch.stack([kv[:i + 1].max() for i in pos.tolist()])
+    if w.scale["k"] is not None:
+        top = top * w.scale["k"][0].double()
+    top = top * 2.0 ** e
+    # the weights' rounding and the output's; gaps are 160 or more
+    tol = 2 * oa.BF * v.abs().amax()
+    # ln of up to 1100 ties, and the roundings of a score in two domains and the head's scale
+    tol_l = 8 * oa.U24 * top.abs() + 8
+    n = torch.tensor([L], dtype=torch.int32, device="cuda")
+    for what, max_len in (("decode", 0), ("decode", 1), ("prefill", 1), ("prefill", 512), ("prefill", 0)):
+        rows = 1 if what == "decode" else new
+        kw = {} if what == "decode" else dict(q_start=starts([new]), T=new)
+        batch = mc.KVBatch(n, w.table.cuda(), max_len=max_len, **kw)
+        o, lse = torch.empty((rows, Hq * D), dtype=BF16, device="cuda"), torch.empty((rows, Hq), device="cuda")
+        call = mc.attn_decode if what == "decode" else mc.attn_prefill
+        call(q[-rows:].cuda(), batch, w.cache, mc.Attention(Hq, float(sign)), o, w.workspace(mc, rows, Hq), lse=lse)
+        torch.cuda.synchronize()
+        for h in range(Hq):
+            off = (o[:, h * D:(h + 1) * D].cpu().double() - want[-rows:]).abs()
+            assert bool((off <= tol).all()), (what, max_len, h)
+            assert bool(((lse[:, h].cpu().double() - top[-rows:]).abs() <= tol_l[-rows:]).all()), (what, max_len, h)
+
+
+@pytest.mark.parametrize("D,max_len", [(64, 1), (64, 512), (64, 0), (128, 1), (128, 0)])
+@pytest.mark.parametrize("prefix", [None, 900])
+@pytest.mark.parametrize("first", [2.0 ** -40, 0.0, -1.0])
+def test_scores_that_become_far(mc, D, max_len, prefix, first):
+    """Ordinary scores, zeros or far negative ones in the first tiles, far ones behind them."""
+    Hq, L, new, cut = 2, 1100, 400, 777
+    w, q, kv = _far_scores(mc, D, BF16, 40, 1)
+    k = torch.zeros((cut, D), dtype=BF16)
+    k[:, 0] = (kv[:cut] * first).float().to(BF16)
+    kv[:cut] = k[:, 0].double()
+    flat = w.flat["k"].clone()
+    was = w.rows("k", 0, 0)[:cut].to(BF16)
+    was[:, 0] = k[:, 0]
+    oa.write("k", flat, w.table[0], torch.arange(cut), 0, was, w.page, 1, D, 8)
+    w.cache.k.copy_(flat.view(w.cache.k.shape))
+    v = w.rows("v", 0, 0)
+    pos = torch.arange(L - new, L)
+    s = kv * 2.0 ** 40
+    want = torch.stack([torch.softmax(s[:max(i + 1, prefix or 0)], 0) @ v[:max(i + 1, prefix or 0)] for i in pos.tolist()])
+    # in rows before the far scores the weights' rounding, the sums of 1100 terms, and twice the
+    # roundings of scores up to 4
+    tol = (2 * oa.BF + (2 * L + 64) * oa.U24) * v.abs().amax()
+    batch = mc.KVBatch(torch.tensor([L], dtype=torch.int32, device="cuda"), w.table.cuda(), q_start=starts([new]), T=new,
+                       max_len=max_len)
+    at = mc.Attention(Hq, 1.0, prefix=None if prefix is None else torch.tensor([prefix], dtype=torch.int32, device="cuda"))
+    o = torch.empty((new, Hq * D), dtype=BF16, device="cuda")
+    mc.attn_prefill(q[-new:].cuda(), batch, w.cache, at, o, w.workspace(mc, new, Hq))
+    torch.cuda.synchronize()
+    for h in range(Hq):
+        assert bool(((o[:, h * D:(h + 1) * D].cpu().double() - want).abs() <= tol).all()), h
