@@ -111,6 +111,14 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Waits for the wave's direct loads to LDS; what it reads of them afterwards stays behind the wait
+// (which alone the compiler need not keep LDS accesses behind).
+__device__ __forceinline__ void loads_landed() {
+  asm volatile("" ::: "memory");
+  wait_vmcnt<0>();
+  asm volatile("" ::: "memory");
+}
+
 // ----------------------------------------------------------- direct loads --
 // 16 or 4 bytes a lane to LDS from a buffer, `bytes` at a wave-uniform address: read at
 // OFF (below 4096) plus the lane's own offset and a uniform one, to dst + OFF + 16 l (or dst

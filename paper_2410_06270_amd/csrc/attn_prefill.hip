@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   auto begin_round = [&](char* vt, int t) {
     if constexpr (!E4) wait_vmcnt<0>();
     lds_barrier();
-    if constexpr (E4) wait_vmcnt<0>();
+    if constexpr (E4) loads_landed();
     bool any = false;                                  // a tile of some team
 #pragma unroll
     for (int tm = 0; tm < G; ++tm) {
@@ -456,13 +456,13 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     find_offsets();
     load(t_begin, s_k[0], s_v[1]);
     if constexpr (E4) {
-      wait_vmcnt<0>();
+      loads_landed();
       widen(raw_k, true, s_k[0] + wave * kBlk);
       lds_done();
     }
     load(t_begin + 1, s_k[1], s_v[0]);
     if constexpr (E4) {
-      wait_vmcnt<0>();
+      loads_landed();
       if (t_begin + 1 < t_end) widen(raw_k, true, s_k[1] + wave * kBlk);
       widen(raw_v, false, s_v[0] + wave * kBlk);
       lds_done();
