@@ -474,6 +474,12 @@ def _device_of(*tensors):
     return found.pop() if found else None
 
 
+def _bounded(n) -> int:
+    """A window or length as a C int: any negative number stays one (and is refused), any
+    past the largest says as much as that (a ctypes field would take it modulo 2^32)."""
+    return max(-1, min(int(n), 2 ** 31 - 1))
+
+
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)      # bf16, or its bits
 
 
@@ -525,7 +531,7 @@ class KVBatch:
         self.S, self.T, self.max_pages = S, S if T is None else int(T), max_pages
         self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
         self.dev = _device_of(kv_len, page_table, q_start)
-        self.desc = _KVBatch(S, self.T, max_pages, int(max_len), None if q_start is None else q_start.data_ptr(),
+        self.desc = _KVBatch(S, self.T, max_pages, _bounded(max_len), None if q_start is None else q_start.data_ptr(),
                              kv_len.data_ptr(), page_table.data_ptr())
         self.ref = ctypes.byref(self.desc)
 
@@ -559,7 +565,7 @@ class Attention:
         assert prefix is None or (prefix.dtype == torch.int32 and prefix.is_contiguous())
         self.dev = _device_of(slopes, prefix)
         self.Hq, self.slopes, self.prefix = Hq, slopes, prefix
-        self.desc = _Attention(Hq, float(scale), float(softcap), int(window),
+        self.desc = _Attention(Hq, float(scale), float(softcap), _bounded(window),
                                None if slopes is None else slopes.data_ptr(),
                                None if prefix is None else prefix.data_ptr())
         self.ref = ctypes.byref(self.desc)
