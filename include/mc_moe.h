@@ -453,7 +453,8 @@ typedef struct mc_qk_prep {
  * values to the cache.  For every row of the batch and every head of q and k:
  *   y = x * w / sqrt(mean(x^2) + eps)          (over D, or over the row)
  *   (y_a, y_b) <- (y_a cos - y_b sin, y_a sin + y_b cos)   (each rotated pair)
- * in fp32, rounded once: queries to bf16 into q_out, keys to the cache's type;
+ * in fp32 (the sum of x^2 as well: below 2^128, and mean(x^2) + eps above 2^-126),
+ * rounded once: queries to bf16 into q_out, keys to the cache's type;
  * values are stored as they are.  An e4m3 code is the nearest one (ties to even)
  * of y * (1 / scale[h]), both in fp32, clamped to +-448; NaN stays NaN.
  * q [T][Hq*D], k and v [T][Hkv*D] bf16 with the given elements between rows
@@ -499,7 +500,9 @@ mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t *bytes);
  * (b->T is ignored), after its key and value are in the cache.
  *   o = sum_j exp(s_j - lse) v_j,   lse = ln sum_j exp(s_j)   over visible j
  * Scores, sums and statistics in fp32; the weights exp(s - max) are rounded to
- * bf16 for the product with the values.  A row that sees no key (kv_len 0), or
+ * bf16 for the product with the values.  The products are summed in fp32 before they are
+ * divided, with weights up to 2^8 in mc_attn_prefill: the visible |v| (of e4m3, the
+ * codes') have to sum to less than 2^120.  A row that sees no key (kv_len 0), or
  * only scores of -infinity, gets o = 0 and lse = -infinity.  What the cache
  * holds at positions a row does not see has no effect on it, NaN included.
  * q [S][Hq*D] bf16 and o likewise with their elements between rows (multiples
@@ -526,7 +529,9 @@ mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch 
  *   I_j = ||x_j||_1 * (1/Hq) * sum_h sum_{i=j}^{L-1} exp(s_hij - lse[i][h]) / (L - j)
  * (0 for a pair that the window hides), fp32 sums in a fixed order, and
  * important[j] = 1 for the floor(rho*L + 1/2) largest I_j (equal values: lower j
- * first).  One sequence a call: b->S = 1, L = b->T its tokens, at positions
+ * first).  lse has 24 bits, so a probability is off by some 2^-22 |lse| of itself
+ * beside its score's error: scores of 2^20 and more leave little of it.
+ * One sequence a call: b->S = 1, L = b->T its tokens, at positions
  * 0 .. L-1 of page_table[0] (q_start and kv_len are ignored; rows 0 .. L-1 of
  * q and lse).  a->prefix must be NULL (Eq. 6 is of causal attention).  x [L][d]
  * bf16; importance [L] fp32 may be NULL.  Workspace: mc_attn_importance_workspace.

@@ -70,10 +70,10 @@ __device__ __forceinline__ size_t kv_block_offset(const KvArgs& c, int p, int h,
   return (size_t)p * c.page_stride + (size_t)((h << c.lb) + in_page) * BYTES;
 }
 
-// The largest s in [0, S) with start[s] / div + mul * s <= key (0 if there is
-// none), found by the whole wave with 64 probes a round: one load for up to 64
-// sequences, two for 4096.  key must be wave-uniform; every s it returns is in
-// range whatever the array holds.
+// The largest s in [0, S) with start[s] * g / div + mul * s <= key (0 if there is
+// none; g: rows of a tile that a token takes), found by the whole wave with 64 probes a
+// round: one load for up to 64 sequences, two for 4096.  key must be wave-uniform; every s
+// it returns is in range whatever the array holds.
 __device__ __forceinline__ int find_sequence(const int32_t* __restrict__ start, int S, int key, int div, int mul,
                                              int g) {
   const int lane = threadIdx.x & 63;

@@ -32,8 +32,9 @@ constexpr int kMaxSplit = 128;
 // fit a CU's registers), as long as every wave has a step; more, up to
 // kDecTarget workgroups, where a part keeps kDecPart bytes of keys and values: the
 // shorter the parts, the less a long sequence of a ragged batch is waited for (48
-// sequences of 300 to 8191 tokens: 158 us at one round of workgroups, 145 at four), and
-// the more their starts and the join cost (64 sequences of 512: 23 and 30).
+// sequences of 300 to 8191 tokens, 0.9 GB: 204 us at one round of workgroups, 159 at four),
+// and the more their starts and the join cost (64 sequences of 512: 24 us, with parts of a
+// quarter 31).
 constexpr int kDecFill = 512, kDecTarget = 2048, kDecPart = 192 << 10;
 
 static int decode_splits(int S, int Hkv, int head_tiles, int max_len, int keys, int key_bytes) {
@@ -109,9 +110,9 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   const int voff = (E4 ? 0 : (quarter & 1) * D * 16) + n * 16;
 
   // Values are read once and by whole lines: past the caches (64 sequences of 4096
-  // e4m3 tokens, 537 MB: 101 -> 84 us; of 1024 bf16 tokens and 16 heads 95 -> 84).  A
+  // e4m3 tokens, 537 MB: 109 -> 86 us; of 1024 bf16 tokens and 16 heads 100 -> 83).  A
   // load of keys takes half of each line that it touches, the next the other half: those
-  // stay ordinary loads (non-temporal ones: 54 us for 48 at 4 x 32768 e4m3 tokens).
+  // stay ordinary loads (non-temporal ones: 58 us for 50 at 4 x 32768 e4m3 tokens).
   auto load = [&](Step& st, int i, int kp, int vp) {
     const int blk = step_blk(i);
     const int kb = min(blk + kblk, last_blk), vb = min(blk + vblk, last_blk);
@@ -201,6 +202,8 @@ __global__ void __launch_bounds__(kDecThreads, 2)
       x[e] = exp2_fast(x[e] - m0);
       l += x[e];
     }
+    // for the matrix units the weights are rounded to bf16, by up to 2^-8 of each (values are
+    // bf16 or less, and so is the result); their sum takes them as they are
 #pragma unroll
     for (int w = 0; w < KT / 2; ++w) {
       u32x4 pr;
@@ -307,7 +310,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
 // 256 threads 8 (D = 128) or 16 parts at once, and their sums are joined in LDS in a fixed
 // order.  Parts without a visible key have l = 0 and no o: what lies in its place is
 // read, so that no load waits for another, and left out.  (A wave for all parts of a
-// (row, head) took 56 us for 64 of them in 128 parts, this 4.7.)
+// (row, head) took 56 us for 64 of them in 128 parts, this 4.8.)
 constexpr int kJoinThreads = 256;
 
 template <int D>
@@ -377,9 +380,9 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(SplitArgs sp, i
 }
 
 // Few parts, FEW at most: D/4 threads a (row, head), 16 bytes of a part each, all
-// loads at once.  896 rows of 32 heads in two parts: 34.6 us by the kernel above, 11.8 by
-// this for up to 8, 7.9 for 2 (fewer registers, more waves).  One row of 16 heads in 7
-// parts: 6.4 us one part after the other, 2.9 so.
+// loads at once.  A prefill of 896 rows of 32 heads in two parts: 48.2 us with the kernel
+// above, 33.7 with this for up to 8, 30.8 for 2 (fewer registers, more waves).  One row of
+// 16 heads in 7 parts: the kernel takes 2.9 us (6.4 where one part followed the other).
 constexpr int kJoinFew = 8;
 
 template <int D, int FEW>

@@ -9,8 +9,8 @@
 // and one exponential a pair.  Bound by the vector units: 16 pairs a lane of a 32 x 32
 // tile cost 8 matrix instructions (256 cycles of a SIMD for D = 128) and 16 x (an
 // exponential, a multiply-add and an add: 24 cycles).  4096 tokens of 32 query heads over
-// 8: 97 us in all, what reading the lower half of a map takes alone (0.54 GB); 0.82
-// PFLOP/s in the sums' kernel; 16384 tokens: 0.99 PFLOP/s.
+// 8: 96 us in all, what reading the lower half of a map takes alone (0.54 GB); 0.82
+// PFLOP/s in the sums' kernel; 16384 tokens: 1.12 ms, 0.98 PFLOP/s.
 //
 // attn_colsum_kernel: a workgroup keeps 256 keys of one key-value head in
 // registers (64 a wave) and walks the rows below the diagonal, 32 at a time, of each of
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
       t.ls = v == kNegInf ? -kNegInf : v * kLog2e;       // a row without keys: every probability 0
     }
     if (t.live && prev.live && !prev.masked) {
-      // the wave with matrix work goes first (4096 tokens of 32 heads over 8: 109 -> 102 us)
+      // the wave with matrix work goes first (4096 tokens of 32 heads over 8: 101 -> 96 us)
       __builtin_amdgcn_s_setprio(1);
       qk(cur, sv);
       add(std::false_type{}, sp, prev);

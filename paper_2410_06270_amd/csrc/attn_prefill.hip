@@ -8,10 +8,11 @@
 // keys cost 32 matrix instructions of 32x32x16 for D = 128 (1024 cycles of a SIMD), and 32
 // exponentials and some 105 other vector instructions (800 cycles).  Each wave has both in
 // every round, the vector work of one tile beside the products of the next.  8192 tokens
-// of 32 query heads over 8: 535 us, 1.03 PFLOP/s (the library's product of two 8192 x
+// of 32 query heads over 8: 528 us, 1.04 PFLOP/s (the library's product of two 8192 x
 // 8192 matrices reaches 1.19, and this loop with nothing but its products 1.33: the
-// clock falls under matrix load); 4096 of 16 heads: 84 us, 0.82, matrix units busy half of
-// the time, as late row tiles end alone.
+// clock falls under matrix load); 4096 of 16 heads: 83 us, 0.83, matrix units busy half of
+// the time, as late row tiles end alone: with a prefix of all 4096 every row tile has 64 tiles of
+// keys, and 33/64 of that call's 129 us would be 67.
 //
 // A workgroup of four waves (or two teams of four, each half of the keys) takes 128
 // rows of one sequence and key-value head; the g query heads that share it are packed into
@@ -54,10 +55,10 @@ static int prefill_splits(int slots, int Hkv, int max_len) {
 // Heads of 64, whose products are half as long, leave a lone wave waiting for 30 % of its
 // time, and a row tile is as long as its keys are many.  Up to two workgroups a CU that
 // are not split take two teams of waves, each half of the keys, joined in LDS (32 query
-// heads over 8 key-value heads, one prompt of 1024 tokens: 23.1 -> 19.5 us, of 2048: 41.9
-// -> 39.2; chunks of 2048 over 14000 tokens, 16 heads: 272 -> 196); more keep one (4096
-// tokens of 32 heads: 101, with two 128), and so do short ones (256 tokens: 9.7, with two
-// 9.9).  Heads of 128: 4096 tokens of 16 heads 89, with two 93.
+// heads over 8 key-value heads, one prompt of 1024 tokens: 23.0 -> 19.4 us, of 2048: 41.8
+// -> 38.8; chunks of 2048 over 14000 tokens, 16 heads: 253 -> 179); more keep one (4096
+// tokens of 32 heads: 101, with two 120), and so do short ones (256 tokens: 10.2, with two
+// 10.4).  Heads of 128: no difference (4096 tokens of 16 heads 85.3, with two 85.8).
 static bool prefill_two_teams(int slots, int Hkv, int nsplit, int max_len) {
   return nsplit == 1 && (long long)slots * Hkv <= kPreTarget && max_len >= 512;
 }
@@ -112,9 +113,9 @@ __device__ __forceinline__ bool clean_values(char* vt, int n) {
 // The order of a round's instructions: LDS reads some matrix instructions before their
 // use, and the vector work (some 135 instructions) spread over the spaces between all of
 // them: the first products with the values need only the first weights.  Heads of 128, 32
-// products: 3 instructions a space (8192 tokens of 32 heads over 8: 551 us, with 4 559 and
-// with 5 567); of 64, 16 products: 10 and reads 3 ahead (2048 tokens over 14000 187 us,
-// with 8 and 5 ahead 192).
+// products: 3 instructions a space (8192 tokens of 32 heads over 8: 528 us, with 4 532 and
+// with 5 543); of 64, 16 products: 10 and reads 3 ahead (2048 tokens over 14000 175 us,
+// with 8 and 5 ahead 178).
 template <int DK, int DT>
 __device__ __forceinline__ void interleave() {
   constexpr int kMfmas = 2 * DK + 4 * DT, kReadAhead = DT == 2 ? 3 : 5, kVector = DT == 2 ? 10 : 3;
@@ -151,9 +152,10 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   const int split = id % sp.nsplit;
   // Later rows see more keys: the later half of the row tiles goes first, from the
   // last on, then the other from the first on, so that where all workgroups are on the chip
-  // at once a CU has a long and a short one (4096 tokens of 16 heads, 512 workgroups: 108
-  // us from the last to the first, 105 so).  Of two teams a CU holds one workgroup, and the
-  // first to end takes the next: from the last to the first (80 us by halves, 68 so).
+  // at once a CU has a long and a short one (4096 tokens of 16 heads, 512 workgroups: 92.1
+  // us from the last to the first, 86.6 so).  Of two teams a CU holds one workgroup, and the
+  // first to end takes the next: from the last to the first (4096 tokens, 16 heads over 4: 68.5
+  // us by halves, 57.0 so).
   const int turn = id / sp.nsplit, later = (slots + 1) / 2;
   const int slot = G > 1 || turn < later ? slots - 1 - turn : turn - later;
   const int s = find_sequence(b.q_start, b.S, slot, kPreRows, 1, a.g);
@@ -323,8 +325,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // a multiple of the product, and the running maximum.  Returns what weigh multiplies by.
   auto settle = [&](f32x16 (&sv)[2], float mx, int t) {
     const int key0 = tile_key(t);
-    // (those inside first: two teams, 2048 tokens over 14000, 173 -> 168 us; one team, 8192
-    // tokens of heads of 64, 333 -> 342)
+    // (those inside first: two teams, 2048 tokens over 14000, 175 -> 173 us; one team, 8192
+    // tokens of heads of 64, no difference)
     const bool masked =
         (G == 1 || (unsigned)(t - in_first) >= (unsigned)wave_inside) &&
         !(((wpos_first >= 0) & (key0 + kPreKeys <= pre)) |
@@ -419,8 +421,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     }
     if (wave_live && (G == 1 || t < t_end)) {
       // (the last round's next tile is whatever its buffer holds, and not used)
-      // The wave with matrix work goes first: chunks of capped scores 416 -> 366 us, 8192
-      // tokens of e4m3 576 -> 558; plain scores of heads of 64 gain nothing.
+      // The wave with matrix work goes first: chunks of capped scores 366 -> 349 us, 8192
+      // tokens of e4m3 570 -> 555; plain scores of heads of 64 lose (343 -> 347).
       constexpr bool kFirst = MODE || D == 128;
       if (kFirst) __builtin_amdgcn_s_setprio(1);
       u32x4 p[4];
