@@ -21,8 +21,29 @@ struct KvArgs {
   char *k, *v;
   size_t page_stride;                // bytes
   int n_pages, Hkv, lb;              // lb: log2 of the blocks in a page
-  const float *k_scale, *v_scale;    // null for bf16
+  const float *k_scale, *v_scale;    // e4m3 only
+  int kind;                          // MC_KV_*
 };
+
+// How a kind of cache holds its elements: bytes of a block's codes, tokens (of values) or
+// dimensions (of keys) that 16 bytes hold.  e2m1 has scales behind a page's codes.
+template <int D, int KV>
+struct KvFormat {
+  static constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  static constexpr int kBlockBytes = E2 ? 8 * D : kKvBlock * D * (E4 ? 1 : 2);
+  static constexpr int kScaleBytes = E2 ? D / 2 : 0;       // of a block
+};
+
+// Calls f(integral constant of the cache's kind).
+template <class F>
+void with_kv_kind(const KvArgs& c, F&& f) {
+  if (c.kind == MC_KV_E2M1)
+    f(std::integral_constant<int, MC_KV_E2M1>{});
+  else if (c.kind == MC_KV_E4M3)
+    f(std::integral_constant<int, MC_KV_E4M3>{});
+  else
+    f(std::integral_constant<int, MC_KV_BF16>{});
+}
 
 struct BatchArgs {
   const int32_t *q_start, *kv_len, *page_table;
@@ -68,6 +89,13 @@ template <int BYTES>
 __device__ __forceinline__ size_t kv_block_offset(const KvArgs& c, int p, int h, int blk) {
   const int in_page = blk & ((1 << c.lb) - 1);
   return (size_t)p * c.page_stride + (size_t)((h << c.lb) + in_page) * BYTES;
+}
+
+// Byte offset of a block's scales (e2m1).
+template <int D>
+__device__ __forceinline__ size_t kv_scale_offset(const KvArgs& c, int p, int h, int blk) {
+  const int in_page = blk & ((1 << c.lb) - 1);
+  return (size_t)p * c.page_stride + (size_t)(c.Hkv << c.lb) * (8 * D) + (size_t)((h << c.lb) + in_page) * (D / 2);
 }
 
 // The largest s in [0, S) with start[s] * g / div + mul * s <= key (0 if there is
@@ -173,6 +201,32 @@ __device__ __forceinline__ u32x4 e4m3_to_bf16(uint32_t a, uint32_t b) {
   __builtin_memcpy(&r, t, 16);
   return r;
 }
+
+// Eight e2m1 codes (a word, the first in the lowest bits) times 2^(byte - 127), as bf16: exact, but
+// for results below 2^-126.  (The instruction takes its factor's exponent; 255 gives NaN.)
+__device__ __forceinline__ u32x4 e2m1_to_bf16(uint32_t w, float scale) {
+  bf16x2 t[4];
+  t[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  t[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  t[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  t[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  u32x4 r;
+  __builtin_memcpy(&r, t, 16);
+  return r;
+}
+
+// 2^(byte - 127) for byte `at` of w.
+__device__ __forceinline__ float e8m0_scale(uint32_t w, int at) {
+  return __uint_as_float(((w >> (8 * at)) & 0xffu) << 23);
+}
+
+// The value of an e2m1 code, and bf16 halves of a word as floats.
+__device__ __forceinline__ float e2m1_value(uint32_t code) {
+  const float m = (code & 6u) ? __uint_as_float(((126u + ((code >> 1) & 3u)) << 23) | ((code & 1u) << 22))
+                              : 0.5f * (float)(code & 1u);
+  return code & 8u ? -m : m;
+}
+__device__ __forceinline__ float half_of(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xffff0000u : w << 16); }
 
 // Four e4m3 codes: nearest, ties to even, clamped to +-448 (the comparison
 // leaves a NaN as it is, and NaN converts to NaN).

@@ -27,6 +27,7 @@ constexpr int kDecWaves = 4;
 constexpr int kDecThreads = 64 * kDecWaves;
 constexpr int kDecHeads = 16;        // query heads of a workgroup
 constexpr int kMaxSplit = 128;
+constexpr int kNowhere = 0x7f000000;     // a position past all others
 
 // The parts a cache is cut into.  Enough to fill the chip (two workgroups of 4 waves
 // fit a CU's registers), as long as every wave has a step; more, up to
@@ -48,23 +49,43 @@ static int decode_splits(int S, int Hkv, int head_tiles, int max_len, int keys, 
   return (int)(n < 1 ? 1 : n > kMaxSplit ? kMaxSplit : n);
 }
 
-// The keys of a step as a lane takes them.
-template <int D, bool E4>
+// The keys of a step as a lane takes them: whole 16-byte units, of e2m1 keys the part of a unit
+// that holds D / 4 dimensions.  e2m1: the scale bytes of the lane's key in each tile, and the
+// scales of its values, 64 dimensions after the other.
+template <int D, int KV>
 struct DecodeStep {
-  static constexpr int kTiles = E4 ? 4 : 2;              // 16-key tiles
-  static constexpr int kChunks = D / (E4 ? 64 : 32);     // 16-byte units of a key that a lane takes
-  static constexpr int kKeys = 16 * kTiles;
-  u32x4 k[kTiles][kChunks], v[D / 16];
+  static constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  static constexpr int kTiles = KV == MC_KV_BF16 ? 2 : 4;                    // 16-key tiles
+  static constexpr int kChunks = E2 ? 1 : D / (E4 ? 64 : 32);                // pieces of a key that a lane takes
+  static constexpr int kKeys = 16 * kTiles, kValues = D / (E2 ? 32 : 16);
+  using Piece = typename std::conditional<E2 && D == 64, u32x2, u32x4>::type;
+  Piece k[kTiles][kChunks];
+  u32x4 v[kValues];
+  uint32_t ks;
+  u32x4 vs[E2 ? D / 32 : 1];
 };
 
-template <int D, bool E4, int MODE>
+// The pages that each row of a sparse call reads: sel [row][Hkv][n_sel] positions in the sequence's
+// table row, the first count [row][Hkv] of them.
+struct SparseArgs {
+  const int32_t *sel, *count;
+  int n_sel;
+};
+
+// SPARSE: a row's keys are those of its listed pages, one after the other; a row is any token of
+// a ragged batch (b.q_start null: the last of its sequence).
+template <int D, int KV, int MODE, bool SPARSE>
 __global__ void __launch_bounds__(kDecThreads, 2)
     attn_decode_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
-                       int head_tiles) {
-  using Step = DecodeStep<D, E4>;
-  constexpr int KS = Step::kKeys, KT = Step::kTiles, KC = Step::kChunks, DT = D / 16, DP = D + 4;
-  constexpr int kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
-  __shared__ float s_o[kDecWaves][kDecHeads][DP];
+                       int head_tiles, SparseArgs sparse) {
+  using Step = DecodeStep<D, KV>;
+  constexpr bool E4 = Step::E4, E2 = Step::E2;
+  constexpr int KS = Step::kKeys, KT = Step::kTiles, KC = Step::kChunks, DT = D / 16, DP = D + 4, VT = Step::kValues;
+  constexpr int kBlockBytes = KvFormat<D, KV>::kBlockBytes;
+  // the waves' results; before them, of a sparse call, its pages: place in the table, and number
+  constexpr int kResults = kDecWaves * kDecHeads * DP * 4, kLists = SPARSE ? 8 * MC_MAX_SELECT : 0;
+  __shared__ __attribute__((aligned(16))) char s_all[kResults > kLists ? kResults : kLists];
+  float (*s_o)[kDecHeads][DP] = reinterpret_cast<float (*)[kDecHeads][DP]>(s_all);
   __shared__ float s_ml[2][kDecWaves][kDecHeads];
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 15, quarter = lane >> 4;
   int id = blockIdx.x;
@@ -72,42 +93,78 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   id /= sp.nsplit;
   const int ht = id % head_tiles;
   id /= head_tiles;
-  const int hk = id % c.Hkv, s = id / c.Hkv;
+  const int hk = id % c.Hkv, row = id / c.Hkv;
   const int head0 = hk * a.g + ht * kDecHeads, heads = min(kDecHeads, a.g - ht * kDecHeads);
+  int s = row;
+  if (SPARSE && b.q_start) {
+    if (row < b.q_start[0] || row >= b.q_start[b.S]) return;         // padding
+    s = find_sequence(b.q_start, b.S, row, 1, 0, 1);
+  }
 
   // queries: lane (head n, quarter) holds the units that it takes of a key
   bf16x8 qf[D / 32];
   {
-    const uint16_t* qr = q.p + (size_t)s * q.stride + (size_t)(head0 + n) * D;
+    const uint16_t* qr = q.p + (size_t)row * q.stride + (size_t)(head0 + n) * D;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       u32x4 r = {0u, 0u, 0u, 0u};
-      const int at = E4 ? 16 * (4 * (i / 2) + quarter) + 8 * (i & 1) : 8 * (4 * i + quarter);
+      const int at = E2 ? D / 4 * quarter + 8 * i
+                        : E4 ? 16 * (4 * (i / 2) + quarter) + 8 * (i & 1) : 8 * (4 * i + quarter);
       if (n < heads) r = *reinterpret_cast<const u32x4*>(qr + at);
       qf[i] = as_bf16x8(r);
     }
   }
 
-  const int len = kv_length(c, b, s), pos = len - 1;
-  const int pre = kv_prefix(a, s, len);
+  // (of a sparse call: the tokens up to the row's own)
+  int len = kv_length(c, b, s);
+  if (SPARSE && b.q_start) {
+    const long long own = (long long)b.kv_len[s] - ((long long)b.q_start[s + 1] - row) + 1;
+    len = own < 0 ? 0 : own < len ? (int)own : len;
+  }
+  const int pos = len - 1;
+  const int pre = SPARSE ? 0 : kv_prefix(a, s, len);
   const int wstart = a.window > 0 && len > a.window ? len - a.window : 0;   // first key of the window
+  int listed = 0;
+  const int32_t* list = nullptr;
+  if (SPARSE) {
+    listed = sparse.count[(size_t)row * c.Hkv + hk];
+    listed = len == 0 || listed < 0 ? 0 : min(listed, sparse.n_sel);
+    list = sparse.sel + ((size_t)row * c.Hkv + hk) * sparse.n_sel;
+  }
   // steps that hold a visible key: [0, ia) and [ib, all)
-  const int all = (len + KS - 1) / KS;
-  int ia = (pre + KS - 1) / KS, ib = wstart / KS;
+  const int all = ((SPARSE ? (listed << c.lb) * kKvBlock : len) + KS - 1) / KS;
+  int ia = (pre + KS - 1) / KS, ib = SPARSE ? 0 : wstart / KS;
   if (ib <= ia) ia = ib = 0;
   const int steps = ia + all - ib, per = (steps + sp.nsplit - 1) / sp.nsplit;
   const int i_end = min(steps, (split + 1) * per);
   int it = split * per + wave;
 
   const int32_t* pages = b.page_table + (size_t)s * b.max_pages;
-  const int last_blk = len > 0 ? (len - 1) >> 4 : 0;
-  // the lane's blocks of a step: keys 8 n/4 .. (bf16) or 16 n/4 .. (e4m3) of
+  const int last_blk = SPARSE ? max((listed << c.lb) - 1, 0) : len > 0 ? (len - 1) >> 4 : 0;
+  // the lane's blocks of a step: keys 8 n/4 .. (bf16) or 16 n/4 .. (the others) of
   // the step go through it as a score row, keys 8 or 16 quarter .. as values
-  const int kblk = E4 ? n >> 2 : n >> 3, vblk = E4 ? quarter : quarter >> 1;
+  const int kblk = KT == 4 ? n >> 2 : n >> 3, vblk = KT == 4 ? quarter : quarter >> 1;
   auto step_blk = [&](int i) { return ((i < ia ? i : i - ia + ib) * KS) >> 4; };
   auto page_of = [&](int blk) { return pages[(blk < last_blk ? blk : last_blk) >> c.lb]; };
-  const int koff = (E4 ? (n & 3) : 8 * ((n >> 2) & 1) + (n & 3)) * 16 + quarter * 256;
-  const int voff = (E4 ? 0 : (quarter & 1) * D * 16) + n * 16;
+  const int koff = (E2 && D == 64) ? (n & 3) * 16 + (quarter >> 1) * 256 + 8 * (quarter & 1)
+                                   : (KT == 4 ? (n & 3) : 8 * ((n >> 2) & 1) + (n & 3)) * 16 + quarter * 256;
+  const int voff = (KT == 4 ? 0 : (quarter & 1) * D * 16) + n * 16;
+
+  // Of a sparse call: the workgroup's pages, entries e0 on of the list.  A place outside the table
+  // is one past every position.
+  const int e0 = SPARSE ? min(((split * per * KS) >> 4) >> c.lb, max(listed - 1, 0)) : 0;
+  int* s_sel = reinterpret_cast<int*>(s_all);
+  int* s_page = s_sel + MC_MAX_SELECT;
+  if (SPARSE) {
+    const int e1 = min(((min(i_end, steps) * KS) >> 4 >> c.lb) + 1, listed);
+    for (int i = e0 + (int)threadIdx.x; i < e1; i += kDecThreads) {
+      const int at = list[i];
+      const bool in = at >= 0 && at < b.max_pages;
+      s_sel[i - e0] = in ? at : b.max_pages;
+      s_page[i - e0] = in ? kv_page(c, pages[at]) : 0;
+    }
+    __syncthreads();
+  }
 
   // Values are read once and by whole lines: past the caches (64 sequences of 4096
   // e4m3 tokens, 537 MB: 109 -> 86 us; of 1024 bf16 tokens and 16 heads 100 -> 83).  A
@@ -116,14 +173,24 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   auto load = [&](Step& st, int i, int kp, int vp) {
     const int blk = step_blk(i);
     const int kb = min(blk + kblk, last_blk), vb = min(blk + vblk, last_blk);
-    const char* kp0 = c.k + kv_block_offset<kBlockBytes>(c, kv_page(c, kp), hk, kb) + koff;
-    const char* vp0 = c.v + kv_block_offset<kBlockBytes>(c, kv_page(c, vp), hk, vb) + voff;
+    const int kpage = SPARSE ? s_page[(kb >> c.lb) - e0] : kv_page(c, kp);
+    const int vpage = SPARSE ? s_page[(vb >> c.lb) - e0] : kv_page(c, vp);
+    const char* kp0 = c.k + kv_block_offset<kBlockBytes>(c, kpage, hk, kb) + koff;
+    const char* vp0 = c.v + kv_block_offset<kBlockBytes>(c, vpage, hk, vb) + voff;
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int u = 0; u < KC; ++u) st.k[t][u] = *reinterpret_cast<const u32x4*>(kp0 + 64 * t + 1024 * u);
+      for (int u = 0; u < KC; ++u)
+        st.k[t][u] = *reinterpret_cast<const typename Step::Piece*>(kp0 + 64 * t + 1024 * u);
 #pragma unroll
-    for (int t = 0; t < DT; ++t) st.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp0 + 256 * t));
+    for (int t = 0; t < VT; ++t) st.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp0 + 256 * t));
+    if constexpr (E2) {
+      const char* ks = c.k + kv_scale_offset<D>(c, kpage, hk, kb);
+      const char* vs = c.v + kv_scale_offset<D>(c, vpage, hk, vb);
+      st.ks = *reinterpret_cast<const uint32_t*>(ks + 16 * (D == 64 ? quarter >> 1 : quarter) + 4 * (n & 3));
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) st.vs[t] = *reinterpret_cast<const u32x4*>(vs + 16 * t);
+    }
   };
 
   f32x4 acc[DT];
@@ -142,7 +209,13 @@ __global__ void __launch_bounds__(kDecThreads, 2)
       sv[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < KC; ++u) {
-        if constexpr (E4) {
+        if constexpr (E2) {
+          const float scale = e8m0_scale(st.ks, t);
+#pragma unroll
+          for (int w = 0; w < D / 32; ++w)
+            sv[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e2m1_to_bf16(st.k[t][u][w], scale)), qf[w], sv[t],
+                                                            0, 0, 0);
+        } else if constexpr (E4) {
           sv[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e4m3_to_bf16(st.k[t][u][0], st.k[t][u][1])),
                                                           qf[2 * u], sv[t], 0, 0, 0);
           sv[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(e4m3_to_bf16(st.k[t][u][2], st.k[t][u][3])),
@@ -153,12 +226,18 @@ __global__ void __launch_bounds__(kDecThreads, 2)
       }
     }
     // lane (n, quarter): score (t, r) is of key key0 + 4 KT quarter + 4 t + r
-    const int lane_key = key0 + 4 * KT * quarter;
+    int lane_key = key0 + 4 * KT * quarter;
+    if (SPARSE) {
+      const int vb = min((key0 >> 4) + vblk, last_blk), at = s_sel[(vb >> c.lb) - e0];
+      lane_key = (((at << c.lb) + (vb & ((1 << c.lb) - 1))) << 4) + (KT == 4 ? 0 : 8 * (quarter & 1));
+      if (at >= b.max_pages || (key0 >> 4) + vblk > last_blk) lane_key = kNowhere;
+    }
     const float dist = (float)(lane_key - pos);
     float x[4 * KT];
 #pragma unroll
     for (int e = 0; e < 4 * KT; ++e) x[e] = score2<MODE>(sv[e / 4][e % 4], sc, slope2, dist + (float)e);
-    const bool whole = (key0 >= wstart && key0 + KS <= len) || key0 + KS <= pre;
+    const bool whole = SPARSE ? __all(lane_key >= wstart && lane_key + 4 * KT <= len)
+                              : (key0 >= wstart && key0 + KS <= len) || key0 + KS <= pre;
     if (!whole) {
       // keys out of sight: weight 0, and values 0 whatever the cache holds there
       uint32_t seen = 0;
@@ -170,7 +249,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
         seen |= in ? 1u << e : 0u;
       }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < (E2 ? 8 : 4); ++w) {
         uint32_t keep = 0;
         if constexpr (E4) {
 #pragma unroll
@@ -178,8 +257,14 @@ __global__ void __launch_bounds__(kDecThreads, 2)
         } else {
           keep = ((seen >> (2 * w)) & 1u ? 0xffffu : 0u) | ((seen >> (2 * w + 1)) & 1u ? 0xffff0000u : 0u);
         }
+        // (an e2m1 code is always a number: it is the scales that may be anything)
+        if constexpr (E2) {
 #pragma unroll
-        for (int t = 0; t < DT; ++t) st.v[t][w] &= keep;
+          for (int t = 0; t < D / 64; ++t) st.vs[2 * t + w / 4][w % 4] &= keep;
+        } else {
+#pragma unroll
+          for (int t = 0; t < DT; ++t) st.v[t][w] &= keep;
+        }
       }
     }
     float mx = x[0];
@@ -203,20 +288,40 @@ __global__ void __launch_bounds__(kDecThreads, 2)
       l += x[e];
     }
     // for the matrix units the weights are rounded to bf16, by up to 2^-8 of each (values are
-    // bf16 or less, and so is the result); their sum takes them as they are
+    // bf16 or less, and so is the result); their sum takes them as they are.  Those of e2m1 values
+    // are multiplied with the values' scales first, and the values are their codes'.
+    if constexpr (E2) {
 #pragma unroll
-    for (int w = 0; w < KT / 2; ++w) {
-      u32x4 pr;
+      for (int w = 0; w < KT / 2; ++w)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pr[e] = bf16_pair(x[8 * w + 2 * e], x[8 * w + 2 * e + 1]);
-      const bf16x8 p = as_bf16x8(pr);
+        for (int h = 0; h < D / 64; ++h) {
+          u32x4 pr;
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        if constexpr (E4)
-          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              as_bf16x8(e4m3_to_bf16(st.v[t][2 * w], st.v[t][2 * w + 1])), p, acc[t], 0, 0, 0);
-        else
-          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(st.v[t]), p, acc[t], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t vs = st.vs[2 * h + w][e];
+            pr[e] = bf16_pair(x[8 * w + 2 * e] * half_of(vs, 0), x[8 * w + 2 * e + 1] * half_of(vs, 1));
+          }
+          const bf16x8 p = as_bf16x8(pr);
+#pragma unroll
+          for (int t = 4 * h; t < 4 * h + 4; ++t)
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                as_bf16x8(e2m1_to_bf16(st.v[t / 2][2 * (t & 1) + w], 1.0f)), p, acc[t], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int w = 0; w < KT / 2; ++w) {
+        u32x4 pr;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pr[e] = bf16_pair(x[8 * w + 2 * e], x[8 * w + 2 * e + 1]);
+        const bf16x8 p = as_bf16x8(pr);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          if constexpr (E4)
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                as_bf16x8(e4m3_to_bf16(st.v[t][2 * w], st.v[t][2 * w + 1])), p, acc[t], 0, 0, 0);
+          else
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(st.v[t]), p, acc[t], 0, 0, 0);
+        }
       }
     }
   };
@@ -226,11 +331,12 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   if (it < i_end) {
     Step s0, s1;
     auto ids = [&](int i, int& kp, int& vp) {
+      if (SPARSE) return;
       const int blk = step_blk(min(i, i_end - 1));
       kp = page_of(blk + kblk);
       vp = page_of(blk + vblk);
     };
-    int kp0, vp0, kp1, vp1;
+    int kp0 = 0, vp0 = 0, kp1 = 0, vp1 = 0;
     ids(it, kp0, vp0);
     ids(it + kDecWaves, kp1, vp1);
     load(s0, it, kp0, vp0);
@@ -254,7 +360,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
     s_ml[0][wave][n] = m;
     s_ml[1][wave][n] = l;
   }
-  __syncthreads();
+  __syncthreads();                   // (and the lists of a sparse call have been read)
   float M = kNegInf;
 #pragma unroll
   for (int w = 0; w < kDecWaves; ++w) M = fmaxf(M, s_ml[0][w][n]);
@@ -292,10 +398,10 @@ __global__ void __launch_bounds__(kDecThreads, 2)
       u32x2 w;
       w[0] = L == 0.0f ? 0u : bf16_pair(r[0] * f1, r[1] * f1);
       w[1] = L == 0.0f ? 0u : bf16_pair(r[2] * f1, r[3] * f1);
-      *reinterpret_cast<u32x2*>(o.p + (size_t)s * o.stride + (size_t)hq * D + d) = w;
-      if (lse && d == 0) lse[(size_t)s * a.Hq + hq] = L == 0.0f ? kNegInf : (Mh0 + __log2f(L)) * kLn2;
+      *reinterpret_cast<u32x2*>(o.p + (size_t)row * o.stride + (size_t)hq * D + d) = w;
+      if (lse && d == 0) lse[(size_t)row * a.Hq + hq] = L == 0.0f ? kNegInf : (Mh0 + __log2f(L)) * kLn2;
     } else {
-      const size_t part = ((size_t)s * a.Hq + hq) * sp.nsplit + split;
+      const size_t part = ((size_t)row * a.Hq + hq) * sp.nsplit + split;
       if (L != 0.0f) *reinterpret_cast<f32x4*>(sp.o + part * D + d) = r;
       if (d == 0) {
         sp.ml[2 * part] = Mh0;
@@ -465,36 +571,62 @@ size_t attn_workspace_bytes(int T, int Hq, int Hkv, int D) {
   return rows * (size_t)(D + 2) * sizeof(float);
 }
 
-template <int D, bool E4>
-static void decode_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
-                          const SplitArgs& sp, int head_tiles, hipStream_t stream) {
-  const dim3 grid((unsigned)((size_t)b.S * c.Hkv * head_tiles * sp.nsplit));
-  with_score_mode(a, [&](auto mode) {
-    hipLaunchKernelGGL((attn_decode_kernel<D, E4, decltype(mode)::value>), grid, dim3(kDecThreads), 0, stream, q, b,
-                       c, a, o, lse, sp, head_tiles);
+template <int D, bool SPARSE>
+static void decode_launch(RowsIn q, int rows, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
+                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse,
+                          hipStream_t stream) {
+  const dim3 grid((unsigned)((size_t)rows * c.Hkv * head_tiles * sp.nsplit));
+  with_kv_kind(c, [&](auto kind) {
+    with_score_mode(a, [&](auto mode) {
+      hipLaunchKernelGGL((attn_decode_kernel<D, decltype(kind)::value, decltype(mode)::value, SPARSE>), grid,
+                         dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp, head_tiles, sparse);
+    });
   });
+}
+
+// Keys of a step, and bytes of a key and its value.
+static int step_keys(const KvArgs& c) { return c.kind == MC_KV_BF16 ? 32 : 64; }
+static int pair_bytes(const KvArgs& c, int D) {
+  return c.kind == MC_KV_BF16 ? 4 * D : c.kind == MC_KV_E4M3 ? 2 * D : D + D / 16;
 }
 
 hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
                               float* lse, int max_len, void* ws, hipStream_t stream) {
-  const bool e4 = c.k_scale != nullptr;
   const int head_tiles = (a.g + kDecHeads - 1) / kDecHeads;
   if (a.window > 0 && !a.prefix && a.window < max_len) max_len = a.window;
   SplitArgs sp;
-  sp.nsplit = decode_splits(b.S, c.Hkv, head_tiles, max_len, (e4 ? 64 : 32) * kDecWaves, D * (e4 ? 2 : 4));
+  sp.nsplit = decode_splits(b.S, c.Hkv, head_tiles, max_len, step_keys(c) * kDecWaves, pair_bytes(c, D));
   sp.o = static_cast<float*>(ws);
   sp.ml = sp.o + (size_t)b.S * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnDecode);
   if (D == 64)
-    e4 ? decode_launch<64, true>(q, b, c, a, o, lse, sp, head_tiles, stream)
-       : decode_launch<64, false>(q, b, c, a, o, lse, sp, head_tiles, stream);
+    decode_launch<64, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
   else
-    e4 ? decode_launch<128, true>(q, b, c, a, o, lse, sp, head_tiles, stream)
-       : decode_launch<128, false>(q, b, c, a, o, lse, sp, head_tiles, stream);
+    decode_launch<128, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
   timing_end(stream, kSiteAttnDecode);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;
   return launch_attn_join(sp, b.S, a.Hq, a.g, D, c.v_scale, o, lse, nullptr, stream);
+}
+
+hipError_t launch_attn_sparse(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a,
+                              const int32_t* sel, const int32_t* count, int n_sel, RowsOut o, float* lse, void* ws,
+                              hipStream_t stream) {
+  const int rows = b.q_start ? b.T : b.S, head_tiles = (a.g + kDecHeads - 1) / kDecHeads;
+  const int keys = (n_sel << c.lb) * kKvBlock;
+  SplitArgs sp;
+  sp.nsplit = decode_splits(rows, c.Hkv, head_tiles, keys, step_keys(c) * kDecWaves, pair_bytes(c, D));
+  sp.o = static_cast<float*>(ws);
+  sp.ml = sp.o + (size_t)rows * a.Hq * sp.nsplit * D;
+  timing_begin(stream, kSiteAttnSparse);
+  if (D == 64)
+    decode_launch<64, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
+  else
+    decode_launch<128, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
+  timing_end(stream, kSiteAttnSparse);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess || sp.nsplit == 1) return err;
+  return launch_attn_join(sp, rows, a.Hq, a.g, D, c.v_scale, o, lse, b.q_start ? &b : nullptr, stream);
 }
 
 }  // namespace mc

@@ -64,11 +64,12 @@ size_t attn_importance_bytes(int Hq, int L) {
 // products a fraction of one.
 constexpr int kColRing = 4;
 
-template <int D, bool E4, int MODE>
+template <int D, int KV, int MODE>
 __global__ void __launch_bounds__(kColThreads, 2)
     attn_colsum_kernel(RowsIn q, const float* __restrict__ lse, BatchArgs b, KvArgs c, ScoreArgs a, int L, int slices,
                        float* __restrict__ partial) {
-  constexpr int DK = D / 16, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2), kRowBytes = 32 * D * 2;
+  constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  constexpr int DK = D / 16, kBlockBytes = KvFormat<D, KV>::kBlockBytes, kRowBytes = 32 * D * 2;
   constexpr int kLoads = D / 64 + 1;            // direct loads of a wave for a row tile
   // a tile's queries, then its rows' lse: a copy for each wave, twice over the half waves
   constexpr int kSlotBytes = kRowBytes + kColWaves * 256;
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(kColThreads, 2)
   for (int i = 0; i < kColRing - 1; ++i)
     if (i < count) fetch(s_ring + i * kSlotBytes);
   // keys: lane (key n of 32, half) holds units half, half + 2, ... (bf16), or units of
-  // 16 whose first and last 8 dimensions go to two steps (e4m3).
+  // 16 whose first and last 8 dimensions go to two steps (e4m3), or of 32 that go to four (e2m1).
   bf16x8 kf[2][DK];
   const int last_blk = (L - 1) >> 4;
 #pragma unroll
@@ -141,6 +142,15 @@ __global__ void __launch_bounds__(kColThreads, 2)
         const u32x4 r = *reinterpret_cast<const u32x4*>(kp + 512 * i);
         kf[h][2 * i] = as_bf16x8(e4m3_to_bf16(r[0], r[1]));
         kf[h][2 * i + 1] = as_bf16x8(e4m3_to_bf16(r[2], r[3]));
+      }
+    } else if constexpr (E2) {
+      const uint8_t* ks = reinterpret_cast<const uint8_t*>(c.k + kv_scale_offset<D>(c, page, hk, blk));
+#pragma unroll
+      for (int i = 0; i < DK / 4; ++i) {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(kp + 512 * i);
+        const float scale = __uint_as_float((uint32_t)ks[16 * (2 * i + half) + 4 * (n & 3) + ((n & 15) >> 2)] << 23);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) kf[h][4 * i + u] = as_bf16x8(e2m1_to_bf16(r[u], scale));
       }
     } else {
 #pragma unroll
@@ -158,9 +168,9 @@ __global__ void __launch_bounds__(kColThreads, 2)
       for (int r = 0; r < 16; ++r) sv[h][r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < DK; ++i) {
-      // unit 2 i + half, or for e4m3 units 2 (i & ~1) + 2 half + (i & 1): the
-      // dimensions of the key's unit
-      const int u = E4 ? 2 * (i & ~1) + 2 * half + (i & 1) : 2 * i + half;
+      // unit 2 i + half, or for e4m3 units 2 (i & ~1) + 2 half + (i & 1), for e2m1 2 (i & ~3) + 4
+      // half + (i & 3): the dimensions of the key's unit
+      const int u = E2 ? 2 * (i & ~3) + 4 * half + (i & 3) : E4 ? 2 * (i & ~1) + 2 * half + (i & 1) : 2 * i + half;
       const bf16x8 qv = as_bf16x8(*reinterpret_cast<const u32x4*>(slot + u * 512 + n * 16));
 #pragma unroll
       for (int h = 0; h < 2; ++h) sv[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][i], qv, sv[h], 0, 0, 0);
@@ -307,12 +317,12 @@ __global__ void __launch_bounds__(kFinishThreads) attn_finish_kernel(const float
   }
 }
 
-template <int D, bool E4>
+template <int D, int KV>
 static void colsum_launch(RowsIn q, const float* lse, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, int L,
                           int slices, float* partial, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)col_tiles(L) * slices * c.Hkv));
   with_score_mode(a, [&](auto mode) {
-    hipLaunchKernelGGL((attn_colsum_kernel<D, E4, decltype(mode)::value>), grid, dim3(kColThreads), 0, stream, q,
+    hipLaunchKernelGGL((attn_colsum_kernel<D, KV, decltype(mode)::value>), grid, dim3(kColThreads), 0, stream, q,
                        lse, b, c, a, L, slices, partial);
   });
 }
@@ -323,14 +333,12 @@ hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const Batch
   const int L = b.T, slices = col_slices(L, c.Hkv, a.g);
   float* partial = static_cast<float*>(ws);
   uint64_t* keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + col_partial_bytes(L, c.Hkv, a.g));
-  const bool e4 = c.k_scale != nullptr;
   timing_begin(stream, kSiteAttnColsum);
-  if (D == 64)
-    e4 ? colsum_launch<64, true>(q, lse, b, c, a, L, slices, partial, stream)
-       : colsum_launch<64, false>(q, lse, b, c, a, L, slices, partial, stream);
-  else
-    e4 ? colsum_launch<128, true>(q, lse, b, c, a, L, slices, partial, stream)
-       : colsum_launch<128, false>(q, lse, b, c, a, L, slices, partial, stream);
+  with_kv_kind(c, [&](auto kind) {
+    constexpr int KV = decltype(kind)::value;
+    D == 64 ? colsum_launch<64, KV>(q, lse, b, c, a, L, slices, partial, stream)
+            : colsum_launch<128, KV>(q, lse, b, c, a, L, slices, partial, stream);
+  });
   timing_end(stream, kSiteAttnColsum);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;

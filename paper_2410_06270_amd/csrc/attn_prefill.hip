@@ -129,17 +129,19 @@ __device__ __forceinline__ void interleave() {
 }
 
 // MODE: as score2 (attn.hpp).
-template <int D, bool E4, int MODE, int G>
+template <int D, int KV, int MODE, int G>
 __global__ void __launch_bounds__(G * kPreThreads, 2)
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                         int slots) {
   constexpr int DT = D / 32, DK = D / 16;      // value tiles; score steps
   constexpr int kTileBytes = kPreKeys * D * 2, kBlk = kKvBlock * D * 2;      // in LDS: bf16
-  constexpr int kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);                   // in the cache
-  constexpr int kPieces = kBlockBytes / 1024, kUnit = E4 ? 16 : 8;
+  constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1, kWiden = KV != MC_KV_BF16;
+  constexpr int kBlockBytes = KvFormat<D, KV>::kBlockBytes;                  // in the cache
+  constexpr int kPieces = (kBlockBytes + 1023) / 1024, kUnit = kWiden ? 16 : 8;
+  constexpr int kRawBytes = 1024 * kPieces + (E2 ? 256 : 0);                 // a block as it lies in the cache, in LDS
   // one array: for several the compiler keeps marks of its own that replace those
   // of the parameters of round() below, and then waits for every load before a read
-  constexpr int kTeamBytes = 4 * kTileBytes + (E4 ? kPreWaves * 2 * kBlockBytes : 0);
+  constexpr int kTeamBytes = 4 * kTileBytes + (kWiden ? kPreWaves * 2 * kRawBytes : 0);
   __shared__ __attribute__((aligned(16))) char s_all[G * kTeamBytes];
   const int team = G == 1 ? 0 : wave_id() / kPreWaves, wave = wave_id() % kPreWaves;
   char* const s_lds = s_all + team * kTeamBytes;
@@ -223,14 +225,18 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // A tile's 4 blocks of keys and 4 of values: wave w takes block w of each, both
   // at the same offset.  The lanes find the offsets of 64 tiles together, from `known` on.
   int known = t_begin;
-  uint32_t off_lo = 0, off_hi = 0;
+  // (e2m1: of the codes; their scales lie behind the codes of the page)
+  uint32_t off_lo = 0, off_hi = 0, off_scale = 0;
   auto find_offsets = [&]() {
     const int blk = min((tile_key(min(known + lane, max(t_end - 1, 0))) >> 4) + wave, last_blk);
-    const size_t off = kv_block_offset<kBlockBytes>(c, kv_page(c, pages[blk >> c.lb]), hk, blk);
+    const int page = kv_page(c, pages[blk >> c.lb]);
+    const size_t off = kv_block_offset<kBlockBytes>(c, page, hk, blk);
     off_lo = (uint32_t)off;
     off_hi = (uint32_t)(off >> 32);
+    if constexpr (E2) off_scale = (uint32_t)(kv_scale_offset<D>(c, page, hk, blk) - off);
   };
-  auto fetch = [&](const char* from, size_t off, char* to) {
+  auto fetch = [&](const char* from, size_t off, uint32_t scale, char* to) {
+    if constexpr (E2) lds_dma4(buffer_of(from + off + scale, D / 2), 4 * lane, to + 1024 * kPieces);
     const Buffer src = buffer_of(from + off, kBlockBytes);
     lds_dma16<0>(src, 16 * lane, 0, to);
     if constexpr (kPieces > 1) lds_dma16<1024>(src, 16 * lane, 0, to);
@@ -241,8 +247,40 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   };
   // e4m3: a fetched block's units, widened to bf16 units.  Unit x of the keys is
   // (16 dimensions, token): two bf16 units, 256 bytes apart; of the values (dimension,
-  // 16 tokens): D * 16 apart.
+  // 16 tokens): D * 16 apart.  e2m1: unit x of the keys is (32 dimensions, token) and its scale
+  // byte 16 (x / 16) + 4 (token % 4) + token / 4; of the values two dimensions, 16 apart, of 16 tokens, each
+  // of which has a scale for 64 dimensions: the product is a bf16 number (a scale has 6
+  // significant bits, a code 2).
   auto widen = [&](const char* raw, bool keys, char* to) {
+    if constexpr (E2) {
+      if (D == 64 && lane >= 32) return;               // a block of 32 units
+      const u32x4 w = *reinterpret_cast<const u32x4*>(raw + 16 * lane);
+      const int j = lane >> 4, t = lane & 15;
+      if (keys) {
+        const float scale =
+            __uint_as_float((uint32_t)reinterpret_cast<const uint8_t*>(raw)[1024 + 16 * j + 4 * (t & 3) + (t >> 2)]
+                            << 23);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<u32x4*>(to + (4 * j + u) * 256 + t * 16) = e2m1_to_bf16(w[u], scale);
+      } else {
+        const u32x4* sc = reinterpret_cast<const u32x4*>(raw + 1024 + 32 * (j >> 1));
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {                  // eight tokens
+          const u32x4 vs = sc[g];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                // dimensions 32 j + 16 h + t
+            const u32x4 codes = e2m1_to_bf16(w[2 * h + g], 1.0f);
+            u32x4 r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              r[e] = bf16_pair(half_of(codes[e], 0) * half_of(vs[e], 0), half_of(codes[e], 1) * half_of(vs[e], 1));
+            *reinterpret_cast<u32x4*>(to + (g * D + 32 * j + 16 * h + t) * 16) = r;
+          }
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const u32x4 w = *reinterpret_cast<const u32x4*>(raw + 1024 * i + 16 * lane);
@@ -388,13 +426,14 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // more, the ones before being widened).  The buffers are distinct and passed as
   // such: reads of one do not wait for the loads into another.
   size_t off_v = 0;                                    // of the next tile of values
+  uint32_t scale_v = 0;
   float mul = 1.0f;
   bool odd = false;
-  char* raw_k = s_lds + 4 * kTileBytes + wave * 2 * kBlockBytes;      // e4m3 only
-  char* raw_v = raw_k + (E4 ? kBlockBytes : 0);
+  char* raw_k = s_lds + 4 * kTileBytes + wave * 2 * kRawBytes;        // not of bf16
+  char* raw_v = raw_k + (kWiden ? kRawBytes : 0);
   // the values of tile t - 1 and the keys of tile t
   auto load = [&](int t, char* kt, char* vt) {
-    if (t > t_begin && t <= t_end) fetch(c.v, off_v, E4 ? raw_v : vt + wave * kBlk);
+    if (t > t_begin && t <= t_end) fetch(c.v, off_v, scale_v, kWiden ? raw_v : vt + wave * kBlk);
     if (t >= t_end) return;
     if (t == known + 64) {
       known = t;
@@ -402,7 +441,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     }
     off_v = (size_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, t - known) << 32 |
             (uint32_t)__builtin_amdgcn_readlane(off_lo, t - known);
-    fetch(c.k, off_v, E4 ? raw_k : kt + wave * kBlk);
+    if constexpr (E2) scale_v = __builtin_amdgcn_readlane(off_scale, t - known);
+    fetch(c.k, off_v, scale_v, kWiden ? raw_k : kt + wave * kBlk);
   };
   auto lds_done = [&]() {                              // what was read may be overwritten
     asm volatile("" ::: "memory");
@@ -411,7 +451,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   };
   auto round = [&](const char* __restrict__ kt, const char* __restrict__ vt, char* __restrict__ knext,
                    char* __restrict__ vnext, f32x16 (&cur)[2], f32x16 (&nxt)[2], int t) {
-    if constexpr (E4) {
+    if constexpr (kWiden) {
       if (t + 2 < t_end) widen(raw_k, true, knext + wave * kBlk);
       if (t + 1 < t_end) widen(raw_v, false, vnext + wave * kBlk);
       lds_done();
@@ -439,9 +479,9 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   // what the last round loaded is in LDS once every wave's loads are; the barrier
   // also ends every wave's reads of the buffers that are filled next
   auto begin_round = [&](char* vt, int t) {
-    if constexpr (!E4) wait_vmcnt<0>();
+    if constexpr (!kWiden) wait_vmcnt<0>();
     lds_barrier();
-    if constexpr (E4) loads_landed();
+    if constexpr (kWiden) loads_landed();
     bool any = false;                                  // a tile of some team
 #pragma unroll
     for (int tm = 0; tm < G; ++tm) {
@@ -457,13 +497,13 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
     f32x16 sa[2], sb[2];
     find_offsets();
     load(t_begin, s_k[0], s_v[1]);
-    if constexpr (E4) {
+    if constexpr (kWiden) {
       loads_landed();
       widen(raw_k, true, s_k[0] + wave * kBlk);
       lds_done();
     }
     load(t_begin + 1, s_k[1], s_v[0]);
-    if constexpr (E4) {
+    if constexpr (kWiden) {
       loads_landed();
       if (t_begin + 1 < t_end) widen(raw_k, true, s_k[1] + wave * kBlk);
       widen(raw_v, false, s_v[0] + wave * kBlk);
@@ -498,9 +538,23 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
         const int t = t_begin + i / kPreKeys, j = tile_key(t) + i % kPreKeys;
         if (j >= len || !edge(t)) continue;
         const int blk = j >> 4, page = kv_page(c, pages[blk >> c.lb]), u = (j & 15) / kUnit;
-        const char* vj = c.v + kv_block_offset<kBlockBytes>(c, page, hk, blk) + u * D * 16 + 64 * half +
-                         (j % kUnit) * (E4 ? 1 : 2);
+        const char* vj = c.v + kv_block_offset<kBlockBytes>(c, page, hk, blk);
         const bool in = visible(Mask{pos, rlow, rpre}, j);
+        if constexpr (E2) {
+          const uint16_t* vs = reinterpret_cast<const uint16_t*>(c.v + kv_scale_offset<D>(c, page, hk, blk));
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int i = 8 * (r >> 2) + 4 * half + (r & 3);           // of the 32 dimensions
+              const uint32_t w = (uint8_t)vj[256 * d + 16 * (i & 15) + 8 * (i >> 4) + ((j & 15) >> 1)];
+              const float x = e2m1_value((w >> (4 * (j & 1))) & 15u) *
+                              bf16_bits_to_float(vs[16 * (d >> 1) + (j & 15)]);
+              acc[d][r] += in && !(fabsf(x) < -kNegInf) ? x : 0.0f;
+            }
+          continue;
+        }
+        vj += u * D * 16 + 64 * half + (j % kUnit) * (E4 ? 1 : 2);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -577,7 +631,7 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
   if (lse && half == 0) lse[out_row * a.Hq + head] = l == 0.0f ? kNegInf : (m0 + __log2f(l)) * kLn2;
 }
 
-template <int D, bool E4>
+template <int D, int KV>
 static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                            const SplitArgs& sp, int slots, int max_len, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)slots * c.Hkv * sp.nsplit));
@@ -585,19 +639,18 @@ static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const 
     constexpr int MODE = decltype(mode)::value;
     if constexpr (D == 64) {
       if (prefill_two_teams(slots, c.Hkv, sp.nsplit, max_len)) {
-        hipLaunchKernelGGL((attn_prefill_kernel<D, E4, MODE, 2>), grid, dim3(2 * kPreThreads), 0, stream, q, b, c, a,
+        hipLaunchKernelGGL((attn_prefill_kernel<D, KV, MODE, 2>), grid, dim3(2 * kPreThreads), 0, stream, q, b, c, a,
                            o, lse, sp, slots);
         return;
       }
     }
-    hipLaunchKernelGGL((attn_prefill_kernel<D, E4, MODE, 1>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse,
+    hipLaunchKernelGGL((attn_prefill_kernel<D, KV, MODE, 1>), grid, dim3(kPreThreads), 0, stream, q, b, c, a, o, lse,
                        sp, slots);
   });
 }
 
 hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
                                float* lse, int max_len, void* ws, hipStream_t stream) {
-  const bool e4 = c.k_scale != nullptr;
   const int slots = prefill_slots(b.T, b.S, a.g);
   if (a.window > 0 && !a.prefix && a.window + kPreRows < max_len) max_len = a.window + kPreRows;
   SplitArgs sp;
@@ -605,12 +658,11 @@ hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs
   sp.o = static_cast<float*>(ws);
   sp.ml = sp.o + (size_t)b.T * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnPrefill);
-  if (D == 64)
-    e4 ? prefill_launch<64, true>(q, b, c, a, o, lse, sp, slots, max_len, stream)
-       : prefill_launch<64, false>(q, b, c, a, o, lse, sp, slots, max_len, stream);
-  else
-    e4 ? prefill_launch<128, true>(q, b, c, a, o, lse, sp, slots, max_len, stream)
-       : prefill_launch<128, false>(q, b, c, a, o, lse, sp, slots, max_len, stream);
+  with_kv_kind(c, [&](auto kind) {
+    constexpr int KV = decltype(kind)::value;
+    D == 64 ? prefill_launch<64, KV>(q, b, c, a, o, lse, sp, slots, max_len, stream)
+            : prefill_launch<128, KV>(q, b, c, a, o, lse, sp, slots, max_len, stream);
+  });
   timing_end(stream, kSiteAttnPrefill);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;

@@ -24,8 +24,6 @@ __host__ __device__ constexpr int row_chunks(int norm) { return norm == 2 ? 8 : 
 // floor(q_start[s] / U) + 2 s on, at least floor(n / U) + 2 of them.
 __host__ __device__ static inline int append_slots(int T, int S, int U) { return T / U + 2 * S; }
 
-__device__ __forceinline__ float half_of(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xffff0000u : w << 16); }
-
 // Where a token goes: false if it is skipped.
 struct Place {
   int pos, page;
@@ -38,11 +36,90 @@ __device__ __forceinline__ bool append_place(const KvArgs& c, const BatchArgs& b
   return out.page >= 0 && out.page < c.n_pages;
 }
 
+// ------------------------------------------------------------------ e2m1 --
+// Groups of e2m1 codes share a scale.  Of keys, 32 dimensions: 2^e, e the least with max|y| <=
+// 7 2^e (7 being the border between 6, the largest level, and the next that there would be).  Of
+// values, 64 dimensions: max|v| / 6, rounded to 6 significant bits so that its products with the codes
+// are bf16 numbers.  Groups below 2^-100 are 0, those with a NaN, an infinity or more than 7 2^125 NaN.
+constexpr double kGroupLeast = 0x1p-100, kGroupMost = 0x1.cp127;
+
+// Byte of the scale 2^(byte - 127) of a group of keys whose largest magnitude is m (NaN: 255).
+__device__ __forceinline__ uint32_t key_scale_byte(double m) {
+  if (!(m <= kGroupMost)) return 255u;
+  if (m < kGroupLeast) return 0u;
+  const unsigned long long b = __double_as_longlong(m);
+  // m = 2^k (1 + f): e = k - 2, or k - 1 where 1 + f > 7/4
+  const int k = (int)(b >> 52) - 1023;
+  return (uint32_t)(k - 2 + ((b & 0xfffffffffffffull) > 0xc000000000000ull ? 1 : 0) + 127);
+}
+
+// The scale of a group of values (bf16) whose largest magnitude is m, as a float.
+__device__ __forceinline__ float value_scale(float m) {
+  if (!(m <= (float)kGroupMost)) return __uint_as_float(0x7fc00000u);
+  if (m < (float)kGroupLeast) return 0.0f;
+  uint32_t u = __float_as_uint(m / 6.0f);               // IEEE division
+  u += 0x1ffffu + ((u >> 18) & 1u);
+  return __uint_as_float(u & ~0x3ffffu);
+}
+
+// The larger magnitude, NaN if one of them is (fmaxf would drop it).
+__device__ __forceinline__ float magnitude(float a, float b) {
+  a = fabsf(a);
+  b = fabsf(b);
+  return a >= b || a != a ? a : b;
+}
+__device__ __forceinline__ double magnitude(double a, double b) {
+  a = fabs(a);
+  b = fabs(b);
+  return a >= b || a != a ? a : b;
+}
+
+// x of the lane that the DPP control names.
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double x) {
+  const unsigned long long b = __double_as_longlong(x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)b, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double(((long long)hi << 32) | lo);
+}
+
+// Two codes, each the nearest to x (ties to the even code, magnitudes above 6 to 6), the first in the
+// low half; into byte `AT` of w.
+template <int AT>
+__device__ __forceinline__ uint32_t e2m1_pair(uint32_t w, float a, float b) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, 1.0f, AT);
+}
+
+// A double as a float that every comparison with a border of the codes takes the same way: rounded
+// towards odd (the borders have 3 significant bits).
+__device__ __forceinline__ float sticky_float(double v) {
+  float f = (float)v;
+  if ((double)f != v) {
+    uint32_t b = __float_as_uint(f);
+    if (fabs((double)f) > fabs(v)) b -= 1u;
+    f = __uint_as_float(b | 1u);
+  }
+  return f;
+}
+
+// v / s, so exact that a quotient on a border of the codes is on it: v and s are bf16 numbers, whose
+// quotient is a border (3 significant bits) or away from it by more than 2^-12 of itself, and where it
+// is one the remainder of the first estimate corrects it to the last bit.
+struct Divisor {
+  float s, r;
+  __device__ explicit Divisor(float scale) : s(scale), r(scale > 0.0f ? __builtin_amdgcn_rcpf(scale) : 0.0f) {}
+  __device__ __forceinline__ float operator()(float v) const {
+    const float x = v * r;
+    return __builtin_fmaf(__builtin_fmaf(-s, x, v), r, x);
+  }
+};
+
 // Values of one unit group: lanes hold 8 dimensions each, in pieces of 64.
-template <int D, bool E4>
+template <int D, int KV>
 __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int n_pos, int slot, int piece,
                               u32x4* lds) {
-  constexpr int U = E4 ? 16 : 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
+  constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  constexpr int U = KV == MC_KV_BF16 ? 8 : 16, kBlockBytes = KvFormat<D, KV>::kBlockBytes;
   const int lane = threadIdx.x & 63, chunk = piece * 64 + lane;
   const int s = find_sequence(b.q_start, b.S, slot, U, 2, 1);
   const long long first = b.q_start[s], n = (long long)b.q_start[s + 1] - first;
@@ -73,6 +150,70 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
   auto unit_of = [&](int h) {                    // the group's first unit of head h
     return c.v + kv_block_offset<kBlockBytes>(c, at.page, h, at.pos >> 4) + (size_t)(in_block / U) * D * 16;
   };
+  if constexpr (E2) {
+    // lane: dimensions d0 .. d0 + 7, half of a unit's eight bytes; 64 dimensions in 8 neighbouring lanes
+    if (!mine) return;                           // (whole groups of 8 lanes are)
+    const int blk = at.pos >> 4;
+    char* codes = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, blk) + d0 / 32 * 256 + (d0 & 15) * 16 +
+                  (d0 / 16 & 1) * 8;
+    uint16_t* scales = reinterpret_cast<uint16_t*>(c.v + kv_scale_offset<D>(c, at.page, head, blk)) + d0 / 64 * 16;
+    // the other tokens' codes of the bytes
+    u32x2 w[8];
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x2*>(codes + 16 * i);
+    }
+    uint32_t sw[8] = {};
+    float x[16][8];
+    uint32_t live = 0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const long long pos = base + u, row = first + pos - p0;
+      const bool in = pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T;
+      live |= in ? 1u << u : 0u;
+      float m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[u][i] = half_of(raw[u][i / 2], i & 1);
+        m = magnitude(x[u][i], m);
+      }
+      m = magnitude(m, dpp<0xb1>(m));
+      m = magnitude(m, dpp<0x4e>(m));
+      m = magnitude(m, dpp<0x141>(m));
+      const float s = value_scale(m);
+      sw[u / 2] |= (__float_as_uint(s) >> 16) << (16 * (u & 1));
+      const Divisor by(s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[u][i] = s > 0.0f ? by(x[u][i]) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u32x2 r;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t t = 0;
+        t = e2m1_pair<0>(t, x[8 * q][i], x[8 * q + 1][i]);
+        t = e2m1_pair<1>(t, x[8 * q + 2][i], x[8 * q + 3][i]);
+        t = e2m1_pair<2>(t, x[8 * q + 4][i], x[8 * q + 5][i]);
+        t = e2m1_pair<3>(t, x[8 * q + 6][i], x[8 * q + 7][i]);
+        if (!all) {
+          uint32_t keep = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) keep |= (live >> (8 * q + e)) & 1u ? 0u : 0xfu << (4 * e);
+          t = (t & ~keep) | (w[i][q] & keep);
+        }
+        r[q] = t;
+      }
+      // bytes of other tokens are written back as they were: nobody else writes this block's values
+      *reinterpret_cast<u32x2*>(codes + 16 * i) = r;
+    }
+    if ((lane & 7) == 0) {
+#pragma unroll
+      for (int u = 0; u < 16; ++u)
+        if ((live >> u) & 1u) scales[u] = (uint16_t)(sw[u / 2] >> (16 * (u & 1)));
+    }
+    return;
+  }
   const float sc = E4 ? 1.0f / c.v_scale[head] : 1.0f;
   if (all) {
     // The lane's 8 units lie side by side.  They go out 64 side by side at a time, by
@@ -141,17 +282,44 @@ __device__ __forceinline__ float head_sum(float x) {
   return x;
 }
 
+__device__ __forceinline__ double square_sum64(const u32x4& r) {
+  double s = 0.0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const double a = half_of(r[q], 0), z = half_of(r[q], 1);
+    s = __builtin_fma(a, a, s);
+    s = __builtin_fma(z, z, s);
+  }
+  return s;
+}
+
+template <int DU>
+__device__ __forceinline__ double head_sum64(double x) {
+  x += dpp64<0xb1>(x);
+  x += dpp64<0x4e>(x);
+  x += dpp64<0x141>(x);
+  if (DU == 16) x += dpp64<0x140>(x);
+  return x;
+}
+
+__device__ __forceinline__ double wave_sum64(double x) {
+  x = head_sum64<16>(x);
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
 // Queries and keys of one token: chunk i of 8 elements in [0, nq + nk), the queries'
 // first, 64 neighbouring ones at a time.  A head's chunks lie in D/8 neighbouring
 // lanes, and a lane's chunks all start at the same dimension of their heads, so that
 // its cosines and sines are loaded once.  A norm over the row needs one wave for the
 // token; without it a wave takes one of its parts of 64 kRowChunks chunks: shorter waves
 // overlap their loads, arithmetic and stores better.
-template <int D, bool E4, int NORM>
+template <int D, int KV, int NORM>
 __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, const BatchArgs& b, const KvArgs& c,
                             RowsOut out, int t, int part) {
   constexpr int kRowChunks = row_chunks(NORM);
-  constexpr int DU = D / 8, kBlockBytes = kKvBlock * D * (E4 ? 1 : 2);
+  constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  constexpr int DU = D / 8, kBlockBytes = KvFormat<D, KV>::kBlockBytes;
   const int lane = threadIdx.x & 63;
   const int nq = q.p ? Hq * DU : 0, total = nq + c.Hkv * DU;
   const uint16_t* qr = q.p + (size_t)t * q.stride;
@@ -197,8 +365,10 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
     wk = *reinterpret_cast<const u32x4*>(p.k_norm + d0);
   }
   float row_scale[2] = {1.0f, 1.0f};
+  double key_scale = 1.0;
   if (NORM == 2) {
     float ss[2] = {0.0f, 0.0f};
+    double sk = 0.0;
     for (int i0 = 0; i0 < total; i0 += 64 * kRowChunks) {
       if (i0) load(i0);
 #pragma unroll
@@ -207,8 +377,10 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
         const bool is_q = i0 + 64 * r + lane < nq;
         ss[0] += is_q ? x : 0.0f;
         ss[1] += is_q ? 0.0f : x;
+        if (E2) sk += is_q ? 0.0 : square_sum64(raw[r]);
       }
     }
+    if (E2) key_scale = 1.0 / sqrt(wave_sum64(sk) / (double)(c.Hkv * D) + (double)p.eps);
     if (total > 64 * kRowChunks) load(0);
 #pragma unroll
     for (int w = 0; w < 2; ++w)
@@ -224,6 +396,69 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
       if (i0 + 64 * r >= total) break;           // the same for the whole wave
       const int i = i0 + 64 * r + lane;
       const bool is_q = i < nq;
+      if constexpr (E2) {
+        // keys in 64 bits, whose rounding next to a border of the codes does not count (the lanes of
+        // a head are all keys or all queries)
+        if (i0 + 64 * r + 63 >= nq) {
+          double y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = (double)half_of(raw[r][j / 2], j & 1);
+          if (NORM) {
+            const double sc =
+                NORM == 2 ? key_scale : 1.0 / sqrt(head_sum64<DU>(square_sum64(raw[r])) * (1.0 / D) + (double)p.eps);
+            u32x4 w = wk;
+            if (NORM == 2 && i < total && !is_q) w = *reinterpret_cast<const u32x4*>(p.k_norm + 8 * (i - nq));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = y[j] * (double)half_of(w[j / 2], j & 1) * sc;
+          }
+          if (p.rot && p.pairs) {
+            if (turns) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const double co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
+                const double a = y[2 * j], z = y[2 * j + 1];
+                y[2 * j] = a * co - z * si;
+                y[2 * j + 1] = z * co + a * si;
+              }
+            }
+          } else if (p.rot) {
+            double o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = p.rot == 128 ? dpp64<0x128>(y[j]) : __shfl(y[j], partner);
+            if (turns) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                y[j] = y[j] * (double)tab[j / 2][2 * (j & 1)] + o[j] * (double)tab[j / 2][2 * (j & 1) + 1];
+            }
+          }
+          double m = 0.0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) m = magnitude(y[j], m);
+          m = magnitude(m, dpp64<0xb1>(m));
+          m = magnitude(m, dpp64<0x4e>(m));              // of the lanes of 32 dimensions
+          const uint32_t byte = key_scale_byte(m);
+          if (i < total && !is_q) {
+            const bool number = byte != 0u && byte != 255u;
+            // 2^(127 - byte)
+            const double by = __longlong_as_double((long long)(1023 + 127 - (int)byte) << 52);
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = number ? sticky_float(y[j] * by) : 0.0f;
+            uint32_t w = 0;
+            w = e2m1_pair<0>(w, f[0], f[1]);
+            w = e2m1_pair<1>(w, f[2], f[3]);
+            w = e2m1_pair<2>(w, f[4], f[5]);
+            w = e2m1_pair<3>(w, f[6], f[7]);
+            const int head = (i - nq) / DU, t16 = at.pos & 15;
+            char* dst = c.k + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4);
+            *reinterpret_cast<uint32_t*>(dst + d0 / 32 * 256 + t16 * 16 + (d0 / 8 & 3) * 4) = w;
+            if ((lane & 3) == 0)
+              c.k[kv_scale_offset<D>(c, at.page, head, at.pos >> 4) + d0 / 32 * 16 + 4 * (t16 & 3) + (t16 >> 2)] =
+                  (char)byte;
+          }
+        }
+        if (i0 + 64 * r >= nq) continue;               // no queries among them
+      }
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = half_of(raw[r][j / 2], j & 1);
@@ -269,7 +504,7 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
         *reinterpret_cast<u32x4*>(out.p + (size_t)t * out.stride + 8 * i) = w;
-      } else {
+      } else if constexpr (!E2) {
         const int head = (i - nq) / DU;
         char* dst = c.k + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4) + (at.pos & 15) * 16;
         if constexpr (E4) {
@@ -293,7 +528,7 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
 // neighbouring tokens share the lines of the key blocks, and workgroups go round the 8
 // XCDs in turn: of 16 row workgroups of a part, number r and r + 8 take 8 neighbouring
 // tokens, so that one XCD's cache sees whole lines.
-template <int D, bool E4, int NORM>
+template <int D, int KV, int NORM>
 __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
                      int slots, int pieces, int parts) {
@@ -302,18 +537,18 @@ __global__ void __launch_bounds__(kAppendThreads)
   if (blk < nv) {
     const int w = blk * (kAppendThreads / 64) + wave_id();
     if (w < slots * pieces)
-      append_values<D, E4>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 512);
+      append_values<D, KV>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 512);
     return;
   }
   const int r0 = blk - nv, group = r0 / (16 * parts), in = r0 - group * 16 * parts, r = in & 15;
   const int t = 4 * (16 * group + 2 * (r & 7) + (r >> 3)) + wave_id();
-  if (t < b.T) append_rows<D, E4, NORM>(q, k, Hq, p, b, c, out, t, in >> 4);
+  if (t < b.T) append_rows<D, KV, NORM>(q, k, Hq, p, b, c, out, t, in >> 4);
 }
 
-template <int D, bool E4>
+template <int D, int KV>
 static void append_launch(RowsIn q, RowsIn k, RowsIn v, int Hq, const QkPrepArgs& p, const BatchArgs& b,
                           const KvArgs& c, RowsOut out, hipStream_t stream) {
-  const int pieces = (c.Hkv * (D / 8) + 63) / 64, slots = append_slots(b.T, b.S, E4 ? 16 : 8);
+  const int pieces = (c.Hkv * (D / 8) + 63) / 64, slots = append_slots(b.T, b.S, KV == MC_KV_BF16 ? 8 : 16);
   const int per = kAppendThreads / 64, nv = (slots * pieces + per - 1) / per;
   const int chunks = ((q.p ? Hq : 0) + c.Hkv) * (D / 8);
   auto launch = [&](auto kernel, int parts) {
@@ -322,24 +557,102 @@ static void append_launch(RowsIn q, RowsIn k, RowsIn v, int Hq, const QkPrepArgs
   };
   const int each = 64 * row_chunks(0);
   if (!p.q_norm)
-    launch(kv_append_kernel<D, E4, 0>, (chunks + each - 1) / each);
+    launch(kv_append_kernel<D, KV, 0>, (chunks + each - 1) / each);
   else if (!p.norm_row)
-    launch(kv_append_kernel<D, E4, 1>, (chunks + each - 1) / each);
+    launch(kv_append_kernel<D, KV, 1>, (chunks + each - 1) / each);
   else
-    launch(kv_append_kernel<D, E4, 2>, 1);
+    launch(kv_append_kernel<D, KV, 2>, 1);
 }
 
 hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const QkPrepArgs& p, const BatchArgs& b,
                             const KvArgs& c, RowsOut out, hipStream_t stream) {
   timing_begin(stream, kSiteKvAppend);
-  const bool e4 = c.k_scale != nullptr;
-  if (D == 64)
-    e4 ? append_launch<64, true>(q, k, v, Hq, p, b, c, out, stream)
-       : append_launch<64, false>(q, k, v, Hq, p, b, c, out, stream);
-  else
-    e4 ? append_launch<128, true>(q, k, v, Hq, p, b, c, out, stream)
-       : append_launch<128, false>(q, k, v, Hq, p, b, c, out, stream);
+  with_kv_kind(c, [&](auto kind) {
+    constexpr int KV = decltype(kind)::value;
+    D == 64 ? append_launch<64, KV>(q, k, v, Hq, p, b, c, out, stream)
+            : append_launch<128, KV>(q, k, v, Hq, p, b, c, out, stream);
+  });
   timing_end(stream, kSiteKvAppend);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------- read --
+// What the cache holds at the new tokens' places: a lane takes 8 dimensions of one token and head,
+// keys and values.
+template <int D, int KV>
+__global__ void __launch_bounds__(kAppendThreads)
+    kv_read_kernel(BatchArgs b, KvArgs c, RowsOut ko, RowsOut vo, int total) {
+  constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
+  constexpr int DU = D / 8, kBlockBytes = KvFormat<D, KV>::kBlockBytes, U = E4 ? 16 : 8;
+  const int id = blockIdx.x * kAppendThreads + threadIdx.x, per = c.Hkv * DU;
+  // a wave's lanes may lie on two tokens or more: each finds its own
+  const int t = id / per, chunk = id - t * per, head = chunk / DU, d0 = 8 * (chunk % DU);
+  if (id >= total) return;
+  int lo = 0, hi = b.S;                          // the last s with q_start[s] <= t
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (b.q_start[mid] <= t)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const long long first = b.q_start[lo], last = b.q_start[lo + 1];
+  Place at;
+  if (!(t >= first && t < last && append_place(c, b, lo, (long long)b.kv_len[lo] - (last - t), 0x7fffffff, at))) return;
+  const size_t off = kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4);
+  const char *kp = c.k + off, *vp = c.v + off;
+  const int t16 = at.pos & 15;
+  u32x4 kw, vw;
+  if constexpr (E2) {
+    const size_t so = kv_scale_offset<D>(c, at.page, head, at.pos >> 4);
+    const uint32_t byte = (uint8_t)c.k[so + d0 / 32 * 16 + 4 * (t16 & 3) + (t16 >> 2)];
+    const float vs = bf16_bits_to_float(reinterpret_cast<const uint16_t*>(c.v + so)[d0 / 64 * 16 + t16]);
+    kw = e2m1_to_bf16(*reinterpret_cast<const uint32_t*>(kp + d0 / 32 * 256 + t16 * 16 + (d0 / 8 & 3) * 4),
+                      __uint_as_float(byte << 23));
+    const char* codes = vp + d0 / 32 * 256 + (d0 & 15) * 16 + (d0 / 16 & 1) * 8 + t16 / 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        x[e] = e2m1_value(((uint32_t)(uint8_t)codes[16 * (2 * i + e)] >> (4 * (t16 & 1))) & 15u) * vs;
+      vw[i] = bf16_pair(x[0], x[1]);
+    }
+  } else if constexpr (E4) {
+    const u32x2 k = *reinterpret_cast<const u32x2*>(kp + d0 / 16 * 256 + t16 * 16 + (d0 & 8));
+    const u32x4 kb = e4m3_to_bf16(k[0], k[1]);
+    uint32_t v[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i / 4] |= (uint32_t)(uint8_t)vp[(d0 + i) * 16 + t16] << (8 * (i & 3));
+    const u32x4 vb = e4m3_to_bf16(v[0], v[1]);
+    const float ks = c.k_scale[head], vs = c.v_scale[head];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kw[i] = bf16_pair(half_of(kb[i], 0) * ks, half_of(kb[i], 1) * ks);
+      vw[i] = bf16_pair(half_of(vb[i], 0) * vs, half_of(vb[i], 1) * vs);
+    }
+  } else {
+    kw = *reinterpret_cast<const u32x4*>(kp + d0 / 8 * 256 + t16 * 16);
+    const uint16_t* v = reinterpret_cast<const uint16_t*>(vp) + (t16 / U) * D * U + d0 * U + t16 % U;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vw[i] = (uint32_t)v[2 * i * U] | ((uint32_t)v[(2 * i + 1) * U] << 16);
+  }
+  if (ko.p) *reinterpret_cast<u32x4*>(ko.p + (size_t)t * ko.stride + 8 * chunk) = kw;
+  if (vo.p) *reinterpret_cast<u32x4*>(vo.p + (size_t)t * vo.stride + 8 * chunk) = vw;
+}
+
+hipError_t launch_kv_read(int D, const BatchArgs& b, const KvArgs& c, RowsOut k, RowsOut v, hipStream_t stream) {
+  const int total = b.T * c.Hkv * (D / 8);       // at most 2^16 2^8 2^4
+  const dim3 grid((total + kAppendThreads - 1) / kAppendThreads);
+  timing_begin(stream, kSiteKvRead);
+  with_kv_kind(c, [&](auto kind) {
+    constexpr int KV = decltype(kind)::value;
+    if (D == 64)
+      hipLaunchKernelGGL((kv_read_kernel<64, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, total);
+    else
+      hipLaunchKernelGGL((kv_read_kernel<128, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, total);
+  });
+  timing_end(stream, kSiteKvRead);
   return hipGetLastError();
 }
 

@@ -310,7 +310,7 @@ def prepare(case, seed):
         need = mc.attn_workspace(T, Hq, Hkv, D)
         if kind == "sparse":
             st["summary"] = mc.KVSummary(st["cache"], bounds=st["bounds"], scale=st["bound_scale"])
-            need = max(need, mc.attn_select_workspace(T, Hq, Hkv, max(used)))
+            need = max(need, mc.attn_select_workspace(T, Hkv, max(used)))
         st["ws"] = torch.empty(need, dtype=torch.uint8, device=dev)
     return st
 
