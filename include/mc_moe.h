@@ -20,6 +20,11 @@
  *   mc_kv_append, mc_attn_decode, mc_attn_prefill
  *                      the blocks' attention over a paged key-value cache
  *   mc_attn_importance the protected set without an attention map
+ *   mc_kv_reserve, mc_kv_release
+ *                      a batch's row starts, lengths and page tables on the GPU
+ *   mc_kv_summarize, mc_attn_select, mc_attn_sparse
+ *                      attention over the pages that bounds select for each query
+ *   mc_kv_read         the keys and values that a cache stands for
  *   mc_odp_threshold, mc_pmq_significance, mc_pmq_allocate
  *                      host helpers: the pruning threshold, expert
  *                      significance and the Eq. 4 width allocation
@@ -395,6 +400,19 @@ mc_status mc_pmq_expert_error(const float *w_gate, const float *w_up, const floa
  * transposes anything it reads.  e4m3 is the OCP format (no infinities, NaN =
  * 0x7f and 0xff); the value of a code is code * scale[h].
  *
+ * e2m1 (the levels 0, 1/2, 1, 3/2, 2, 3, 4 and 6 and a sign, two codes a byte, the first in its low
+ * half) has its scales beside it: the codes of the page first, 8 D bytes a block, then D/2 bytes of
+ * scales a block.  With B = h*page/16 + t/16 and Z = Hkv*page*D/2, in bytes of a page:
+ *   k code   B*8*D + (i/32)*256 + (t%16)*16 + (i%32)/2, half i%2
+ *   k scale  Z + B*D/2 + (i/32)*16 + 4*(t%4) + t%16/4: one byte, 2^(byte - 127), 255: NaN
+ *   v code   B*8*D + (i/32)*256 + (i%16)*16 + 8*(i/16%2) + (t%16)/2, half t%2
+ *   v scale  Z + B*D/2 + (i/64)*32 + 2*(t%16): bf16
+ * so that 32 dimensions of a key and 64 of a value share a scale.  mc_kv_append takes of keys the
+ * least power 2^e with max|y| <= 7 * 2^e, of values max|v| / 6 (in fp32, times the number
+ * nearest to 1/6) rounded to 6 significant bits, and the nearest level (ties to the even code); every value is then a bf16 number.  Groups
+ * whose largest magnitude is below 2^-100 are 0; those with a NaN, an infinity or more than
+ * 7 * 2^125 are NaN.
+ *
  * Batch.  S sequences; sequence s has kv_len[s] tokens in the cache, the last
  * q_start[s+1] - q_start[s] of them new in this call; the new tokens' rows
  * q_start[s] .. q_start[s+1]-1 of q, k, v and the outputs hold them in order,
@@ -408,13 +426,14 @@ mc_status mc_pmq_expert_error(const float *w_gate, const float *w_up, const floa
  * an access outside a buffer. */
 #define MC_KV_BF16 0
 #define MC_KV_E4M3 1
+#define MC_KV_E2M1 4
 
 typedef struct mc_kv_cache {
   int n_pages;             /* pages in k and in v */
   int page;                /* tokens a page: 16, 32, 64, 128 or 256 */
   int Hkv;                 /* key-value heads, 1 .. 256 */
   int D;                   /* head size, 64 or 128 (other values: MC_EUNSUPPORTED) */
-  int dtype;               /* MC_KV_BF16 or MC_KV_E4M3 */
+  int dtype;               /* MC_KV_BF16, MC_KV_E4M3 or MC_KV_E2M1 */
   void *k, *v;             /* device, 16-byte aligned */
   size_t page_stride;      /* bytes between pages, a multiple of 16; mc_kv_page_bytes
                               or more (layers may share an allocation) */
@@ -464,7 +483,9 @@ typedef struct mc_qk_prep {
  * A token is skipped, its q_out row and its place in the cache left as they
  * were, where its position is negative, not below kv_len or max_pages*page or
  * (with rot) n_pos, or its page outside [0, n_pages).  Two rows must not share a
- * place of the cache.  Limits: 1 <= Hq, Hkv <= 256; T and S at most MC_MAX_TOKENS.
+ * place of the cache, nor, of an e2m1 cache, two sequences a block of 16 tokens that one of them
+ * appends to (a byte holds two tokens).  Keys of an e2m1 cache are formed in 64 bits, so that their codes are
+ * those of the exact values wherever these lie further than some 2^-48 from a border.  Limits: 1 <= Hq, Hkv <= 256; T and S at most MC_MAX_TOKENS.
  * Errors: MC_EINVAL (shape, stride, NULL or misaligned pointer), MC_ENOSPACE
  * (cache arrays too short), MC_EUNSUPPORTED, MC_EHIP. */
 mc_status mc_kv_append(const uint16_t *q, size_t q_stride, const uint16_t *k, size_t k_stride,
@@ -523,6 +544,101 @@ mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch 
                           const mc_attention *a, uint16_t *o, size_t o_stride, float *lse, void *workspace,
                           size_t ws_bytes, void *stream);
 
+/* Keys and values of the batch's new tokens as the cache stands for them, as bf16 rows [T][Hkv*D]
+ * with the given elements between them (multiples of 8); k or v may be NULL.  bf16 and e2m1 values
+ * come exactly, e4m3's code * scale[h] is rounded once.  Rows of tokens that mc_kv_append would skip (but
+ * for n_pos) and padding rows are left as they were.  Errors as mc_kv_append. */
+mc_status mc_kv_read(const mc_kv_batch* b, const mc_kv_cache* c, uint16_t* k, size_t k_stride, uint16_t* v,
+                     size_t v_stride, void* stream);
+
+/* Tables of a batch from the requests' lengths, on the GPU: a loop of steps (reserve, append, attend,
+ * release) needs no word from the host and can be captured into a graph.  Free pages are a stack:
+ * free_list[0 .. n_free - 1], the top last. */
+typedef struct mc_kv_pool {
+  int n_pages;               /* entries of free_list */
+  int page;                  /* tokens a page: 16, 32, 64, 128 or 256 */
+  int32_t *free_list;        /* device [n_pages] */
+  const int32_t *n_free;     /* device [1]: the stack's height (taken within 0 .. n_pages) */
+  int32_t *n_free_out;       /* device [1]: its height after the call; may be n_free */
+} mc_kv_pool;
+
+typedef struct mc_kv_tables {
+  int S, T, max_pages;       /* as in mc_kv_batch, whose arrays these are; T: rows of the batch's buffers */
+  int32_t *q_start;          /* device [S+1], written by mc_kv_reserve */
+  int32_t *kv_len;           /* device [S], written */
+  int32_t *page_table;       /* device [S][max_pages], entries of new pages written */
+  int32_t *positions;        /* device [T] or NULL: position of each row, -1 for padding */
+  int64_t *slots;            /* device [T] or NULL: page * (tokens a page) + token of the page, or -1 */
+} mc_kv_tables;
+
+mc_status mc_kv_tables_workspace(int S, size_t *bytes);
+
+/* Makes room for want[s] more tokens of each request s, which has past[s] in the cache on pages
+ * page_table[s][0 .. ceil(past[s] / page) - 1]:
+ *   need[s] = ceil((past[s] + want[s]) / page) - ceil(past[s] / page)
+ * A request whose lengths are negative or exceed its table row (past + want > max_pages*page) asks for
+ * nothing.  With P and R the sums of need and want over the requests up to and with s, request s is granted
+ * its tokens where R[s] <= T and (need[s] = 0 or P[s] <= n_free); the others get none this time, so that a short
+ * pool stops no request that needs no page.  q_start: the sums of granted tokens; kv_len[s] = past[s]
+ * + granted; new page i of s is free_list[n_free - 1 - (P[s] - need[s]) - i], and n_free_out what is left.
+ * past may be kv_len itself (each call is then a step of a loop).  Entries of free_list are not checked.
+ * Limits: S and T at most MC_MAX_TOKENS, max_pages*page at most 2^30.  The workspace (4-byte aligned)
+ * holds nothing between calls.  Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
+mc_status mc_kv_reserve(const int32_t *want, const int32_t *past, const mc_kv_pool *pool, const mc_kv_tables *t,
+                        void *workspace, size_t ws_bytes, void *stream);
+
+/* Requests with done[s] != 0 end: their pages page_table[s][0 .. ceil(past[s] / page) - 1] are pushed in the
+ * order of s and of the table, kv_len[s] = 0; kv_len[s] = past[s] for the others (past may be kv_len).  What
+ * would not fit free_list is dropped.  T, q_start, positions and slots are ignored.  A page that two
+ * requests share is pushed by each.  Limits and errors as mc_kv_reserve. */
+mc_status mc_kv_release(const uint8_t *done, const int32_t *past, const mc_kv_pool *pool, const mc_kv_tables *t,
+                        void *workspace, size_t ws_bytes, void *stream);
+
+/* Attention over some of the pages.  Rows of the calls below are those of a ragged batch, or, where
+ * b->q_start is NULL, the last token of each sequence (T is then ignored, and S is the rows).
+ *
+ * Bounds on the keys of a page, for each key-value head (of e4m3, of the codes):
+ *   s = max|k| * fp32(1/127),  hi_i = ceil(max_t k_i / s),  lo_i = floor(min_t k_i / s)   in fp32, within +-127
+ * over the page's tokens below kv_len, NaN and infinities aside (a page without any number: 0). */
+typedef struct mc_kv_summary {
+  int8_t *bounds;            /* device [n_pages][Hkv][2][D]: lo, hi; 16-byte aligned */
+  float *scale;              /* device [n_pages][Hkv]: s */
+  size_t bounds_bytes, scale_bytes;
+} mc_kv_summary;
+
+/* Renews the bounds of the pages that the batch's new tokens lie on (pages outside [0, n_pages) are left out).
+ * To be called after mc_kv_append, with its batch.  Limits: (T/page + 2 S)*Hkv below 2^24.
+ * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
+mc_status mc_kv_summarize(const mc_kv_batch *b, const mc_kv_cache *c, const mc_kv_summary *m, void *stream);
+
+/* Selects pages for each row and key-value head.  With q8_i = rint(q_i / sq) and sq = max|q| * fp32(1/127)
+ * for each query head (fp32; NaN and infinities of q count as 0; a negative a->scale turns q's signs), a page's
+ * score is
+ *   max over the group's heads of (sq * s) * sum_i q8_i * (q8_i > 0 ? hi_i : lo_i),
+ * the sum of whole numbers being exact.  Of the pages 0 .. pos / page that a row at position pos sees (with a window,
+ * those from (pos - window + 1) / page on) the first keep_first of the sequence, the last keep_last and then those
+ * with the largest scores are taken, up to n_sel, equal scores by the lower page.  sel [rows][Hkv][n_sel]:
+ * their places in the sequence (columns of page_table), ascending, -1 behind them; count [rows][Hkv].
+ * Padding rows are left as they were.  a->prefix and a->slopes must be NULL; the cap does not change the
+ * order.  1 <= keep_last, keep_first + keep_last <= n_sel <= MC_MAX_SELECT.
+ * Limits: rows*Hkv, and the rows' heads over 16 times Hkv times max_pages over 256, below 2^24.
+ * Workspace: mc_attn_select_workspace (at most some 256 MB, or one row's scores where they are more).
+ * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
+#define MC_MAX_SELECT 4096
+mc_status mc_attn_select_workspace(int T, int Hkv, int max_pages, size_t *bytes);
+mc_status mc_attn_select(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
+                         const mc_kv_summary *m, const mc_attention *a, int n_sel, int keep_first, int keep_last,
+                         int32_t *sel, int32_t *count, void *workspace, size_t ws_bytes, void *stream);
+
+/* Attention of each row to the visible keys of the pages sel[row][head][0 .. count[row][head] - 1]
+ * (columns of its sequence's page_table row; others than 0 .. max_pages - 1 hold no key, and a page listed
+ * twice counts twice).  Everything else as mc_attn_decode: a row that sees no key gets o = 0 and lse =
+ * -infinity.  a->prefix must be NULL.  Workspace: mc_attn_workspace of the rows.  Limits: rows*Hkv*ceil(g/16)
+ * below 2^24, n_sel at most MC_MAX_SELECT. */
+mc_status mc_attn_sparse(const uint16_t *q, size_t q_stride, const mc_kv_batch *b, const mc_kv_cache *c,
+                         const mc_attention *a, const int32_t *sel, const int32_t *count, int n_sel, uint16_t *o,
+                         size_t o_stride, float *lse, void *workspace, size_t ws_bytes, void *stream);
+
 /* mc_token_importance without an attention map: the probabilities of Eq. 6 are
  * recomputed as exp(s - lse) from the prompt's queries, its cached keys and the
  * lse that mc_attn_prefill returned:
@@ -555,7 +671,8 @@ mc_status mc_attn_importance(const uint16_t *q, size_t q_stride, const float *ls
  * route_lists, prefill_prep, gateup, down, combine, importance_colsum,
  * importance_finish, importance_select, rmsnorm, router, gptq_hessian,
  * gptq_factor, gptq_quantize (each a whole call), kv_append, attn_decode,
- * attn_prefill, attn_join, attn_colsum, attn_finish.
+ * attn_prefill, attn_join, attn_colsum, attn_finish, kv_tables, kv_read, kv_summary, attn_select (scores and
+ * selection), attn_sparse.
  * Errors: MC_EINVAL (unknown name, NULL pointer), MC_EHIP. */
 mc_status mc_timing_enable(int on);
 mc_status mc_timing_read(const char *kernel, double *total_ms, int *launches);

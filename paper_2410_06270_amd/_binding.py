@@ -66,6 +66,22 @@ class _Attention(ctypes.Structure):
                 ("window", ctypes.c_int), ("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p)]
 
 
+class _KVPool(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("free_list", ctypes.c_void_p),
+                ("n_free", ctypes.c_void_p), ("n_free_out", ctypes.c_void_p)]
+
+
+class _KVTables(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int), ("T", ctypes.c_int), ("max_pages", ctypes.c_int), ("q_start", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p)]
+
+
+class _KVSummary(ctypes.Structure):
+    _fields_ = [("bounds", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("bounds_bytes", ctypes.c_size_t),
+                ("scale_bytes", ctypes.c_size_t)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -148,6 +164,22 @@ def load():
         lib.mc_attn_importance_workspace.argtypes = [I, I, ctypes.POINTER(S)]
         lib.mc_attn_importance.restype = st
         lib.mc_attn_importance.argtypes = [P, S, P, KB, KC, AT, P, I, ctypes.c_float, P, P, P, S, P]
+        KP, KT, KS = (ctypes.POINTER(t) for t in (_KVPool, _KVTables, _KVSummary))
+        lib.mc_kv_read.restype = st
+        lib.mc_kv_read.argtypes = [KB, KC, P, S, P, S, P]
+        lib.mc_kv_tables_workspace.restype = st
+        lib.mc_kv_tables_workspace.argtypes = [I, ctypes.POINTER(S)]
+        for f in (lib.mc_kv_reserve, lib.mc_kv_release):
+            f.restype = st
+            f.argtypes = [P, P, KP, KT, P, S, P]
+        lib.mc_kv_summarize.restype = st
+        lib.mc_kv_summarize.argtypes = [KB, KC, KS, P]
+        lib.mc_attn_select_workspace.restype = st
+        lib.mc_attn_select_workspace.argtypes = [I, I, I, ctypes.POINTER(S)]
+        lib.mc_attn_select.restype = st
+        lib.mc_attn_select.argtypes = [P, S, KB, KC, KS, AT, I, I, I, P, P, P, S, P]
+        lib.mc_attn_sparse.restype = st
+        lib.mc_attn_sparse.argtypes = [P, S, KB, KC, AT, P, P, I, P, S, P, P, S, P]
         lib.mc_timing_enable.restype = st
         lib.mc_timing_enable.argtypes = [I]
         lib.mc_timing_read.restype = st
@@ -435,9 +467,12 @@ def kv_page_bytes(page: int, Hkv: int, D: int, dtype=torch.bfloat16) -> int:
     return b.value
 
 
+_KV_DTYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float4_e2m1fn_x2: 4}
+
+
 def _kv_dtype(dtype) -> int:
-    assert dtype in (torch.bfloat16, torch.float8_e4m3fn), "a cache holds bfloat16 or float8_e4m3fn"
-    return 1 if dtype == torch.float8_e4m3fn else 0
+    assert dtype in _KV_DTYPES, "a cache holds bfloat16, float8_e4m3fn or float4_e2m1fn_x2"
+    return _KV_DTYPES[dtype]
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -487,7 +522,8 @@ class KVCache:
     """Device buffers + descriptor of a paged cache (torch-allocated, or the
     given k and v: [n_pages][..] with contiguous pages, which may be slices of
     an allocation that layers share).  k_scale, v_scale: float32 [Hkv], for
-    float8_e4m3fn caches."""
+    float8_e4m3fn caches.  float4_e2m1fn_x2 caches are uint8 arrays (a page holds
+    codes and their scales)."""
 
     def __init__(self, n_pages: int, page: int, Hkv: int, D: int, dtype=torch.bfloat16, k=None, v=None,
                  k_scale=None, v_scale=None, device=None):
@@ -495,16 +531,17 @@ class KVCache:
         per = kv_page_bytes(page, Hkv, D, dtype)
         e = 1 if kind else 2
         device = device or torch.device("cuda")
+        held = torch.uint8 if kind == 4 else dtype
         if k is None:
-            k = torch.zeros((n_pages, per // e), dtype=dtype, device=device)
+            k = torch.zeros((n_pages, per // e), dtype=held, device=device)
         if v is None:
-            v = torch.zeros((n_pages, per // e), dtype=dtype, device=device)
+            v = torch.zeros((n_pages, per // e), dtype=held, device=device)
         for t in (k, v):
-            assert t.dtype in ((torch.float8_e4m3fn, torch.uint8) if kind else _BF16) and t.shape[0] == n_pages
+            assert t.dtype in ((held, torch.uint8) if kind else _BF16) and t.shape[0] == n_pages
             assert t.numel() * e == n_pages * per and t[0].is_contiguous()
         stride = k.stride(0) * e if n_pages > 1 else per
         assert n_pages == 1 or v.stride(0) * e == stride, "k and v differ in their page stride"
-        if kind:
+        if kind == 1:
             for t in (k_scale, v_scale):
                 assert t is not None and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == Hkv
         self.n_pages, self.page, self.Hkv, self.D, self.dtype = n_pages, page, Hkv, D, dtype
@@ -628,6 +665,137 @@ def attn_prefill(q, batch: KVBatch, cache: KVCache, attn: Attention, o, workspac
     """q, o [T][Hq*D] bf16 (rows may be slices of wider ones); lse [T][Hq] float32."""
     assert batch.q_start is not None
     _attn(load().mc_attn_prefill, batch.T, q, batch, cache, attn, o, workspace, lse, stream)
+
+
+def kv_read(batch: KVBatch, cache: KVCache, k=None, v=None, stream=None):
+    """The batch's new tokens as the cache stands for them: k, v [T][Hkv*D] bf16 (rows may be
+    slices of wider ones), either may be None."""
+    dev = _here(k, v)
+    _here_too(dev, cache, batch)
+    assert batch.q_start is not None
+    width = cache.Hkv * cache.D
+    kp, ks = (None, 0) if k is None else _row_matrix(k, batch.T, width)
+    vp, vs = (None, 0) if v is None else _row_matrix(v, batch.T, width)
+    _check(load().mc_kv_read(batch.ref, cache.ref, kp, ks, vp, vs, _stream_on(dev, stream)))
+
+
+class KVPool:
+    """Free pages of a cache: free_list int32 [n_pages] of which the first n_free (int32 [1]) are
+    free, the top last.  n_free_out: where a call leaves the new height (n_free itself if None)."""
+
+    def __init__(self, page: int, free_list, n_free, n_free_out=None):
+        n_free_out = n_free if n_free_out is None else n_free_out
+        for t in (free_list, n_free, n_free_out):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        assert n_free.numel() == 1 and n_free_out.numel() == 1
+        self.page, self.free_list, self.n_free, self.n_free_out = page, free_list, n_free, n_free_out
+        self.dev = _device_of(free_list, n_free, n_free_out)
+        self.desc = _KVPool(free_list.numel(), page, free_list.data_ptr(), n_free.data_ptr(), n_free_out.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+
+def kv_tables_workspace(S: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load().mc_kv_tables_workspace(S, ctypes.byref(b)))
+    return b.value
+
+
+def _tables(batch: KVBatch, positions=None, slots=None):
+    return ctypes.byref(_KVTables(batch.S, batch.T, batch.max_pages,
+                                  None if batch.q_start is None else batch.q_start.data_ptr(), batch.kv_len.data_ptr(),
+                                  batch.page_table.data_ptr(), None if positions is None else positions.data_ptr(),
+                                  None if slots is None else slots.data_ptr()))
+
+
+def kv_reserve(want, past, pool: KVPool, batch: KVBatch, workspace, positions=None, slots=None, stream=None):
+    """want, past: int32 [S] (past may be batch.kv_len).  Writes the batch's q_start, kv_len and new
+    page table entries, and, if given, positions (int32 [T]) and slots (int64 [T])."""
+    dev = _here(want, past, workspace, positions, slots)
+    _here_too(dev, pool, batch)
+    assert batch.q_start is not None
+    for t in (want, past):
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == batch.S
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous()
+                                 and positions.numel() == batch.T)
+    assert slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == batch.T)
+    _check(load().mc_kv_reserve(want.data_ptr(), past.data_ptr(), pool.ref, _tables(batch, positions, slots),
+                                workspace.data_ptr(), workspace.nbytes, _stream_on(dev, stream)))
+
+
+def kv_release(done, past, pool: KVPool, batch: KVBatch, workspace, stream=None):
+    """done: uint8 [S], past: int32 [S] (may be batch.kv_len).  Pushes the pages of requests that are
+    done, and writes the batch's kv_len."""
+    dev = _here(done, past, workspace)
+    _here_too(dev, pool, batch)
+    assert done.dtype == torch.uint8 and done.is_contiguous() and done.numel() == batch.S
+    assert past.dtype == torch.int32 and past.is_contiguous() and past.numel() == batch.S
+    _check(load().mc_kv_release(done.data_ptr(), past.data_ptr(), pool.ref, _tables(batch), workspace.data_ptr(),
+                                workspace.nbytes, _stream_on(dev, stream)))
+
+
+class KVSummary:
+    """Bounds on the keys of a cache's pages: bounds int8 [n_pages][Hkv][2][D], scale float32
+    [n_pages][Hkv] (torch-allocated, or given)."""
+
+    def __init__(self, cache: KVCache, bounds=None, scale=None):
+        if bounds is None:
+            bounds = torch.zeros((cache.n_pages, cache.Hkv, 2, cache.D), dtype=torch.int8, device=cache.k.device)
+        if scale is None:
+            scale = torch.zeros((cache.n_pages, cache.Hkv), dtype=torch.float32, device=cache.k.device)
+        assert bounds.dtype == torch.int8 and bounds.is_contiguous() and scale.dtype == torch.float32
+        assert scale.is_contiguous()
+        self.bounds, self.scale = bounds, scale
+        self.dev = _device_of(bounds, scale)
+        self.desc = _KVSummary(bounds.data_ptr(), scale.data_ptr(), bounds.nbytes, scale.nbytes)
+        self.ref = ctypes.byref(self.desc)
+
+
+def kv_summarize(batch: KVBatch, cache: KVCache, summary: KVSummary, stream=None):
+    """Renews the bounds of the pages that the batch's new tokens lie on (without q_start: the last
+    token of each sequence)."""
+    dev = _here(batch.kv_len)
+    _here_too(dev, cache, batch, summary)
+    _check(load().mc_kv_summarize(batch.ref, cache.ref, summary.ref, _stream_on(dev, stream)))
+
+
+def attn_select_workspace(T: int, Hkv: int, max_pages: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load().mc_attn_select_workspace(T, Hkv, max_pages, ctypes.byref(b)))
+    return b.value
+
+
+def _selection(sel, count, rows: int, Hkv: int) -> int:
+    assert sel.dtype == torch.int32 and sel.is_contiguous() and sel.dim() == 3 and sel.shape[:2] == (rows, Hkv)
+    assert count.dtype == torch.int32 and count.is_contiguous() and count.numel() == rows * Hkv
+    return sel.shape[2]
+
+
+def attn_select(q, batch: KVBatch, cache: KVCache, summary: KVSummary, attn: Attention, sel, count, workspace,
+                keep_first: int = 1, keep_last: int = 1, stream=None):
+    """q [rows][Hq*D] bf16; writes the selected pages sel (int32 [rows][Hkv][n_sel], places in the
+    sequence) and their number count (int32 [rows][Hkv]).  Rows: the batch's, T or, without q_start, S."""
+    dev = _here(q, sel, count, workspace)
+    _here_too(dev, cache, batch, summary, attn)
+    n_sel = _selection(sel, count, batch.T, cache.Hkv)
+    qp, qs = _row_matrix(q, batch.T, attn.Hq * cache.D)
+    _check(load().mc_attn_select(qp, qs, batch.ref, cache.ref, summary.ref, attn.ref, n_sel, _bounded(keep_first),
+                                 _bounded(keep_last), sel.data_ptr(), count.data_ptr(), workspace.data_ptr(),
+                                 workspace.nbytes, _stream_on(dev, stream)))
+
+
+def attn_sparse(q, batch: KVBatch, cache: KVCache, attn: Attention, sel, count, o, workspace, lse=None, stream=None):
+    """Attention to the pages sel[row][head][:count]: q, o [rows][Hq*D] bf16 (rows may be slices of
+    wider ones), lse [rows][Hq] float32.  Rows as for attn_select."""
+    dev = _here(q, sel, count, o, lse, workspace)
+    _here_too(dev, cache, batch, attn)
+    rows, width = batch.T, attn.Hq * cache.D
+    n_sel = _selection(sel, count, rows, cache.Hkv)
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * attn.Hq)
+    qp, qs = _row_matrix(q, rows, width)
+    op, os_ = _row_matrix(o, rows, width)
+    _check(load().mc_attn_sparse(qp, qs, batch.ref, cache.ref, attn.ref, sel.data_ptr(), count.data_ptr(), n_sel, op,
+                                 os_, None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                 _stream_on(dev, stream)))
 
 
 def attn_importance_workspace(Hq: int, L: int) -> int:

@@ -727,12 +727,14 @@ mc_status check_kv_shape(int page, int Hkv, int D, int dtype) {
   if (Hkv < 1 || Hkv > 256) return fail(MC_EINVAL, "Hkv=%d outside [1, 256]", Hkv);
   if (D != 64 && D != 128)
     return fail(D > 0 && D % 16 == 0 ? MC_EUNSUPPORTED : MC_EINVAL, "head size %d: this build supports 64 and 128", D);
-  if (dtype != MC_KV_BF16 && dtype != MC_KV_E4M3) return fail(MC_EINVAL, "cache dtype %d", dtype);
+  if (dtype != MC_KV_BF16 && dtype != MC_KV_E4M3 && dtype != MC_KV_E2M1) return fail(MC_EINVAL, "cache dtype %d", dtype);
   return MC_OK;
 }
 
 size_t kv_page_bytes(int page, int Hkv, int D, int dtype) {
-  return (size_t)page * Hkv * D * (dtype == MC_KV_E4M3 ? 1 : 2);
+  // e2m1: half a byte an element, and D / 32 bytes of scales a token and head
+  const size_t n = (size_t)page * Hkv * D;
+  return dtype == MC_KV_E2M1 ? n / 2 + n / 32 : n * (dtype == MC_KV_E4M3 ? 1 : 2);
 }
 
 mc_status check_cache(const mc_kv_cache* c) {
@@ -801,7 +803,7 @@ mc::KvArgs kv_args(const mc_kv_cache* c) {
   int lb = 0;
   while ((16 << lb) < c->page) ++lb;
   return {static_cast<char*>(c->k), static_cast<char*>(c->v), c->page_stride, c->n_pages, c->Hkv, lb,
-          c->k_scale, c->v_scale};
+          c->k_scale, c->v_scale, c->dtype};
 }
 
 mc::BatchArgs batch_args(const mc_kv_batch* b) {
@@ -919,6 +921,183 @@ mc_status mc_attn_prefill(const uint16_t* q, size_t q_stride, const mc_kv_batch*
                                             {o, o_stride}, lse, longest(b, c), workspace,
                                             static_cast<hipStream_t>(stream)),
                     "mc_attn_prefill launch");
+}
+
+// ------------------------------------------------- reading a cache back --
+mc_status mc_kv_read(const mc_kv_batch* b, const mc_kv_cache* c, uint16_t* k, size_t k_stride, uint16_t* v,
+                     size_t v_stride, void* stream) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_batch(b, c, true);
+  if (s != MC_OK) return s;
+  if (!k && !v) return fail(MC_EINVAL, "k and v are both NULL");
+  if (k) s = check_rows("k", k, k_stride, (size_t)c->Hkv * c->D);
+  if (s == MC_OK && v) s = check_rows("v", v, v_stride, (size_t)c->Hkv * c->D);
+  if (s != MC_OK) return s;
+  (void)hipGetLastError();
+  return hip_status(mc::launch_kv_read(c->D, batch_args(b), kv_args(c), {k, k_stride}, {v, v_stride},
+                                       static_cast<hipStream_t>(stream)),
+                    "mc_kv_read launch");
+}
+
+// ------------------------------------------------------ tables of a batch --
+mc_status mc_kv_tables_workspace(int S, size_t* bytes) {
+  if (!bytes) return fail(MC_EINVAL, "bytes is NULL");
+  if (S < 1) return fail(MC_EINVAL, "S=%d must be >= 1", S);
+  if (S > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "S=%d above %d", S, MC_MAX_TOKENS);
+  *bytes = mc::kv_tables_bytes(S);
+  return MC_OK;
+}
+
+static mc_status check_pool(const mc_kv_pool* p, const mc_kv_tables* t, const int32_t* past, const void* ws,
+                            size_t ws_bytes) {
+  if (!p || !t) return fail(MC_EINVAL, "pool or tables descriptor is NULL");
+  if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1)))
+    return fail(MC_EINVAL, "page=%d: 16, 32, 64, 128 or 256 tokens", p->page);
+  if (p->n_pages < 1) return fail(MC_EINVAL, "n_pages=%d must be >= 1", p->n_pages);
+  if (!p->free_list || !p->n_free || !p->n_free_out) return fail(MC_EINVAL, "free_list, n_free or n_free_out is NULL");
+  if (t->S < 1) return fail(MC_EINVAL, "S=%d must be >= 1", t->S);
+  if (t->S > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "S=%d above %d", t->S, MC_MAX_TOKENS);
+  if (t->max_pages < 1) return fail(MC_EINVAL, "max_pages=%d must be >= 1", t->max_pages);
+  if ((long long)t->max_pages * p->page > kMaxPositions)
+    return fail(MC_EUNSUPPORTED, "max_pages=%d of %d tokens: above 2^30 positions", t->max_pages, p->page);
+  if (!t->kv_len || !t->page_table || !past) return fail(MC_EINVAL, "past, kv_len or page_table is NULL");
+  if (!ws || misaligned(ws, 4)) return fail(MC_EINVAL, "workspace is NULL or not 4-byte aligned");
+  if (ws_bytes < mc::kv_tables_bytes(t->S))
+    return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, mc::kv_tables_bytes(t->S));
+  return MC_OK;
+}
+
+static mc::PoolArgs pool_args(const mc_kv_pool* p) {
+  int log = 4;
+  while ((1 << log) < p->page) ++log;
+  return {p->free_list, p->n_free, p->n_free_out, p->n_pages, log};
+}
+
+mc_status mc_kv_reserve(const int32_t* want, const int32_t* past, const mc_kv_pool* pool, const mc_kv_tables* t,
+                        void* workspace, size_t ws_bytes, void* stream) {
+  mc_status s = check_pool(pool, t, past, workspace, ws_bytes);
+  if (s != MC_OK) return s;
+  if (!want || !t->q_start) return fail(MC_EINVAL, "want or q_start is NULL");
+  if (t->T < 1) return fail(MC_EINVAL, "T=%d must be >= 1", t->T);
+  if (t->T > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "T=%d above %d", t->T, MC_MAX_TOKENS);
+  if (misaligned(t->slots, 8)) return fail(MC_EINVAL, "slots is not 8-byte aligned");
+  (void)hipGetLastError();
+  return hip_status(mc::launch_kv_reserve(want, past, pool_args(pool),
+                                          {t->q_start, t->kv_len, t->page_table, t->S, t->T, t->max_pages},
+                                          t->positions, t->slots, workspace, static_cast<hipStream_t>(stream)),
+                    "mc_kv_reserve launch");
+}
+
+mc_status mc_kv_release(const uint8_t* done, const int32_t* past, const mc_kv_pool* pool, const mc_kv_tables* t,
+                        void* workspace, size_t ws_bytes, void* stream) {
+  mc_status s = check_pool(pool, t, past, workspace, ws_bytes);
+  if (s != MC_OK) return s;
+  if (!done) return fail(MC_EINVAL, "done is NULL");
+  (void)hipGetLastError();
+  return hip_status(mc::launch_kv_release(done, past, pool_args(pool),
+                                          {nullptr, t->kv_len, t->page_table, t->S, 0, t->max_pages}, workspace,
+                                          static_cast<hipStream_t>(stream)),
+                    "mc_kv_release launch");
+}
+
+// ------------------------------------------------ attention over some pages --
+// A batch of ragged rows, or (q_start NULL) of one row a sequence.
+static mc_status check_rows_batch(const mc_kv_batch* b, const mc_kv_cache* c) {
+  return check_batch(b, c, b && b->q_start);
+}
+
+static mc_status check_summary(const mc_kv_summary* m, const mc_kv_cache* c) {
+  if (!m) return fail(MC_EINVAL, "summary descriptor is NULL");
+  if (!m->bounds || !m->scale || misaligned(m->bounds) || misaligned(m->scale, 4))
+    return fail(MC_EINVAL, "bounds or scale is NULL or not aligned (16 and 4 bytes)");
+  const size_t heads = (size_t)c->n_pages * c->Hkv;
+  if (m->bounds_bytes < heads * 2 * c->D || m->scale_bytes < heads * sizeof(float))
+    return fail(MC_ENOSPACE, "summary arrays hold %zu/%zu bytes, need %zu/%zu", m->bounds_bytes, m->scale_bytes,
+                heads * 2 * c->D, heads * sizeof(float));
+  return MC_OK;
+}
+
+mc_status mc_kv_summarize(const mc_kv_batch* b, const mc_kv_cache* c, const mc_kv_summary* m, void* stream) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_rows_batch(b, c);
+  if (s == MC_OK) s = check_summary(m, c);
+  if (s != MC_OK) return s;
+  // a launch holds less than 2^32 threads
+  if ((long long)((b->q_start ? b->T / c->page + b->S : 0) + b->S) * c->Hkv >= 1 << 24)
+    return fail(MC_EUNSUPPORTED, "(T/page + 2 S)*Hkv at or above 2^24");
+  (void)hipGetLastError();
+  return hip_status(mc::launch_kv_summarize(c->D, batch_args(b), kv_args(c), {m->bounds, m->scale},
+                                            static_cast<hipStream_t>(stream)),
+                    "mc_kv_summarize launch");
+}
+
+mc_status mc_attn_select_workspace(int T, int Hkv, int max_pages, size_t* bytes) {
+  if (!bytes) return fail(MC_EINVAL, "bytes is NULL");
+  if (T < 1 || Hkv < 1 || Hkv > 256 || max_pages < 1)
+    return fail(MC_EINVAL, "bad shape T=%d Hkv=%d max_pages=%d", T, Hkv, max_pages);
+  if (T > MC_MAX_TOKENS || max_pages > kMaxPositions / 16)
+    return fail(MC_EUNSUPPORTED, "T=%d above %d or max_pages=%d above 2^26", T, MC_MAX_TOKENS, max_pages);
+  *bytes = mc::attn_select_bytes(T, Hkv, max_pages);
+  return MC_OK;
+}
+
+static mc_status check_list(const int32_t* sel, const int32_t* count, int n_sel) {
+  if (!sel || !count) return fail(MC_EINVAL, "sel or count is NULL");
+  if (n_sel < 1) return fail(MC_EINVAL, "n_sel=%d must be >= 1", n_sel);
+  if (n_sel > MC_MAX_SELECT) return fail(MC_EUNSUPPORTED, "n_sel=%d above %d", n_sel, MC_MAX_SELECT);
+  return MC_OK;
+}
+
+mc_status mc_attn_select(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
+                         const mc_kv_summary* m, const mc_attention* a, int n_sel, int keep_first, int keep_last,
+                         int32_t* sel, int32_t* count, void* workspace, size_t ws_bytes, void* stream) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_rows_batch(b, c);
+  if (s == MC_OK) s = check_summary(m, c);
+  if (s == MC_OK) s = check_attention(a, c);
+  if (s == MC_OK) s = check_list(sel, count, n_sel);
+  if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
+  if (s != MC_OK) return s;
+  if (a->prefix || a->slopes) return fail(MC_EUNSUPPORTED, "a prefix or slopes: the bounds are of the products alone");
+  if (keep_first < 0 || keep_last < 1 || keep_first > n_sel || keep_last > n_sel - keep_first)
+    return fail(MC_EINVAL, "keep_first=%d, keep_last=%d: >= 0 and >= 1, at most n_sel=%d together", keep_first,
+                keep_last, n_sel);
+  const int rows = b->q_start ? b->T : b->S;
+  if (mc::select_workgroups(batch_args(b), kv_args(c), a->Hq / c->Hkv) >= 1 << 24 ||
+      (long long)rows * c->Hkv >= 1 << 24)
+    return fail(MC_EUNSUPPORTED, "rows*Hkv, or with 256 pages a workgroup the launch, at or above 2^24");
+  if (!workspace || misaligned(workspace, 4)) return fail(MC_EINVAL, "workspace is NULL or not 4-byte aligned");
+  const size_t need = mc::attn_select_bytes(rows, c->Hkv, b->max_pages);
+  if (ws_bytes < need) return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+  const mc::ScoreArgs sa = score_args(a, c);
+  (void)hipGetLastError();
+  return hip_status(mc::launch_attn_select({q, q_stride}, c->D, batch_args(b), kv_args(c), {m->bounds, m->scale},
+                                           {sa.g, a->scale < 0.0f, sa.window, n_sel, keep_first, keep_last, sel, count},
+                                           workspace, static_cast<hipStream_t>(stream)),
+                    "mc_attn_select launch");
+}
+
+mc_status mc_attn_sparse(const uint16_t* q, size_t q_stride, const mc_kv_batch* b, const mc_kv_cache* c,
+                         const mc_attention* a, const int32_t* sel, const int32_t* count, int n_sel, uint16_t* o,
+                         size_t o_stride, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  mc_status s = check_cache(c);
+  if (s == MC_OK) s = check_rows_batch(b, c);
+  if (s == MC_OK) s = check_attention(a, c);
+  if (s == MC_OK) s = check_list(sel, count, n_sel);
+  if (s == MC_OK) s = check_rows("q", q, q_stride, (size_t)a->Hq * c->D);
+  if (s == MC_OK) s = check_rows("o", o, o_stride, (size_t)a->Hq * c->D);
+  if (s != MC_OK) return s;
+  if (a->prefix) return fail(MC_EUNSUPPORTED, "a prefix: listed pages are read causally");
+  const int rows = b->q_start ? b->T : b->S;
+  if ((long long)rows * c->Hkv * ((a->Hq / c->Hkv + 15) / 16) >= 1 << 24)
+    return fail(MC_EUNSUPPORTED, "rows*Hkv*ceil(g/16) at or above 2^24");
+  if (!workspace || misaligned(workspace)) return fail(MC_EINVAL, "workspace is NULL or not 16-byte aligned");
+  const size_t need = mc::attn_workspace_bytes(rows, a->Hq, c->Hkv, c->D);
+  if (ws_bytes < need) return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);
+  (void)hipGetLastError();
+  return hip_status(mc::launch_attn_sparse({q, q_stride}, c->D, batch_args(b), kv_args(c), score_args(a, c), sel, count,
+                                           n_sel, {o, o_stride}, lse, workspace, static_cast<hipStream_t>(stream)),
+                    "mc_attn_sparse launch");
 }
 
 mc_status mc_attn_importance_workspace(int Hq, int L, size_t* bytes) {

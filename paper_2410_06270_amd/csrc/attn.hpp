@@ -66,6 +66,31 @@ struct SplitArgs {
   int nsplit;
 };
 
+// Bounds of the pages' keys: bounds [n_pages][Hkv][2][D] (least, largest) in units of scale
+// [n_pages][Hkv].
+struct SummaryArgs {
+  int8_t* bounds;
+  float* scale;
+};
+
+struct SelectArgs {
+  int g, negative, window;           // negative: a negative scale turns the order
+  int n_sel, first, last;            // pages of a row; the first and last ones that are always taken
+  int32_t *sel, *count;
+};
+
+struct PoolArgs {
+  int32_t* free_list;
+  const int32_t* n_free;
+  int32_t* n_free_out;
+  int n_pages, page_log;
+};
+
+struct BatchOut {
+  int32_t *q_start, *kv_len, *page_table;
+  int S, T, max_pages;
+};
+
 // The longest length the tables describe, and a sequence's length within it.
 __device__ __forceinline__ int kv_length(const KvArgs& c, const BatchArgs& b, int s) {
   const int most = (b.max_pages << c.lb) * kKvBlock, n = b.kv_len[s];      // most: 2^30 or less
@@ -331,10 +356,13 @@ __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float sl
   return MODE & 2 ? __builtin_fmaf(slope2, dist, s) : s;
 }
 
-// Calls f(integral constant of the call's MODE).
+// Calls f(integral constant of the call's MODE).  relative: caps keep the error relative from
+// kCapRelative on (where a row sees few keys, an error of 2^-23 cap shows in its lse).
+constexpr float kCapRelative = 1.0f;
+
 template <class F>
-void with_score_mode(const ScoreArgs& a, F&& f) {
-  if (a.softcap > kCapPlain)
+void with_score_mode(const ScoreArgs& a, bool relative, F&& f) {
+  if (a.softcap > kCapPlain || (relative && a.softcap >= kCapRelative))
     a.slopes ? f(std::integral_constant<int, 7>{}) : f(std::integral_constant<int, 5>{});
   else if (a.softcap > 0.0f)
     a.slopes ? f(std::integral_constant<int, 3>{}) : f(std::integral_constant<int, 1>{});

@@ -577,7 +577,8 @@ static void decode_launch(RowsIn q, int rows, const BatchArgs& b, const KvArgs& 
                           hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)rows * c.Hkv * head_tiles * sp.nsplit));
   with_kv_kind(c, [&](auto kind) {
-    with_score_mode(a, [&](auto mode) {
+    // (bound by memory: the relative form costs nothing; the older kinds keep what they had)
+    with_score_mode(a, SPARSE || decltype(kind)::value == MC_KV_E2M1, [&](auto mode) {
       hipLaunchKernelGGL((attn_decode_kernel<D, decltype(kind)::value, decltype(mode)::value, SPARSE>), grid,
                          dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp, head_tiles, sparse);
     });

@@ -39,7 +39,7 @@ __device__ __forceinline__ bool append_place(const KvArgs& c, const BatchArgs& b
 // ------------------------------------------------------------------ e2m1 --
 // Groups of e2m1 codes share a scale.  Of keys, 32 dimensions: 2^e, e the least with max|y| <=
 // 7 2^e (7 being the border between 6, the largest level, and the next that there would be).  Of
-// values, 64 dimensions: max|v| / 6, rounded to 6 significant bits so that its products with the codes
+// values, 64 dimensions: max|v| times the fp32 number nearest to 1/6, rounded to 6 significant bits so that its products with the codes
 // are bf16 numbers.  Groups below 2^-100 are 0, those with a NaN, an infinity or more than 7 2^125 NaN.
 constexpr double kGroupLeast = 0x1p-100, kGroupMost = 0x1.cp127;
 
@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t key_scale_byte(double m) {
 __device__ __forceinline__ float value_scale(float m) {
   if (!(m <= (float)kGroupMost)) return __uint_as_float(0x7fc00000u);
   if (m < (float)kGroupLeast) return 0.0f;
-  uint32_t u = __float_as_uint(m / 6.0f);               // IEEE division
+  uint32_t u = __float_as_uint(m * (1.0f / 6.0f));
   u += 0x1ffffu + ((u >> 18) & 1u);
   return __uint_as_float(u & ~0x3ffffu);
 }

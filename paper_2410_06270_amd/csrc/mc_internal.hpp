@@ -13,6 +13,7 @@ enum TimingSite {
   kSiteGateUp, kSiteDown, kSiteCombine, kSitePrefillPrep, kSiteImpColsum, kSiteImpFinish, kSiteImpSelect,
   kSiteRmsNorm, kSiteRouter, kSiteGptqHessian, kSiteGptqFactor, kSiteGptqQuantize,
   kSiteKvAppend, kSiteAttnDecode, kSiteAttnPrefill, kSiteAttnJoin, kSiteAttnColsum, kSiteAttnFinish,
+  kSiteKvTables, kSiteKvRead, kSiteKvSummary, kSiteAttnSelect, kSiteAttnSparse,
   kNumSites
 };
 void timing_begin(hipStream_t stream, int site);
@@ -158,6 +159,26 @@ hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs&
                               float* lse, int max_len, void* ws, hipStream_t stream);
 hipError_t launch_attn_prefill(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
                                float* lse, int max_len, void* ws, hipStream_t stream);
+// What the cache holds at the new tokens' places (either pointer may be null).
+hipError_t launch_kv_read(int D, const BatchArgs& b, const KvArgs& c, RowsOut k, RowsOut v, hipStream_t stream);
+// Attention over listed pages; rows are b's (those of a ragged batch, or one a sequence).
+hipError_t launch_attn_sparse(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a,
+                              const int32_t* sel, const int32_t* count, int n_sel, RowsOut o, float* lse, void* ws,
+                              hipStream_t stream);
+struct SummaryArgs;
+struct SelectArgs;
+struct PoolArgs;
+struct BatchOut;
+hipError_t launch_kv_summarize(int D, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm, hipStream_t stream);
+size_t attn_select_bytes(int rows, int Hkv, int max_pages);
+long long select_workgroups(const BatchArgs& b, const KvArgs& c, int g);
+hipError_t launch_attn_select(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm,
+                              const SelectArgs& a, void* ws, hipStream_t stream);
+size_t kv_tables_bytes(int S);
+hipError_t launch_kv_reserve(const int32_t* want, const int32_t* past, const PoolArgs& p, const BatchOut& b,
+                             int32_t* positions, int64_t* slots, void* ws, hipStream_t stream);
+hipError_t launch_kv_release(const uint8_t* done, const int32_t* past, const PoolArgs& p, const BatchOut& b, void* ws,
+                             hipStream_t stream);
 size_t attn_importance_bytes(int Hq, int L);
 hipError_t launch_attn_importance(RowsIn q, const float* lse, int D, const BatchArgs& b, const KvArgs& c,
                                   const ScoreArgs& a, const uint16_t* x, int d, float rho, float* importance,

@@ -15,7 +15,8 @@ const char* const kSiteNames[kNumSites] = {
     "pack_scale_zero", "pack_codes", "export", "route_fused", "route_select",
     "route_lists",     "gateup",     "down",   "combine", "prefill_prep",
     "importance_colsum", "importance_finish", "importance_select", "rmsnorm", "router", "gptq_hessian", "gptq_factor", "gptq_quantize",
-    "kv_append", "attn_decode", "attn_prefill", "attn_join", "attn_colsum", "attn_finish"};
+    "kv_append", "attn_decode", "attn_prefill", "attn_join", "attn_colsum", "attn_finish",
+    "kv_tables", "kv_read", "kv_summary", "attn_select", "attn_sparse"};
 
 struct Pair {
   hipEvent_t start, stop;
