@@ -240,6 +240,24 @@ __device__ __forceinline__ u32x4 e2m1_to_bf16(uint32_t w, float scale) {
   return r;
 }
 
+// Eight e2m1 codes of a dimension's neighbouring tokens times their scales (bf16, of 6 significant bits):
+// the products are bf16 numbers, the upper halves of the floats.
+__device__ __forceinline__ u32x4 e2m1_times(uint32_t w, const u32x4& scales) {
+  typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+  f32x2 t[4];
+  t[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+  t[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+  t[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+  t[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = t[i][0] * __uint_as_float(scales[i] << 16), hi = t[i][1] * __uint_as_float(scales[i] & 0xffff0000u);
+    r[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+  }
+  return r;
+}
+
 // 2^(byte - 127) for byte `at` of w.
 __device__ __forceinline__ float e8m0_scale(uint32_t w, int at) {
   return __uint_as_float(((w >> (8 * at)) & 0xffu) << 23);

@@ -75,7 +75,7 @@ struct SparseArgs {
 // SPARSE: a row's keys are those of its listed pages, one after the other; a row is any token of
 // a ragged batch (b.q_start null: the last of its sequence).
 template <int D, int KV, int MODE, bool SPARSE>
-__global__ void __launch_bounds__(kDecThreads, 2)
+__global__ void __launch_bounds__(kDecThreads, KV == MC_KV_E2M1 ? 3 : 2)
     attn_decode_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                        int head_tiles, SparseArgs sparse) {
   using Step = DecodeStep<D, KV>;
@@ -170,27 +170,36 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   // e4m3 tokens, 537 MB: 109 -> 86 us; of 1024 bf16 tokens and 16 heads 100 -> 83).  A
   // load of keys takes half of each line that it touches, the next the other half: those
   // stay ordinary loads (non-temporal ones: 58 us for 50 at 4 x 32768 e4m3 tokens).
-  auto load = [&](Step& st, int i, int kp, int vp) {
-    const int blk = step_blk(i);
-    const int kb = min(blk + kblk, last_blk), vb = min(blk + vblk, last_blk);
+  auto load_keys = [&](Step& st, int i, int kp) {
+    const int kb = min(step_blk(i) + kblk, last_blk);
     const int kpage = SPARSE ? s_page[(kb >> c.lb) - e0] : kv_page(c, kp);
-    const int vpage = SPARSE ? s_page[(vb >> c.lb) - e0] : kv_page(c, vp);
     const char* kp0 = c.k + kv_block_offset<kBlockBytes>(c, kpage, hk, kb) + koff;
-    const char* vp0 = c.v + kv_block_offset<kBlockBytes>(c, vpage, hk, vb) + voff;
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int u = 0; u < KC; ++u)
         st.k[t][u] = *reinterpret_cast<const typename Step::Piece*>(kp0 + 64 * t + 1024 * u);
+    if constexpr (E2) {
+      const char* ks = c.k + kv_scale_offset<D>(c, kpage, hk, kb);
+      st.ks = *reinterpret_cast<const uint32_t*>(ks + 16 * (D == 64 ? quarter >> 1 : quarter) + 4 * (n & 3));
+    }
+  };
+  auto load_values = [&](Step& st, int i, int vp) {
+    const int vb = min(step_blk(i) + vblk, last_blk);
+    const int vpage = SPARSE ? s_page[(vb >> c.lb) - e0] : kv_page(c, vp);
+    const char* vp0 = c.v + kv_block_offset<kBlockBytes>(c, vpage, hk, vb) + voff;
 #pragma unroll
     for (int t = 0; t < VT; ++t) st.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp0 + 256 * t));
     if constexpr (E2) {
-      const char* ks = c.k + kv_scale_offset<D>(c, kpage, hk, kb);
       const char* vs = c.v + kv_scale_offset<D>(c, vpage, hk, vb);
-      st.ks = *reinterpret_cast<const uint32_t*>(ks + 16 * (D == 64 ? quarter >> 1 : quarter) + 4 * (n & 3));
 #pragma unroll
       for (int t = 0; t < D / 32; ++t) st.vs[t] = *reinterpret_cast<const u32x4*>(vs + 16 * t);
     }
+  };
+
+  auto load = [&](Step& st, int i, int kp, int vp) {
+    load_keys(st, i, kp);
+    load_values(st, i, vp);
   };
 
   f32x4 acc[DT];
@@ -201,7 +210,8 @@ __global__ void __launch_bounds__(kDecThreads, 2)
   const ScoreConsts sc = score_consts(a.scale * kscale, a.softcap);
   const float slope2 = (MODE & 2) && n < heads ? a.slopes[head0 + n] * kLog2e : 0.0f;
 
-  auto compute = [&](Step& st, int i) {
+  // after_keys(): called once the step's keys have been used
+  auto compute = [&](Step& st, int i, auto after_keys) {
     const int key0 = step_blk(i) << 4;
     f32x4 sv[KT];
 #pragma unroll
@@ -225,6 +235,7 @@ __global__ void __launch_bounds__(kDecThreads, 2)
         }
       }
     }
+    after_keys();
     // lane (n, quarter): score (t, r) is of key key0 + 4 KT quarter + 4 t + r
     int lane_key = key0 + 4 * KT * quarter;
     if (SPARSE) {
@@ -328,14 +339,38 @@ __global__ void __launch_bounds__(kDecThreads, 2)
 
   // page numbers are fetched two steps ahead and before the loads of the step
   // between, so that waiting for them does not wait for those
-  if (it < i_end) {
+  auto ids = [&](int i, int& kp, int& vp) {
+    if (SPARSE) return;
+    const int blk = step_blk(min(i, i_end - 1));
+    kp = page_of(blk + kblk);
+    vp = page_of(blk + vblk);
+  };
+  if constexpr (E2) {
+    // One step in registers: the next one's keys are loaded once this one's are used, its values
+    // likewise, and three waves a SIMD instead of two hide each other's starts (48 sequences of 300 to 8191
+    // tokens 54 -> 46 us, 4 of 50000 to 131071 77 -> 71; four waves spill: 70 and 97)
+    if (it < i_end) {
+      Step st;
+      int kp = 0, vp = 0, kn = 0, vn = 0;
+      ids(it, kp, vp);
+      ids(it + kDecWaves, kn, vn);
+      load(st, it, kp, vp);
+      while (true) {
+        ids(it + 2 * kDecWaves, kp, vp);
+        const bool more = it + kDecWaves < i_end;
+        compute(st, it, [&]() {
+          if (more) load_keys(st, it + kDecWaves, kn);
+        });
+        if (!more) break;
+        load_values(st, it + kDecWaves, vn);
+        kn = kp;
+        vn = vp;
+        it += kDecWaves;
+      }
+    }
+  } else if (it < i_end) {
+    const auto none = []() {};
     Step s0, s1;
-    auto ids = [&](int i, int& kp, int& vp) {
-      if (SPARSE) return;
-      const int blk = step_blk(min(i, i_end - 1));
-      kp = page_of(blk + kblk);
-      vp = page_of(blk + vblk);
-    };
     int kp0 = 0, vp0 = 0, kp1 = 0, vp1 = 0;
     ids(it, kp0, vp0);
     ids(it + kDecWaves, kp1, vp1);
@@ -343,12 +378,12 @@ __global__ void __launch_bounds__(kDecThreads, 2)
     while (true) {
       ids(it + 2 * kDecWaves, kp0, vp0);
       if (it + kDecWaves < i_end) load(s1, it + kDecWaves, kp1, vp1);
-      compute(s0, it);
+      compute(s0, it, none);
       it += kDecWaves;
       if (it >= i_end) break;
       ids(it + 2 * kDecWaves, kp1, vp1);
       if (it + kDecWaves < i_end) load(s0, it + kDecWaves, kp0, vp0);
-      compute(s1, it);
+      compute(s1, it, none);
       it += kDecWaves;
       if (it >= i_end) break;
     }

@@ -269,14 +269,8 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
         for (int g = 0; g < 2; ++g) {                  // eight tokens
           const u32x4 vs = sc[g];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                // dimensions 32 j + 16 h + t
-            const u32x4 codes = e2m1_to_bf16(w[2 * h + g], 1.0f);
-            u32x4 r;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              r[e] = bf16_pair(half_of(codes[e], 0) * half_of(vs[e], 0), half_of(codes[e], 1) * half_of(vs[e], 1));
-            *reinterpret_cast<u32x4*>(to + (g * D + 32 * j + 16 * h + t) * 16) = r;
-          }
+          for (int h = 0; h < 2; ++h)                  // dimensions 32 j + 16 h + t
+            *reinterpret_cast<u32x4*>(to + (g * D + 32 * j + 16 * h + t) * 16) = e2m1_times(w[2 * h + g], vs);
         }
       }
       return;

@@ -143,9 +143,8 @@ hipError_t launch_kv_summarize(int D, const BatchArgs& b, const KvArgs& c, const
 }
 
 // ------------------------------------------------------------------ scores --
-constexpr int kScoreThreads = 256;
+constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
 constexpr int kScoreCols = 16;           // (row, head) columns of a product
-constexpr int kScorePages = 256;         // pages of a workgroup, a quarter of them a wave's
 
 // Rows of a workgroup: those whose heads fill the columns.
 __host__ __device__ static inline int score_rows(int g) { return g >= kScoreCols ? 1 : kScoreCols / g; }
@@ -156,26 +155,34 @@ __device__ __forceinline__ void page_range(const SelectArgs& a, int pos, int pag
   lo = a.window > 0 && pos >= a.window ? (pos - a.window + 1) >> page_log : 0;
 }
 
-// The sequence and position of row t (-1: padding, or a row that sees nothing).
-__device__ __forceinline__ int row_position(const BatchArgs& b, const KvArgs& c, int t, int& s) {
-  if (!b.q_start) {
-    s = t;
-    return kv_length(c, b, s) - 1;
-  }
-  s = find_sequence(b.q_start, b.S, t, 1, 0, 1);
-  if (t < b.q_start[s] || t >= b.q_start[s + 1]) return -1;
-  const long long pos = (long long)b.kv_len[s] - ((long long)b.q_start[s + 1] - t);
+// The position of row t of sequence s, whose rows end before `end` (-1: a row that sees nothing).
+__device__ __forceinline__ int row_position(const BatchArgs& b, const KvArgs& c, int s, long long end, int t) {
   const int len = kv_length(c, b, s);
+  const long long pos = (long long)b.kv_len[s] - (end - t);
   return pos < 0 || len == 0 ? -1 : pos < len ? (int)pos : len - 1;
 }
 
-// Workspace: scores [row - row0][Hkv][pages], pages the row length of the tables.
-template <int D>
+// rint(x / by), r being some 1 / by: from the product, unless that is so near to a half that the
+// quotient might lie on the other side of it.
+__device__ __forceinline__ float rint_quotient(float x, float by, float r) {
+  const float y = x * r;
+  float n = rintf(y);
+  if (__any(!(fabsf(y - n) <= 0.4999f))) n = rintf(x / by);     // (and where the product is no number)
+  return n;
+}
+
+// Workspace: scores [row - row0][Hkv][pages], pages the row length of the tables.  A workgroup takes
+// 64 NT pages of a head, a wave NT times 16.  NT = 4 shares a row's quantization among more pages;
+// 1 is for calls that would not fill the chip (one row of 521 pages and 8 heads: 32 workgroups, 9.8
+// us with NT = 4, 7.4 with 1; 16 rows of some 1180 pages: 13.1 us with 4, 17.6 with 1).
+template <int D, int NT>
 __global__ void __launch_bounds__(kScoreThreads)
     page_score_kernel(RowsIn q, BatchArgs b, KvArgs c, SummaryArgs sm, SelectArgs a, int row0, int row1, int chunks,
                       float* __restrict__ scores) {
-  constexpr int NV = D / 64;
-  __shared__ float s_part[kScoreThreads / 64][16][kScoreCols + 1];
+  constexpr int NV = D / 64, kPages = 64 * NT, kQ = D + 16;       // (a row of queries, off the banks of the last)
+  __shared__ float s_part[kScoreWaves][16][kScoreCols + 1];
+  __shared__ float s_most[kScoreWaves][kScoreCols], s_sq[kScoreCols];
+  __shared__ __attribute__((aligned(16))) int8_t s_q[2][kScoreCols][kQ];
   const int lane = threadIdx.x & 63, wave = wave_id(), n = lane & 15, quarter = lane >> 4;
   int id = blockIdx.x;
   const int chunk = id % chunks;
@@ -183,8 +190,10 @@ __global__ void __launch_bounds__(kScoreThreads)
   const int hk = id % c.Hkv, slot = id / c.Hkv, R = score_rows(a.g), page_log = c.lb + 4;
   // rows first, ..., first + rows - 1, of one sequence
   int s, first, rows;
+  long long end;
   if (b.q_start) {
     s = find_sequence(b.q_start, b.S, slot, R, 1, 1);
+    end = b.q_start[s + 1];
     int start, count;
     sequence_rows(b, s, start, count);
     const long long at = ((long long)slot - ((long long)b.q_start[s] / R + s)) * R;
@@ -193,87 +202,109 @@ __global__ void __launch_bounds__(kScoreThreads)
     rows = min(R, count - (int)at);
   } else {
     s = first = slot;
+    end = first + 1;
     rows = 1;
   }
   if (first + rows <= row0 || first >= row1) return;
-  int lo, hi, lo1, hi1, s1;
-  const int pos = row_position(b, c, first + rows - 1, s1), pos0 = row_position(b, c, first, s1);
+  int lo, hi, lo1, hi1;
+  const int pos = row_position(b, c, s, end, first + rows - 1), pos0 = row_position(b, c, s, end, first);
   if (pos < 0) return;
   page_range(a, pos, page_log, lo1, hi);
   page_range(a, pos0 < 0 ? 0 : pos0, page_log, lo, hi1);
-  const int p0 = lo / 16 * 16 + chunk * kScorePages + 16 * wave;
-  if (lo / 16 * 16 + chunk * kScorePages > hi) return;
+  const int p0 = lo / 16 * 16 + chunk * kPages + 16 * wave;       // the wave's: p0 + 64 i ..
+  if (lo / 16 * 16 + chunk * kPages > hi) return;
 
-  // the columns' queries as bytes: lane (column n, quarter) holds dimensions 64 v + 16 quarter ..
-  const int row = first + n / a.g;
-  const bool live = n / a.g < rows && a.g <= kScoreCols;
-  const int32_t* pages = b.page_table + (size_t)s * b.max_pages;
+  // A head tile's queries: thread (wave, column n, quarter) takes dimensions 32 wave + 8 quarter ..
   const int tiles = (a.g + kScoreCols - 1) / kScoreCols;        // of heads, where they pass the columns
+  const int cols = min(a.g, kScoreCols);
+  const int d0 = 32 * wave + 8 * quarter;
+  auto load_q = [&](int ht, bool& mine) {
+    const int r = n / cols, h = a.g > kScoreCols ? kScoreCols * ht + n : n % cols;
+    mine = r < rows && h < a.g && d0 < D;
+    const uint16_t* qr = q.p + (size_t)(first + (mine ? r : 0)) * q.stride + (size_t)(hk * a.g + (mine ? h : 0)) * D;
+    return *reinterpret_cast<const u32x4*>(qr + (mine ? d0 : 0));
+  };
+  bool mine;
+  u32x4 u = load_q(0, mine);
+
+  // the bounds of the wave's pages: lane (page n, quarter) holds dimensions 64 v + 16 quarter ..
+  const int32_t* pages = b.page_table + (size_t)s * b.max_pages;
+  size_t at[NT];
+  i32x4 bl[NT][NV], bh[NT][NV];
+  float ps[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) at[i] = (size_t)kv_page(c, pages[min(p0 + 64 * i + n, hi)]) * c.Hkv + hk;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int8_t* from = sm.bounds + at[i] * 2 * D + 16 * quarter;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      bl[i][v] = *reinterpret_cast<const i32x4*>(from + 64 * v);
+      bh[i][v] = *reinterpret_cast<const i32x4*>(from + D + 64 * v);
+    }
+    ps[i] = sm.scale[at[i]];
+  }
+
+  // The columns' queries as bytes, by way of LDS (each wave for itself: four times the instructions, which a
+  // workgroup runs once and waits for), while the bounds are on their way: the barriers do not wait for them
   for (int ht = 0; ht < tiles; ++ht) {
-    const int h = a.g > kScoreCols ? kScoreCols * ht + n : n % a.g;
-    const bool mine = a.g > kScoreCols ? h < a.g : live;
-    const uint16_t* qr = q.p + (size_t)(mine ? (a.g > kScoreCols ? first : row) : first) * q.stride +
-                         (size_t)(hk * a.g + (mine ? h : 0)) * D + 16 * quarter;
-    float x[NV][16], most = 0.0f;
+    if (ht > 0) u = load_q(ht, mine);
+    float x[8], most = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const u32x4 r = *reinterpret_cast<const u32x4*>(qr + 64 * v + 8 * w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float f = half_of(r[e / 2], e & 1);
-          if (a.negative) f = -f;
-          f = fabsf(f) < -kNegInf ? f : 0.0f;
-          x[v][8 * w + e] = f;
-          most = fmaxf(most, fabsf(f));
-        }
-      }
+    for (int e = 0; e < 8; ++e) {
+      float f = half_of(u[e / 2], e & 1);
+      f = mine && fabsf(f) < -kNegInf ? f : 0.0f;
+      x[e] = a.negative ? -f : f;
+      most = fmaxf(most, fabsf(f));
+    }
     most = halves_max(rows_max(most));
-    const float sq = most * k127th, by = sq > 0.0f ? sq : 1.0f;
+    if (ht > 0) lds_barrier();                     // the last tile's have been read
+    if (quarter == 0) s_most[wave][n] = most;
+    lds_barrier();
+    most = fmaxf(fmaxf(s_most[0][n], s_most[1][n]), fmaxf(s_most[2][n], s_most[3][n]));
+    const float sq = most * k127th, by = sq > 0.0f ? sq : 1.0f, rby = 1.0f / by;
+    if (threadIdx.x < kScoreCols) s_sq[n] = sq;
+    if (d0 < D) {
+      u32x2 lo8 = {0u, 0u}, hi8 = {0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float f = rint_quotient(x[e], by, rby);
+        f = f > 127.0f ? 127.0f : f < -127.0f ? -127.0f : f;
+        const int i = (int)f;
+        lo8[e / 4] |= (uint32_t)((i < 0 ? i : 0) & 0xff) << (8 * (e & 3));
+        hi8[e / 4] |= (uint32_t)((i > 0 ? i : 0) & 0xff) << (8 * (e & 3));
+      }
+      *reinterpret_cast<u32x2*>(&s_q[0][n][d0]) = lo8;
+      *reinterpret_cast<u32x2*>(&s_q[1][n][d0]) = hi8;
+    }
+    lds_barrier();
     i32x4 neg[NV], plus[NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+      neg[v] = *reinterpret_cast<const i32x4*>(&s_q[0][n][64 * v + 16 * quarter]);
+      plus[v] = *reinterpret_cast<const i32x4*>(&s_q[1][n][64 * v + 16 * quarter]);
+    }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t lo4 = 0, hi4 = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float f = rintf(x[v][4 * w + e] / by);
-          f = f > 127.0f ? 127.0f : f < -127.0f ? -127.0f : f;
-          const int i = (int)f;
-          lo4 |= (uint32_t)((i < 0 ? i : 0) & 0xff) << (8 * e);
-          hi4 |= (uint32_t)((i > 0 ? i : 0) & 0xff) << (8 * e);
-        }
-        neg[v][w] = (int)lo4;
-        plus[v][w] = (int)hi4;
-      }
-    for (int p = p0; p <= hi && p < p0 + kScorePages; p += kScoreThreads / 64 * 16) {
-      const int mine_p = min(p + n, b.max_pages - 1);
-      const size_t at = ((size_t)kv_page(c, pages[mine_p]) * c.Hkv + hk) * 2 * D + 16 * quarter;
+    for (int i = 0; i < NT; ++i) {
+      if (p0 + 64 * i > hi) break;                 // the same for the whole wave
       i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const i32x4 bl = *reinterpret_cast<const i32x4*>(sm.bounds + at + 64 * v);
-        const i32x4 bh = *reinterpret_cast<const i32x4*>(sm.bounds + at + D + 64 * v);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bl, neg[v], sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bh, plus[v], sum, 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bl[i][v], neg[v], sum, 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bh[i][v], plus[v], sum, 0, 0, 0);
       }
-      // lane (column n, quarter): pages p + 4 quarter + r
-      asm volatile("" ::: "memory");             // the wave's own places: LDS is in order
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int pr = min(p + 4 * quarter + r, b.max_pages - 1);
-        const float ps = sm.scale[(size_t)kv_page(c, pages[pr]) * c.Hkv + hk];
-        s_part[wave][4 * quarter + r][n] = mine ? (float)sum[r] * (sq * ps) : kNegInf;
-      }
+      // lane (column n, quarter): pages 4 quarter + r of the tile.  Heads are joined by way of LDS, whose
+      // accesses are in order (the places are the wave's own); there lane (n, quarter) has page n
       asm volatile("" ::: "memory");
-      const int page = p + n;
-      for (int i = quarter; i < rows; i += 4) {
-        const int cols = min(a.g, kScoreCols);
-        float m = s_part[wave][n][i * cols];
-        for (int j = 1; j < cols; ++j) m = fmaxf(m, s_part[wave][n][i * cols + j]);
-        const int t = first + i;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) s_part[wave][4 * quarter + r4][n] = (float)sum[r4];
+      asm volatile("" ::: "memory");
+      const int page = p0 + 64 * i + n;
+      for (int k = quarter; k < rows; k += 4) {
+        float m = kNegInf;
+        for (int j = 0; j < cols && cols * ht + j < a.g; ++j)
+          m = fmaxf(m, s_part[wave][n][k * cols + j] * (s_sq[k * cols + j] * ps[i]));
+        const int t = first + k;
         if (page <= hi && t >= row0 && t < row1) {
           float* out = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + page;
           if (ht > 0) m = fmaxf(m, *out);
@@ -287,7 +318,6 @@ __global__ void __launch_bounds__(kScoreThreads)
 
 // --------------------------------------------------------------- selection --
 constexpr int kSelThreads = 256;
-constexpr int kSelCached = 8192;         // scores that fit LDS
 
 // A float's bits, ordered as unsigned numbers (zeros of both signs alike; NaN last).
 __device__ __forceinline__ uint32_t score_key(float f) {
@@ -296,14 +326,19 @@ __device__ __forceinline__ uint32_t score_key(float f) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Threads before this one whose flag is set, and all of them; tmp: one place a wave.
-__device__ __forceinline__ int flags_before(bool flag, int* tmp, int& all) {
-  const uint64_t set = __ballot(flag);
+// The sum over the threads before this one, and over all; tmp: one place a wave.
+__device__ __forceinline__ int counts_before(int x, int* tmp, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int y = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int z = __shfl_up(y, d);
+    if (lane >= d) y += z;
+  }
   __syncthreads();                               // the last call's places have been read
-  if (lane == 0) tmp[wave] = __popcll(set);
+  if (lane == 63) tmp[wave] = y;
   __syncthreads();
-  int before = __popcll(set & ((1ull << lane) - 1)), sum = 0;
+  int before = y - x, sum = 0;
 #pragma unroll
   for (int w = 0; w < kSelThreads / 64; ++w) {
     if (w < wave) before += tmp[w];
@@ -313,42 +348,43 @@ __device__ __forceinline__ int flags_before(bool flag, int* tmp, int& all) {
   return before;
 }
 
-__global__ void __launch_bounds__(kSelThreads)
-    page_select_kernel(BatchArgs b, KvArgs c, SelectArgs a, int row0, const float* __restrict__ scores) {
-  __shared__ uint32_t s_key[kSelCached];
-  __shared__ int s_hist[256], s_tmp[kSelThreads / 64], s_found[2];
-  const int t = row0 + blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv, page_log = c.lb + 4;
-  if (b.q_start && (t < b.q_start[0] || t >= b.q_start[b.S])) return;       // padding
-  int s;
-  const int pos = row_position(b, c, t, s);
-  int32_t* out = a.sel + ((size_t)t * c.Hkv + hk) * a.n_sel;
-  int lo = 0, hi = -1;
-  if (pos >= 0) page_range(a, pos, page_log, lo, hi);
-  const int pages = hi - lo + 1, count = min(pages, a.n_sel);
-  if (threadIdx.x == 0) a.count[(size_t)t * c.Hkv + hk] = count;
-  if (pages <= a.n_sel) {
-    for (int i = threadIdx.x; i < a.n_sel; i += kSelThreads) out[i] = i < pages ? lo + i : -1;
-    return;
-  }
-  const float* row = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + lo;
-  auto key_of = [&](int i) {                     // pages that are always taken come first
-    const int p = lo + i;
-    return p < a.first || p > hi - a.last ? 0xffffffffu : score_key(row[i]);
+// A thread takes K neighbouring pages a round, in registers; more than one round of them (HELD
+// false) are read again in each pass.
+template <int K, bool HELD>
+__device__ void select_pages(const SelectArgs& a, const float* __restrict__ row, int lo, int hi,
+                             int32_t* __restrict__ out, int (*s_hist)[256], int* s_tmp, int* s_found) {
+  const int pages = hi - lo + 1, rounds = HELD ? 1 : (pages + K * kSelThreads - 1) / (K * kSelThreads);
+  uint32_t key[K];
+  auto load = [&](int round) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = (round * kSelThreads + (int)threadIdx.x) * K + k, p = lo + i;
+      key[k] = i >= pages ? 0u : p < a.first || p > hi - a.last ? 0xffffffffu : score_key(row[i]);
+    }
   };
-  const bool cached = pages <= kSelCached;
-  if (cached)
-    for (int i = threadIdx.x; i < pages; i += kSelThreads) s_key[i] = key_of(i);
-  auto key = [&](int i) { return cached ? s_key[i] : key_of(i); };
-  // the n_sel-th largest key, a byte at a time; `left`: how many of its equals are taken
+  // the n_sel-th largest key, a byte at a time; `left`: how many of those at the prefix are taken.  (Places
+  // behind the last page hold 0 and lose to every page.)
   uint32_t prefix = 0;
-  int left = a.n_sel;
-  for (int shift = 24; shift >= 0; shift -= 8) {
+  int left = a.n_sel, shift = 24;
+  for (int i = threadIdx.x; i < 512; i += kSelThreads) s_hist[i >> 8][i & 255] = 0;
+  if (HELD) load(0);
+  for (;; shift -= 8) {
+    int* hist = s_hist[(shift >> 3) & 1];
     __syncthreads();
-    s_hist[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < pages; i += kSelThreads) {
-      const uint32_t k = key(i);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&s_hist[(k >> shift) & 255u], 1);
+    for (int r = 0; r < rounds; ++r) {
+      if (!HELD) load(r);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const bool in = shift == 24 || (key[k] >> (shift + 8)) == prefix;
+        const uint32_t digit = (key[k] >> shift) & 255u;
+        // most scores share their first digits: those of the first lane's are counted at once
+        const uint32_t lead = __builtin_amdgcn_readfirstlane(digit);
+        const uint64_t same = __ballot(in && digit == lead);
+        if (in && digit != lead)
+          atomicAdd(&hist[digit], 1);
+        else if ((threadIdx.x & 63) == 0 && same)
+          atomicAdd(&hist[lead], __popcll(same));
+      }
     }
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -357,7 +393,7 @@ __global__ void __launch_bounds__(kSelThreads)
       int h[4], sum = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = s_hist[255 - 4 * l - i];
+        h[i] = hist[255 - 4 * l - i];
         sum += h[i];
       }
       int before = sum;
@@ -372,27 +408,76 @@ __global__ void __launch_bounds__(kSelThreads)
         if (before < left && before + h[i] >= left) {
           s_found[0] = 255 - 4 * l - i;
           s_found[1] = left - before;
+          s_found[2] = h[i];
         }
         before += h[i];
       }
+    } else {
+      int* next = s_hist[((shift >> 3) & 1) ^ 1];
+      for (int i = threadIdx.x - 64; i < 256; i += kSelThreads - 64) next[i] = 0;
     }
     __syncthreads();
     prefix = prefix << 8 | (uint32_t)s_found[0];
     left = s_found[1];
+    if (shift == 0 || left == s_found[2]) break;           // all at the prefix are taken
   }
+  // those above the prefix and the first `left` at it, in order
   int done = 0, equal = 0;
-  for (int i0 = 0; i0 < pages; i0 += kSelThreads) {
-    const int i = i0 + threadIdx.x;
-    const uint32_t k = i < pages ? key(i) : 0u;
-    int all_eq, all;
-    const bool eq = i < pages && k == prefix;
-    const int rank = equal + flags_before(eq, s_tmp, all_eq);
-    const bool take = i < pages && (k > prefix || (eq && rank < left));
-    const int at = done + flags_before(take, s_tmp, all);
-    if (take && at < a.n_sel) out[at] = lo + i;
-    equal += all_eq;
-    done += all;
+  for (int r = 0; r < rounds; ++r) {
+    if (!HELD) load(r);
+    int above = 0, at = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t top = key[k] >> shift;
+      above += top > prefix;
+      at += top == prefix;
+    }
+    // (both sums in one: up to 2^14 a round)
+    int all;
+    const int before = counts_before(above << 16 | at, s_tmp, all);
+    int rank = equal + (before & 0xffff);                  // of the first at the prefix
+    int place = done + (before >> 16) + min(rank, left);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t top = key[k] >> shift;
+      const bool take = top > prefix || (top == prefix && rank < left);
+      rank += top == prefix;
+      if (take && place < a.n_sel) out[place] = lo + (r * kSelThreads + (int)threadIdx.x) * K + k;
+      place += take;
+    }
+    done += all >> 16;
+    equal += all & 0xffff;
   }
+}
+
+__global__ void __launch_bounds__(kSelThreads)
+    page_select_kernel(BatchArgs b, KvArgs c, SelectArgs a, int row0, const float* __restrict__ scores) {
+  __shared__ int s_hist[2][256], s_tmp[kSelThreads / 64], s_found[3];
+  const int t = row0 + blockIdx.x / c.Hkv, hk = blockIdx.x % c.Hkv, page_log = c.lb + 4;
+  int s = t;
+  long long end = t + 1;
+  if (b.q_start) {
+    s = find_sequence(b.q_start, b.S, t, 1, 0, 1);
+    end = b.q_start[s + 1];
+    if (t < b.q_start[s] || t >= end) return;      // padding
+  }
+  const int pos = row_position(b, c, s, end, t);
+  int32_t* out = a.sel + ((size_t)t * c.Hkv + hk) * a.n_sel;
+  int lo = 0, hi = -1;
+  if (pos >= 0) page_range(a, pos, page_log, lo, hi);
+  const int pages = hi - lo + 1, count = min(pages, a.n_sel);
+  if (threadIdx.x == 0) a.count[(size_t)t * c.Hkv + hk] = count;
+  if (pages <= a.n_sel) {
+    for (int i = threadIdx.x; i < a.n_sel; i += kSelThreads) out[i] = i < pages ? lo + i : -1;
+    return;
+  }
+  const float* row = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + lo;
+  if (pages <= 2 * kSelThreads)
+    select_pages<2, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
+  else if (pages <= 8 * kSelThreads)
+    select_pages<8, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
+  else
+    select_pages<8, false>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
 }
 
 static int score_slots(const BatchArgs& b, int g) {
@@ -410,27 +495,43 @@ size_t attn_select_bytes(int rows, int Hkv, int max_pages) {
   return select_rows(rows, Hkv, max_pages) * Hkv * max_pages * sizeof(float);
 }
 
+// Chunks of 64 NT pages that cover any row's (the first begins at a multiple of 16 pages, below the
+// first page of the row).
+static int score_chunks(int max_pages, int nt) { return (max_pages + 64 * nt - 1) / (64 * nt) + 1; }
+
+// Pages a wave takes, in tiles: see page_score_kernel.
+static int score_tiles(const BatchArgs& b, const KvArgs& c, int g) {
+  return (long long)score_slots(b, g) * c.Hkv * score_chunks(b.max_pages, 4) < 512 ? 1 : 4;
+}
+
 long long select_workgroups(const BatchArgs& b, const KvArgs& c, int g) {
-  return (long long)score_slots(b, g) * c.Hkv * ((b.max_pages + kScorePages - 1) / kScorePages + 1);
+  return (long long)score_slots(b, g) * c.Hkv * score_chunks(b.max_pages, score_tiles(b, c, g));
+}
+
+template <int D, int NT>
+static void score_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm, const SelectArgs& a,
+                         int row0, int row1, float* scores, hipStream_t stream) {
+  const int chunks = score_chunks(b.max_pages, NT);
+  const dim3 grid((unsigned)((size_t)score_slots(b, a.g) * c.Hkv * chunks));
+  hipLaunchKernelGGL((page_score_kernel<D, NT>), grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1,
+                     chunks, scores);
 }
 
 hipError_t launch_attn_select(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm,
                               const SelectArgs& a, void* ws, hipStream_t stream) {
   const int rows = b.q_start ? b.T : b.S, each = (int)select_rows(rows, c.Hkv, b.max_pages);
-  // (the first chunk begins at a multiple of 16 pages, below the first page of the row)
-  const int chunks = (b.max_pages + kScorePages - 1) / kScorePages + 1;
+  const bool few = score_tiles(b, c, a.g) == 1;
   float* scores = static_cast<float*>(ws);
   hipError_t err = hipSuccess;
   for (int row0 = 0; row0 < rows && err == hipSuccess; row0 += each) {
     const int row1 = row0 + each < rows ? row0 + each : rows;
-    const dim3 grid((unsigned)((size_t)score_slots(b, a.g) * c.Hkv * chunks));
     timing_begin(stream, kSiteAttnSelect);
     if (D == 64)
-      hipLaunchKernelGGL(page_score_kernel<64>, grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1,
-                         chunks, scores);
+      few ? score_launch<64, 1>(q, b, c, sm, a, row0, row1, scores, stream)
+          : score_launch<64, 4>(q, b, c, sm, a, row0, row1, scores, stream);
     else
-      hipLaunchKernelGGL(page_score_kernel<128>, grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1,
-                         chunks, scores);
+      few ? score_launch<128, 1>(q, b, c, sm, a, row0, row1, scores, stream)
+          : score_launch<128, 4>(q, b, c, sm, a, row0, row1, scores, stream);
     hipLaunchKernelGGL(page_select_kernel, dim3((unsigned)((size_t)(row1 - row0) * c.Hkv)), dim3(kSelThreads), 0,
                        stream, b, c, a, row0, scores);
     timing_end(stream, kSiteAttnSelect);

@@ -41,22 +41,21 @@ __device__ __forceinline__ bool append_place(const KvArgs& c, const BatchArgs& b
 // 7 2^e (7 being the border between 6, the largest level, and the next that there would be).  Of
 // values, 64 dimensions: max|v| times the fp32 number nearest to 1/6, rounded to 6 significant bits so that its products with the codes
 // are bf16 numbers.  Groups below 2^-100 are 0, those with a NaN, an infinity or more than 7 2^125 NaN.
-constexpr double kGroupLeast = 0x1p-100, kGroupMost = 0x1.cp127;
+constexpr float kGroupLeast = 0x1p-100f, kGroupMost = 0x1.cp127f;
 
 // Byte of the scale 2^(byte - 127) of a group of keys whose largest magnitude is m (NaN: 255).
-__device__ __forceinline__ uint32_t key_scale_byte(double m) {
+__device__ __forceinline__ uint32_t key_scale_byte(float m) {
   if (!(m <= kGroupMost)) return 255u;
   if (m < kGroupLeast) return 0u;
-  const unsigned long long b = __double_as_longlong(m);
+  const uint32_t b = __float_as_uint(m);
   // m = 2^k (1 + f): e = k - 2, or k - 1 where 1 + f > 7/4
-  const int k = (int)(b >> 52) - 1023;
-  return (uint32_t)(k - 2 + ((b & 0xfffffffffffffull) > 0xc000000000000ull ? 1 : 0) + 127);
+  return (b >> 23) - 2u + ((b & 0x7fffffu) > 0x600000u ? 1u : 0u);
 }
 
 // The scale of a group of values (bf16) whose largest magnitude is m, as a float.
 __device__ __forceinline__ float value_scale(float m) {
-  if (!(m <= (float)kGroupMost)) return __uint_as_float(0x7fc00000u);
-  if (m < (float)kGroupLeast) return 0.0f;
+  if (!(m <= kGroupMost)) return __uint_as_float(0x7fc00000u);
+  if (m < kGroupLeast) return 0.0f;
   uint32_t u = __float_as_uint(m * (1.0f / 6.0f));
   u += 0x1ffffu + ((u >> 18) & 1u);
   return __uint_as_float(u & ~0x3ffffu);
@@ -68,12 +67,6 @@ __device__ __forceinline__ float magnitude(float a, float b) {
   b = fabsf(b);
   return a >= b || a != a ? a : b;
 }
-__device__ __forceinline__ double magnitude(double a, double b) {
-  a = fabs(a);
-  b = fabs(b);
-  return a >= b || a != a ? a : b;
-}
-
 // x of the lane that the DPP control names.
 template <int CTRL>
 __device__ __forceinline__ double dpp64(double x) {
@@ -90,16 +83,49 @@ __device__ __forceinline__ uint32_t e2m1_pair(uint32_t w, float a, float b) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, 1.0f, AT);
 }
 
-// A double as a float that every comparison with a border of the codes takes the same way: rounded
-// towards odd (the borders have 3 significant bits).
-__device__ __forceinline__ float sticky_float(double v) {
-  float f = (float)v;
-  if ((double)f != v) {
-    uint32_t b = __float_as_uint(f);
-    if (fabs((double)f) > fabs(v)) b -= 1u;
-    f = __uint_as_float(b | 1u);
+// Eight codes in a word.
+__device__ __forceinline__ uint32_t e2m1_word(const float (&x)[8]) {
+  uint32_t w = 0;
+  w = e2m1_pair<0>(w, x[0], x[1]);
+  w = e2m1_pair<1>(w, x[2], x[3]);
+  w = e2m1_pair<2>(w, x[4], x[5]);
+  return e2m1_pair<3>(w, x[6], x[7]);
+}
+
+// a[i]'s nibble j to a[j]'s nibble i: single nibbles, then bytes, then halves.
+__device__ __forceinline__ void transpose_nibbles(uint32_t (&a)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const uint32_t x = a[i], y = a[i + 1];
+    a[i] = (x & 0x0f0f0f0fu) | ((y & 0x0f0f0f0fu) << 4);
+    a[i + 1] = ((x >> 4) & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u);
   }
-  return f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = 4 * (k >> 1) + (k & 1);
+    const uint32_t x = a[i], y = a[i + 2];       // bytes x0 y0 x2 y2, and x1 y1 x3 y3
+    a[i] = __builtin_amdgcn_perm(y, x, 0x06020400u);
+    a[i + 2] = __builtin_amdgcn_perm(y, x, 0x07030501u);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = a[i], y = a[i + 4];
+    a[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+    a[i + 4] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+  }
+}
+
+// A double as a float that compares with every border of codes and scales (3 significant bits) as the
+// double does: its first 24 bits, the last one set where any follow.  Numbers past a float's range,
+// infinities and NaN become the largest float, those below it the smallest ones.  (In whole numbers: a
+// conversion and back cost four times as much.)
+__device__ __forceinline__ float sticky_float(double v) {
+  const unsigned long long b = __double_as_longlong(v);
+  const uint32_t hi = (uint32_t)(b >> 32), lo = (uint32_t)b;
+  uint32_t h = hi & 0x7fffffffu;
+  h = h < 0x38000000u ? 0x38000000u : h > 0x47efffffu ? 0x47efffffu : h;
+  const uint32_t f = __builtin_amdgcn_alignbit(h - 0x38000000u, lo, 29), rest = lo & 0x1fffffffu;
+  return __uint_as_float(f | (rest < 1u ? rest : 1u) | (hi & 0x80000000u));
 }
 
 // v / s, so exact that a quotient on a border of the codes is on it: v and s are bf16 numbers, whose
@@ -151,31 +177,32 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
     return c.v + kv_block_offset<kBlockBytes>(c, at.page, h, at.pos >> 4) + (size_t)(in_block / U) * D * 16;
   };
   if constexpr (E2) {
-    // lane: dimensions d0 .. d0 + 7, half of a unit's eight bytes; 64 dimensions in 8 neighbouring lanes
-    if (!mine) return;                           // (whole groups of 8 lanes are)
-    const int blk = at.pos >> 4;
-    char* codes = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, blk) + d0 / 32 * 256 + (d0 & 15) * 16 +
-                  (d0 / 16 & 1) * 8;
-    uint16_t* scales = reinterpret_cast<uint16_t*>(c.v + kv_scale_offset<D>(c, at.page, head, blk)) + d0 / 64 * 16;
-    // the other tokens' codes of the bytes
-    u32x2 w[8];
-    if (!all) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x2*>(codes + 16 * i);
-    }
-    uint32_t sw[8] = {};
-    float x[16][8];
+    // lane: dimensions d0 .. d0 + 7, halves of 8 units; 64 dimensions in 8 neighbouring lanes
     uint32_t live = 0;
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
       const long long pos = base + u, row = first + pos - p0;
-      const bool in = pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T;
-      live |= in ? 1u << u : 0u;
-      float m = 0.0f;
+      live |= pos >= lo && pos < hi && pos < end && row >= 0 && row < b.T ? 1u << u : 0u;
+    }
+    live = __builtin_amdgcn_readfirstlane(live);
+    const int blk = at.pos >> 4, unit = d0 / 32 * 256 + (d0 & 15) * 16 + (d0 / 16 & 1) * 8;
+    char* codes = c.v + kv_block_offset<kBlockBytes>(c, at.page, head, blk);
+    u32x2 w[8];                                  // the other tokens' codes of the bytes
+    if (!all && mine) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x2*>(codes + unit + 16 * i);
+    }
+    // a token's eight codes in a word; tokens that are not among the new ones are passed by (one token: 16
+    // tests and one of these)
+    uint32_t code[16] = {}, sw[8] = {};
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      if (!((live >> u) & 1u)) continue;
+      float x[8], m = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[u][i] = half_of(raw[u][i / 2], i & 1);
-        m = magnitude(x[u][i], m);
+        x[i] = half_of(raw[u][i / 2], i & 1);
+        m = magnitude(x[i], m);
       }
       m = magnitude(m, dpp<0xb1>(m));
       m = magnitude(m, dpp<0x4e>(m));
@@ -184,33 +211,59 @@ __device__ void append_values(RowsIn v, const BatchArgs& b, const KvArgs& c, int
       sw[u / 2] |= (__float_as_uint(s) >> 16) << (16 * (u & 1));
       const Divisor by(s);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[u][i] = s > 0.0f ? by(x[u][i]) : 0.0f;
+      for (int i = 0; i < 8; ++i) x[i] = s > 0.0f ? by(x[i]) : 0.0f;
+      code[u] = e2m1_word(x);
     }
+    // words of a dimension's tokens
+    u32x2 t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      u32x2 r;
+    for (int q = 0; q < 2; ++q) {
+      uint32_t a[8];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t t = 0;
-        t = e2m1_pair<0>(t, x[8 * q][i], x[8 * q + 1][i]);
-        t = e2m1_pair<1>(t, x[8 * q + 2][i], x[8 * q + 3][i]);
-        t = e2m1_pair<2>(t, x[8 * q + 4][i], x[8 * q + 5][i]);
-        t = e2m1_pair<3>(t, x[8 * q + 6][i], x[8 * q + 7][i]);
-        if (!all) {
-          uint32_t keep = 0;
+      for (int i = 0; i < 8; ++i) a[i] = code[8 * q + i];
+      transpose_nibbles(a);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) keep |= (live >> (8 * q + e)) & 1u ? 0u : 0xfu << (4 * e);
-          t = (t & ~keep) | (w[i][q] & keep);
-        }
-        r[q] = t;
+      for (int i = 0; i < 8; ++i) t[i][q] = a[i];
+    }
+    if ((lane & 7) == 0 && mine) {
+      uint16_t* scales = reinterpret_cast<uint16_t*>(c.v + kv_scale_offset<D>(c, at.page, head, blk)) + d0 / 64 * 16;
+      if (all) {
+        *reinterpret_cast<u32x4*>(scales) = u32x4{sw[0], sw[1], sw[2], sw[3]};
+        *reinterpret_cast<u32x4*>(scales + 8) = u32x4{sw[4], sw[5], sw[6], sw[7]};
+      } else {
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+          if ((live >> u) & 1u) scales[u] = (uint16_t)(sw[u / 2] >> (16 * (u & 1)));
       }
-      // bytes of other tokens are written back as they were: nobody else writes this block's values
-      *reinterpret_cast<u32x2*>(codes + 16 * i) = r;
     }
-    if ((lane & 7) == 0) {
+    if (!all) {
+      if (!mine) return;
+      uint32_t keep[2] = {0u, 0u};
 #pragma unroll
-      for (int u = 0; u < 16; ++u)
-        if ((live >> u) & 1u) scales[u] = (uint16_t)(sw[u / 2] >> (16 * (u & 1)));
+      for (int u = 0; u < 16; ++u) keep[u / 8] |= (live >> u) & 1u ? 0u : 0xfu << (4 * (u & 7));
+      // (codes of other tokens are written back as they were: nobody else writes this block's values)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<u32x2*>(codes + unit + 16 * i) =
+            u32x2{(t[i][0] & ~keep[0]) | (w[i][0] & keep[0]), (t[i][1] & ~keep[1]) | (w[i][1] & keep[1])};
+      return;
+    }
+    // whole units, 64 side by side, by way of LDS, where unit n of 16 lies at n ^ (its row) so that the halves
+    // that a wave writes at once meet different banks
+    char* half = reinterpret_cast<char*>(lds);
+    const int row = 8 * lane / 32;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      *reinterpret_cast<u32x2*>(half + row * 256 + ((((8 * lane) & 15) + i) ^ (row & 15)) * 16 + (lane >> 1 & 1) * 8) =
+          t[i];
+    asm volatile("" ::: "memory");               // the wave's own: its LDS accesses are in order
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int u = 64 * k + lane, ch = piece * 64 + 4 * (u >> 4);        // the unit's first chunk
+      const u32x4 v16 = *reinterpret_cast<const u32x4*>(half + (u >> 4) * 256 + ((u & 15) ^ (u >> 4 & 15)) * 16);
+      if (ch >= chunks) continue;
+      const int h = ch / (D / 8), j = ch % (D / 8) / 4;
+      *reinterpret_cast<u32x4*>(c.v + kv_block_offset<kBlockBytes>(c, at.page, h, blk) + j * 256 + (u & 15) * 16) = v16;
     }
     return;
   }
@@ -417,8 +470,8 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
               for (int j = 0; j < 4; ++j) {
                 const double co = tab[j / 2][2 * (j & 1)], si = tab[j / 2][2 * (j & 1) + 1];
                 const double a = y[2 * j], z = y[2 * j + 1];
-                y[2 * j] = a * co - z * si;
-                y[2 * j + 1] = z * co + a * si;
+                y[2 * j] = __builtin_fma(-z, si, a * co);
+                y[2 * j + 1] = __builtin_fma(z, co, a * si);
               }
             }
           } else if (p.rot) {
@@ -428,30 +481,27 @@ __device__ void append_rows(RowsIn q, RowsIn k, int Hq, const QkPrepArgs& p, con
             if (turns) {
 #pragma unroll
               for (int j = 0; j < 8; ++j)
-                y[j] = y[j] * (double)tab[j / 2][2 * (j & 1)] + o[j] * (double)tab[j / 2][2 * (j & 1) + 1];
+                y[j] = __builtin_fma(o[j], (double)tab[j / 2][2 * (j & 1) + 1], y[j] * (double)tab[j / 2][2 * (j & 1)]);
             }
           }
-          double m = 0.0;
+          float f[8], m = 0.0f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) m = magnitude(y[j], m);
-          m = magnitude(m, dpp64<0xb1>(m));
-          m = magnitude(m, dpp64<0x4e>(m));              // of the lanes of 32 dimensions
+          for (int j = 0; j < 8; ++j) {
+            f[j] = sticky_float(y[j]);
+            m = fmaxf(m, fabsf(f[j]));
+          }
+          m = fmaxf(m, dpp<0xb1>(m));
+          m = fmaxf(m, dpp<0x4e>(m));                    // of the lanes of 32 dimensions
           const uint32_t byte = key_scale_byte(m);
           if (i < total && !is_q) {
+            // 2^(127 - byte), the products are exact, or far below the first border
             const bool number = byte != 0u && byte != 255u;
-            // 2^(127 - byte)
-            const double by = __longlong_as_double((long long)(1023 + 127 - (int)byte) << 52);
-            float f[8];
+            const float by = number ? __uint_as_float((254u - byte) << 23) : 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = number ? sticky_float(y[j] * by) : 0.0f;
-            uint32_t w = 0;
-            w = e2m1_pair<0>(w, f[0], f[1]);
-            w = e2m1_pair<1>(w, f[2], f[3]);
-            w = e2m1_pair<2>(w, f[4], f[5]);
-            w = e2m1_pair<3>(w, f[6], f[7]);
+            for (int j = 0; j < 8; ++j) f[j] = number ? f[j] * by : 0.0f;
             const int head = (i - nq) / DU, t16 = at.pos & 15;
             char* dst = c.k + kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4);
-            *reinterpret_cast<uint32_t*>(dst + d0 / 32 * 256 + t16 * 16 + (d0 / 8 & 3) * 4) = w;
+            *reinterpret_cast<uint32_t*>(dst + d0 / 32 * 256 + t16 * 16 + (d0 / 8 & 3) * 4) = e2m1_word(f);
             if ((lane & 3) == 0)
               c.k[kv_scale_offset<D>(c, at.page, head, at.pos >> 4) + d0 / 32 * 16 + 4 * (t16 & 3) + (t16 >> 2)] =
                   (char)byte;
@@ -532,12 +582,13 @@ template <int D, int KV, int NORM>
 __global__ void __launch_bounds__(kAppendThreads)
     kv_append_kernel(RowsIn q, RowsIn k, RowsIn v, int Hq, QkPrepArgs p, BatchArgs b, KvArgs c, RowsOut out, int nv,
                      int slots, int pieces, int parts) {
-  __shared__ u32x4 s_units[kAppendThreads * 8];
+  constexpr int kUnits = KV == MC_KV_E2M1 ? 4 : 8;
+  __shared__ u32x4 s_units[kAppendThreads * kUnits];
   const int blk = blockIdx.x;
   if (blk < nv) {
     const int w = blk * (kAppendThreads / 64) + wave_id();
     if (w < slots * pieces)
-      append_values<D, KV>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 512);
+      append_values<D, KV>(v, b, c, p.n_pos, w / pieces, w % pieces, s_units + wave_id() * 64 * kUnits);
     return;
   }
   const int r0 = blk - nv, group = r0 / (16 * parts), in = r0 - group * 16 * parts, r = in & 15;
@@ -577,80 +628,117 @@ hipError_t launch_kv_append(RowsIn q, RowsIn k, RowsIn v, int Hq, int D, const Q
 }
 
 // ------------------------------------------------------------------- read --
-// What the cache holds at the new tokens' places: a lane takes 8 dimensions of one token and head,
-// keys and values.
+// What the cache holds at the new tokens' places: a wave takes one head of a block of 16 tokens.  Keys'
+// units are pieces of rows; values' units, which run along the tokens, become rows in LDS.
 template <int D, int KV>
 __global__ void __launch_bounds__(kAppendThreads)
-    kv_read_kernel(BatchArgs b, KvArgs c, RowsOut ko, RowsOut vo, int total) {
+    kv_read_kernel(BatchArgs b, KvArgs c, RowsOut ko, RowsOut vo, int slots) {
   constexpr bool E4 = KV == MC_KV_E4M3, E2 = KV == MC_KV_E2M1;
-  constexpr int DU = D / 8, kBlockBytes = KvFormat<D, KV>::kBlockBytes, U = E4 ? 16 : 8;
-  const int id = blockIdx.x * kAppendThreads + threadIdx.x, per = c.Hkv * DU;
-  // a wave's lanes may lie on two tokens or more: each finds its own
-  const int t = id / per, chunk = id - t * per, head = chunk / DU, d0 = 8 * (chunk % DU);
-  if (id >= total) return;
-  int lo = 0, hi = b.S;                          // the last s with q_start[s] <= t
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (b.q_start[mid] <= t)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  const long long first = b.q_start[lo], last = b.q_start[lo + 1];
+  constexpr int kBlockBytes = KvFormat<D, KV>::kBlockBytes, kUnits = kBlockBytes / 16, kRow = D + 8;
+  __shared__ __attribute__((aligned(16))) uint16_t s_rows[kAppendThreads / 64][16][kRow];
+  const int lane = threadIdx.x & 63, id = blockIdx.x * (kAppendThreads / 64) + wave_id();
+  const int head = id % c.Hkv, slot = id / c.Hkv;
+  if (slot >= slots) return;
+  const int s = find_sequence(b.q_start, b.S, slot, 16, 2, 1);
+  const long long first = b.q_start[s], n = (long long)b.q_start[s + 1] - first;
+  const long long group = slot - (first / 16 + 2ll * s);
+  if (n <= 0 || group < 0) return;
+  const long long p0 = (long long)b.kv_len[s] - n, base = ((p0 > 0 ? p0 : 0) / 16 + group) * 16;
+  long long hi = kv_length(c, b, s);
+  if (p0 + n < hi) hi = p0 + n;
   Place at;
-  if (!(t >= first && t < last && append_place(c, b, lo, (long long)b.kv_len[lo] - (last - t), 0x7fffffff, at))) return;
+  if (!append_place(c, b, s, base > p0 ? base : p0, 0x7fffffff, at) || base >= hi) return;
   const size_t off = kv_block_offset<kBlockBytes>(c, at.page, head, at.pos >> 4);
+  // token t of the block: its row, or -1
+  auto row_of = [&](int t) {
+    const long long pos = base + t, row = first + pos - p0;
+    return pos >= p0 && pos < hi && row >= 0 && row < b.T ? (int)row : -1;
+  };
   const char *kp = c.k + off, *vp = c.v + off;
-  const int t16 = at.pos & 15;
-  u32x4 kw, vw;
-  if constexpr (E2) {
-    const size_t so = kv_scale_offset<D>(c, at.page, head, at.pos >> 4);
-    const uint32_t byte = (uint8_t)c.k[so + d0 / 32 * 16 + 4 * (t16 & 3) + (t16 >> 2)];
-    const float vs = bf16_bits_to_float(reinterpret_cast<const uint16_t*>(c.v + so)[d0 / 64 * 16 + t16]);
-    kw = e2m1_to_bf16(*reinterpret_cast<const uint32_t*>(kp + d0 / 32 * 256 + t16 * 16 + (d0 / 8 & 3) * 4),
-                      __uint_as_float(byte << 23));
-    const char* codes = vp + d0 / 32 * 256 + (d0 & 15) * 16 + (d0 / 16 & 1) * 8 + t16 / 2;
+  const size_t so = E2 ? kv_scale_offset<D>(c, at.page, head, at.pos >> 4) : 0;
+  const float ks = E4 ? c.k_scale[head] : 1.0f, vs = E4 ? c.v_scale[head] : 1.0f;
+  constexpr int U = (kUnits + 63) / 64;
+  u32x4 kw[U], vw[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float x[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        x[e] = e2m1_value(((uint32_t)(uint8_t)codes[16 * (2 * i + e)] >> (4 * (t16 & 1))) & 15u) * vs;
-      vw[i] = bf16_pair(x[0], x[1]);
+  for (int i = 0; i < U; ++i) {
+    kw[i] = vw[i] = u32x4{0u, 0u, 0u, 0u};
+    if (64 * i + lane < kUnits) {
+      if (ko.p) kw[i] = *reinterpret_cast<const u32x4*>(kp + 16 * (64 * i + lane));
+      if (vo.p) vw[i] = *reinterpret_cast<const u32x4*>(vp + 16 * (64 * i + lane));
     }
-  } else if constexpr (E4) {
-    const u32x2 k = *reinterpret_cast<const u32x2*>(kp + d0 / 16 * 256 + t16 * 16 + (d0 & 8));
-    const u32x4 kb = e4m3_to_bf16(k[0], k[1]);
-    uint32_t v[2] = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i / 4] |= (uint32_t)(uint8_t)vp[(d0 + i) * 16 + t16] << (8 * (i & 3));
-    const u32x4 vb = e4m3_to_bf16(v[0], v[1]);
-    const float ks = c.k_scale[head], vs = c.v_scale[head];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      kw[i] = bf16_pair(half_of(kb[i], 0) * ks, half_of(kb[i], 1) * ks);
-      vw[i] = bf16_pair(half_of(vb[i], 0) * vs, half_of(vb[i], 1) * vs);
-    }
-  } else {
-    kw = *reinterpret_cast<const u32x4*>(kp + d0 / 8 * 256 + t16 * 16);
-    const uint16_t* v = reinterpret_cast<const uint16_t*>(vp) + (t16 / U) * D * U + d0 * U + t16 % U;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vw[i] = (uint32_t)v[2 * i * U] | ((uint32_t)v[(2 * i + 1) * U] << 16);
   }
-  if (ko.p) *reinterpret_cast<u32x4*>(ko.p + (size_t)t * ko.stride + 8 * chunk) = kw;
-  if (vo.p) *reinterpret_cast<u32x4*>(vo.p + (size_t)t * vo.stride + 8 * chunk) = vw;
+  auto scaled = [](u32x4 x, float f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = bf16_pair(half_of(x[e], 0) * f, half_of(x[e], 1) * f);
+    return x;
+  };
+  if (ko.p) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int x = 64 * i + lane, t = x & 15, row = row_of(t);
+      if (x >= kUnits || row < 0) continue;
+      uint16_t* out = ko.p + (size_t)row * ko.stride + (size_t)head * D;
+      if constexpr (E2) {
+        const uint32_t byte = (uint8_t)c.k[so + (x >> 4) * 16 + 4 * (t & 3) + (t >> 2)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<u32x4*>(out + 32 * (x >> 4) + 8 * u) = e2m1_to_bf16(kw[i][u], __uint_as_float(byte << 23));
+      } else if constexpr (E4) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          *reinterpret_cast<u32x4*>(out + 16 * (x >> 4) + 8 * u) =
+              scaled(e4m3_to_bf16(kw[i][2 * u], kw[i][2 * u + 1]), ks);
+      } else {
+        *reinterpret_cast<u32x4*>(out + 8 * (x >> 4)) = kw[i];
+      }
+    }
+  }
+  if (!vo.p) return;
+  uint16_t (*rows)[kRow] = s_rows[wave_id()];
+  auto put = [&](const u32x4& x, int t0, int d) {       // tokens t0 .. t0 + 7 of dimension d
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rows[t0 + e][d] = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
+  };
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int x = 64 * i + lane;
+    if (x >= kUnits) continue;
+    if constexpr (E2) {
+      const int j = x >> 4;
+      const u32x4* sc = reinterpret_cast<const u32x4*>(c.v + so + 32 * (j >> 1));
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const u32x4 sg = sc[g];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) put(e2m1_times(vw[i][2 * h + g], sg), 8 * g, 32 * j + 16 * h + (x & 15));
+      }
+    } else if constexpr (E4) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) put(scaled(e4m3_to_bf16(vw[i][2 * g], vw[i][2 * g + 1]), vs), 8 * g, x);
+    } else {
+      put(vw[i], 8 * (x / D), x % D);
+    }
+  }
+  asm volatile("" ::: "memory");                 // the wave's own: its LDS accesses are in order
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const int x = 64 * i + lane, t = x / (D / 8), d = 8 * (x % (D / 8)), row = row_of(t);
+    if (row >= 0)
+      *reinterpret_cast<u32x4*>(vo.p + (size_t)row * vo.stride + (size_t)head * D + d) =
+          *reinterpret_cast<const u32x4*>(&rows[t][d]);
+  }
 }
 
 hipError_t launch_kv_read(int D, const BatchArgs& b, const KvArgs& c, RowsOut k, RowsOut v, hipStream_t stream) {
-  const int total = b.T * c.Hkv * (D / 8);       // at most 2^16 2^8 2^4
-  const dim3 grid((total + kAppendThreads - 1) / kAppendThreads);
+  const int slots = append_slots(b.T, b.S, 16), per = kAppendThreads / 64;
+  const dim3 grid((unsigned)(((size_t)slots * c.Hkv + per - 1) / per));
   timing_begin(stream, kSiteKvRead);
   with_kv_kind(c, [&](auto kind) {
     constexpr int KV = decltype(kind)::value;
     if (D == 64)
-      hipLaunchKernelGGL((kv_read_kernel<64, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, total);
+      hipLaunchKernelGGL((kv_read_kernel<64, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, slots);
     else
-      hipLaunchKernelGGL((kv_read_kernel<128, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, total);
+      hipLaunchKernelGGL((kv_read_kernel<128, KV>), grid, dim3(kAppendThreads), 0, stream, b, c, k, v, slots);
   });
   timing_end(stream, kSiteKvRead);
   return hipGetLastError();
