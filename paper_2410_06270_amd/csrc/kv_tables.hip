@@ -21,33 +21,55 @@ constexpr int kTabHead = 4;              // workspace: the stack's height, pages
 
 size_t kv_tables_bytes(int S) { return ((size_t)S + kTabHead) * sizeof(int32_t); }
 
-// The inclusive sum over the workgroup's threads before and with this one, and of all; tmp: 17 places.
-__device__ __forceinline__ long long block_scan(long long x, long long* tmp, long long& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+// x plus the x of the lanes that the DPP control and row mask name (0 where there is none).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ long long dpp_add(long long x) {
+  const unsigned long long b = (unsigned long long)x;
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0u, (uint32_t)b, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0u, (uint32_t)(b >> 32), CTRL, ROWS, 0xf, false);
+  return x + (long long)(((unsigned long long)hi << 32) | lo);
+}
+
+// The inclusive sum over the wave's lanes: within rows of 16, then the rows before.
+__device__ __forceinline__ long long wave_scan(long long x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
+}
+
+struct Two {
+  long long a, b;
+};
+
+// The inclusive sums over the workgroup's threads before and with this one, and of all; tmp: a place a wave.
+__device__ __forceinline__ Two block_scan(Two x, Two* tmp, Two& all) {
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  x.a = wave_scan(x.a);
+  x.b = wave_scan(x.b);
   __syncthreads();                               // the last call's places have been read
-  if (lane == 63) tmp[wave] = x;
+  if ((threadIdx.x & 63) == 63) tmp[wave] = x;
   __syncthreads();
-  long long before = 0, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kTabThreads / 64; ++w) {
-    const long long t = tmp[w];
-    if (w < wave) before += t;
-    sum += t;
+  all = Two{0, 0};
+  for (int w = 0; w < waves; ++w) {
+    const Two t = tmp[w];
+    if (w < wave) {
+      x.a += t.a;
+      x.b += t.b;
+    }
+    all.a += t.a;
+    all.b += t.b;
   }
-  all = sum;
-  return x + before;
+  return x;
 }
 
 __device__ __forceinline__ int pages_of(int n, int page_log) {
   return (int)(((long long)n + (1 << page_log) - 1) >> page_log);
 }
 
-// The largest s in [0, S) with start[s] <= key (0 if there is none).
+// The largest s in [0, S) with start[s] <= key (0 if there is none), start being in LDS.
 __device__ __forceinline__ int last_at_most(const int32_t* start, int S, int key) {
   int lo = 0, hi = S;
   while (hi - lo > 1) {
@@ -58,6 +80,27 @@ __device__ __forceinline__ int last_at_most(const int32_t* start, int S, int key
       hi = mid;
   }
   return lo;
+}
+
+// The same in memory for keys first + lane, first being wave-uniform: the whole wave finds the first key's,
+// and the next 64 starts, which the lanes hold, give the others' (2048 requests: 3 loads one after the
+// other for 11).  Every lane of the wave has to take part.
+__device__ __forceinline__ int last_of_wave(const int32_t* __restrict__ start, int S, int first) {
+  const int lane = threadIdx.x & 63, key = first + lane;
+  int base = find_sequence(start, S, first, 1, 0, 1), s = base;
+  while (base + 1 < S) {
+    const int v = base + 1 + lane < S ? start[base + 1 + lane] : 0x7fffffff;
+    // how many of the 64 are at most key (they ascend)
+    int n = 0;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1)
+      if (__shfl(v, n + d - 1) <= key) n += d;
+    const int end = __builtin_amdgcn_readlane(v, 63);
+    s += n == 63 && end <= key ? 64 : n;         // (0 for lanes that have theirs)
+    if (end > first + 63) break;
+    base += 64;
+  }
+  return s;
 }
 
 struct TabArgs {
@@ -73,39 +116,53 @@ struct TabArgs {
   int64_t* slots;
 };
 
-// Pages and rows number i, i + step, ... of a reservation.
-__device__ __forceinline__ void reserve_fill(const TabArgs& a, const int32_t* off, int height, int total, int i,
+// The sums as the second half of a call reads them: offsets of the requests' pages among those that
+// move, row starts and lengths.
+struct TabSums {
+  const int32_t *off, *start, *len;
+};
+
+// Pages and rows number i, i + step, ... of a reservation (FUSED: the sums are in LDS; else i - lane is a
+// multiple of 64 and wave-uniform, and so is step).
+template <bool FUSED>
+__device__ __forceinline__ void reserve_fill(const TabArgs& a, const TabSums& t, int height, int total, int i,
                                              int step) {
   const int mask = (1 << a.page_log) - 1;
-  for (int p = i; p < total; p += step) {
-    const int s = last_at_most(off, a.S, p);
-    const int past = a.kv_len[s] - (a.q_start[s + 1] - a.q_start[s]);
-    a.table[(size_t)s * a.max_pages + pages_of(past, a.page_log) + (p - off[s])] = a.free_list[height - 1 - p];
+  const int lane = threadIdx.x & 63;
+  for (int p = i; FUSED ? p < total : p - lane < total; p += step) {
+    const int s = FUSED ? last_at_most(t.off, a.S, p) : last_of_wave(t.off, a.S, p - lane);
+    if (p >= total) continue;
+    const int past = t.len[s] - (t.start[s + 1] - t.start[s]);
+    a.table[(size_t)s * a.max_pages + pages_of(past, a.page_log) + (p - t.off[s])] = a.free_list[height - 1 - p];
   }
   if (!a.positions && !a.slots) return;
-  const int rows = a.q_start[a.S];
-  for (int t = i; t < a.T; t += step) {
+  const int rows = t.start[a.S];
+  for (int r = i; FUSED ? r < a.T : r - lane < a.T; r += step) {
     int pos = -1;
     int64_t slot = -1;
-    if (t < rows) {
-      const int s = last_at_most(a.q_start, a.S, t);
-      const int end = a.kv_len[s], next = a.q_start[s + 1], past = end - (next - a.q_start[s]);
-      pos = end - (next - t);
+    const int s = FUSED ? last_at_most(t.start, a.S, r) : last_of_wave(t.start, a.S, r - lane);
+    if (r >= a.T) continue;
+    if (r < rows) {
+      const int end = t.len[s], next = t.start[s + 1], past = end - (next - t.start[s]);
+      pos = end - (next - r);
       // a page that another thread is about to write is read where that one reads it
       const int e = pos >> a.page_log, old = pages_of(past, a.page_log);
-      const int page = e < old ? a.table[(size_t)s * a.max_pages + e] : a.free_list[height - 1 - (off[s] + e - old)];
-      slot = ((int64_t)page << a.page_log) | (pos & mask);
+      const int32_t* from =
+          e < old ? a.table + (size_t)s * a.max_pages + e : a.free_list + (height - 1 - (t.off[s] + e - old));
+      slot = ((int64_t)*from << a.page_log) | (pos & mask);
     }
-    if (a.positions) a.positions[t] = pos;
-    if (a.slots) a.slots[t] = slot;
+    if (a.positions) a.positions[r] = pos;
+    if (a.slots) a.slots[r] = slot;
   }
 }
 
+template <bool FUSED>
 __device__ __forceinline__ void release_fill(const TabArgs& a, const int32_t* off, int height, int total, int i,
                                              int step) {
-  for (int p = i; p < total; p += step) {
-    const int s = last_at_most(off, a.S, p);
-    if (height + p < a.n_pages) a.free_list[height + p] = a.table[(size_t)s * a.max_pages + (p - off[s])];
+  const int lane = threadIdx.x & 63;
+  for (int p = i; FUSED ? p < total : p - lane < total; p += step) {
+    const int s = FUSED ? last_at_most(off, a.S, p) : last_of_wave(off, a.S, p - lane);
+    if (p < total && height + p < a.n_pages) a.free_list[height + p] = a.table[(size_t)s * a.max_pages + (p - off[s])];
   }
 }
 
@@ -114,18 +171,20 @@ __device__ __forceinline__ int stack_height(const TabArgs& a) {
   return n < 0 ? 0 : n > a.n_pages ? a.n_pages : n;
 }
 
-// FUSED: the whole call (S <= kTabFused); else the sums, left in the workspace for tab_fill_kernel.
+// FUSED: the whole call (S <= kTabFused), the sums in LDS; else they are left in the workspace for
+// tab_fill_kernel.
 template <bool RESERVE, bool FUSED>
 __global__ void __launch_bounds__(kTabThreads) tab_scan_kernel(TabArgs a, int32_t* ws) {
-  __shared__ long long tmp[kTabThreads / 64];
-  __shared__ int32_t s_off[FUSED ? kTabFused : 1];
+  constexpr int N = FUSED ? kTabFused : 1;
+  __shared__ Two tmp[kTabThreads / 64];
+  __shared__ int32_t s_off[N], s_start[N + 1], s_len[N];
   int32_t* off = FUSED ? s_off : ws + kTabHead;
-  const int height = stack_height(a);
-  const int per = FUSED ? 1 : (a.S + kTabThreads - 1) / kTabThreads;
+  const int height = stack_height(a), threads = blockDim.x;
+  const int per = FUSED && threads == kTabThreads ? 1 : (a.S + threads - 1) / threads;
   const int s0 = threadIdx.x * per < a.S ? threadIdx.x * per : a.S, s1 = s0 + per < a.S ? s0 + per : a.S;
   const long long most = (long long)a.max_pages << a.page_log;
   // a request that fits its row of the table (and, of a release, has ended)
-  auto fits = [&](int s, int& past, int& want, int& need) {
+  auto read = [&](int s, int& past, int& want, int& need) {
     past = a.past[s];
     want = need = 0;
     if (RESERVE) {
@@ -137,66 +196,95 @@ __global__ void __launch_bounds__(kTabThreads) tab_scan_kernel(TabArgs a, int32_
       need = past > most ? a.max_pages : pages_of(past, a.page_log);
     }
   };
-  int past, want, need;
-  long long np = 0, nr = 0, all;
-  for (int s = s0; s < s1; ++s) {
-    fits(s, past, want, need);
-    np += need;
-    nr += want;
+  // a thread's requests stay in registers, where they are few (2048 requests in 1024 threads)
+  constexpr int kHeld = FUSED ? 1 : 4;
+  int held[kHeld][3];
+  if (per <= kHeld) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (s0 + i < s1) read(s0 + i, held[i][0], held[i][1], held[i][2]);
   }
-  long long P = block_scan(np, tmp, all) - np;
+  int past, want, need;
+  auto each = [&](auto f) {
+    if (per <= kHeld) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (s0 + i < s1) {
+          past = held[i][0];
+          want = held[i][1];
+          need = held[i][2];
+          f(s0 + i);
+        }
+    } else {
+      for (int s = s0; s < s1; ++s) {
+        read(s, past, want, need);
+        f(s);
+      }
+    }
+  };
+  Two mine = {0, 0}, all;
+  each([&](int) {
+    mine.a += need;
+    mine.b += want;
+  });
+  const Two upto = block_scan(mine, tmp, all);
+  const long long P = upto.a - mine.a, R = upto.b - mine.b;
   int total;
   if (RESERVE) {
-    long long R = block_scan(nr, tmp, all) - nr;
     // which are granted, and how many rows and pages that makes
     auto granted = [&](long long p, long long r) { return r <= a.T && (need == 0 || p <= height); };
-    long long p = P, r = R, rows = 0, taken = 0;
-    for (int s = s0; s < s1; ++s) {
-      fits(s, past, want, need);
+    long long p = P, r = R;
+    Two got = {0, 0};
+    each([&](int) {
       p += need;
       r += want;
       if (granted(p, r)) {
-        rows += want;
-        taken += need;
+        got.a += want;
+        got.b += need;
       }
+    });
+    long long start = block_scan(got, tmp, all).a - got.a;
+    total = (int)all.b;
+    if (threadIdx.x == 0) {
+      a.q_start[a.S] = (int)all.a;
+      if (FUSED) s_start[a.S] = (int)all.a;
+      *a.n_free_out = height - total;
     }
-    long long start = block_scan(rows, tmp, all) - rows;
-    if (threadIdx.x == 0) a.q_start[a.S] = (int)all;
-    block_scan(taken, tmp, all);
-    total = (int)all;
     p = P;
     r = R;
-    for (int s = s0; s < s1; ++s) {
-      fits(s, past, want, need);
+    each([&](int s) {
       off[s] = (int)(p < total ? p : total);     // (those that are not granted any lie behind the last)
       p += need;
       r += want;
       const int n = granted(p, r) ? want : 0;
       a.q_start[s] = (int)start;
       a.kv_len[s] = past + n;
+      if (FUSED) {
+        s_start[s] = (int)start;
+        s_len[s] = past + n;
+      }
       start += n;
-    }
-    if (threadIdx.x == 0) *a.n_free_out = height - total;
+    });
   } else {
     const long long room = a.n_pages;            // (what is beyond it is not written)
-    total = (int)(all < room ? all : room);
-    for (int s = s0; s < s1; ++s) {
-      fits(s, past, want, need);
-      off[s] = (int)(P < total ? P : total);
-      P += need;
+    long long p = P;
+    total = (int)(all.a < room ? all.a : room);
+    each([&](int s) {
+      off[s] = (int)(p < total ? p : total);
+      p += need;
       a.kv_len[s] = a.done[s] ? 0 : past;
-    }
+    });
     if (threadIdx.x == 0) {
-      const long long n = height + all;
+      const long long n = height + all.a;
       *a.n_free_out = (int)(n < room ? n : room);
     }
   }
   if (FUSED) {
     __syncthreads();
     if (RESERVE)
-      reserve_fill(a, off, height, total, threadIdx.x, kTabThreads);
+      reserve_fill<true>(a, TabSums{s_off, s_start, s_len}, height, total, threadIdx.x, threads);
     else
-      release_fill(a, off, height, total, threadIdx.x, kTabThreads);
+      release_fill<true>(a, s_off, height, total, threadIdx.x, threads);
   } else if (threadIdx.x == 0) {
     ws[0] = height;
     ws[1] = total;
@@ -209,17 +297,17 @@ template <bool RESERVE>
 __global__ void __launch_bounds__(kTabFillThreads) tab_fill_kernel(TabArgs a, const int32_t* __restrict__ ws) {
   const int i = blockIdx.x * kTabFillThreads + threadIdx.x, step = gridDim.x * kTabFillThreads;
   if (RESERVE)
-    reserve_fill(a, ws + kTabHead, ws[0], ws[1], i, step);
+    reserve_fill<false>(a, TabSums{ws + kTabHead, a.q_start, a.kv_len}, ws[0], ws[1], i, step);
   else
-    release_fill(a, ws + kTabHead, ws[0], ws[1], i, step);
+    release_fill<false>(a, ws + kTabHead, ws[0], ws[1], i, step);
 }
 
 template <bool RESERVE>
-static hipError_t tab_launch(const TabArgs& a, bool fused, void* ws, hipStream_t stream) {
+static hipError_t tab_launch(const TabArgs& a, bool fused, bool few, void* ws, hipStream_t stream) {
   int32_t* w = static_cast<int32_t*>(ws);
   timing_begin(stream, kSiteKvTables);
   if (fused) {
-    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(kTabThreads), 0, stream, a, w);
+    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(few ? 256 : kTabThreads), 0, stream, a, w);
   } else {
     hipLaunchKernelGGL((tab_scan_kernel<RESERVE, false>), dim3(1), dim3(kTabThreads), 0, stream, a, w);
     hipLaunchKernelGGL(tab_fill_kernel<RESERVE>, dim3(256), dim3(kTabFillThreads), 0, stream, a, w);
@@ -232,14 +320,14 @@ hipError_t launch_kv_reserve(const int32_t* want, const int32_t* past, const Poo
                              int32_t* positions, int64_t* slots, void* ws, hipStream_t stream) {
   const TabArgs a = {want, past, nullptr, p.free_list, p.n_free, p.n_free_out, p.n_pages, p.page_log, b.q_start,
                      b.kv_len, b.page_table, b.S, b.T, b.max_pages, positions, slots};
-  return tab_launch<true>(a, b.S <= kTabFused && b.T <= kTabRows, ws, stream);
+  return tab_launch<true>(a, b.S <= kTabFused && b.T <= kTabRows, b.S <= 256 && b.T <= 1024, ws, stream);
 }
 
 hipError_t launch_kv_release(const uint8_t* done, const int32_t* past, const PoolArgs& p, const BatchOut& b, void* ws,
                              hipStream_t stream) {
   const TabArgs a = {nullptr, past, done, p.free_list, p.n_free, p.n_free_out, p.n_pages, p.page_log, nullptr,
                      b.kv_len, b.page_table, b.S, 0, b.max_pages, nullptr, nullptr};
-  return tab_launch<false>(a, b.S <= kTabFused && (long long)b.S * b.max_pages <= kTabPages, ws, stream);
+  return tab_launch<false>(a, b.S <= kTabFused && (long long)b.S * b.max_pages <= kTabPages, false, ws, stream);
 }
 
 }  // namespace mc
