@@ -316,6 +316,20 @@ __device__ __forceinline__ float half_wave_sum(float x) {
   return rows_sum(x);
 }
 
+// The inclusive sum over the wave's lanes: within rows of 16, then the rows before.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + (int)__builtin_amdgcn_update_dpp(0u, (uint32_t)x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xf>(x);
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
+}
+
 // The largest over the wave's lanes, and the sum.
 __device__ __forceinline__ float wave_max(float x) {
   x = fmaxf(x, dpp<0xb1>(x));

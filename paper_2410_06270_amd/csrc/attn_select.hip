@@ -329,15 +329,10 @@ __device__ __forceinline__ uint32_t score_key(float f) {
 // The sum over the threads before this one, and over all; tmp: one place a wave.
 __device__ __forceinline__ int counts_before(int x, int* tmp, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int y = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int z = __shfl_up(y, d);
-    if (lane >= d) y += z;
-  }
-  __syncthreads();                               // the last call's places have been read
+  const int y = wave_scan(x);
+  lds_barrier();                                 // the last call's places have been read
   if (lane == 63) tmp[wave] = y;
-  __syncthreads();
+  lds_barrier();
   int before = y - x, sum = 0;
 #pragma unroll
   for (int w = 0; w < kSelThreads / 64; ++w) {
@@ -370,7 +365,7 @@ __device__ void select_pages(const SelectArgs& a, const float* __restrict__ row,
   if (HELD) load(0);
   for (;; shift -= 8) {
     int* hist = s_hist[(shift >> 3) & 1];
-    __syncthreads();
+    lds_barrier();
     for (int r = 0; r < rounds; ++r) {
       if (!HELD) load(r);
 #pragma unroll
@@ -386,7 +381,7 @@ __device__ void select_pages(const SelectArgs& a, const float* __restrict__ row,
           atomicAdd(&hist[lead], __popcll(same));
       }
     }
-    __syncthreads();
+    lds_barrier();
     if (threadIdx.x < 64) {
       // lane l: digits 255 - 4 l downwards; the first whose running count reaches `left`
       const int l = threadIdx.x;
@@ -396,13 +391,7 @@ __device__ void select_pages(const SelectArgs& a, const float* __restrict__ row,
         h[i] = hist[255 - 4 * l - i];
         sum += h[i];
       }
-      int before = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(before, d);
-        if (l >= d) before += y;
-      }
-      before -= sum;
+      int before = wave_scan(sum) - sum;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (before < left && before + h[i] >= left) {
@@ -416,7 +405,7 @@ __device__ void select_pages(const SelectArgs& a, const float* __restrict__ row,
       int* next = s_hist[((shift >> 3) & 1) ^ 1];
       for (int i = threadIdx.x - 64; i < 256; i += kSelThreads - 64) next[i] = 0;
     }
-    __syncthreads();
+    lds_barrier();
     prefix = prefix << 8 | (uint32_t)s_found[0];
     left = s_found[1];
     if (shift == 0 || left == s_found[2]) break;           // all at the prefix are taken
