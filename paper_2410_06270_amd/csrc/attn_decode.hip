@@ -72,10 +72,16 @@ struct SparseArgs {
   int n_sel;
 };
 
+// How many steps a wave holds in registers.  One, and three waves a SIMD, of an e2m1 cache (48
+// sequences of 300 to 8191 tokens 54 -> 46 us, 4 of 50000 to 131071 77 -> 71; four waves a SIMD spill: 70 and
+// 97) and of listed pages (228 rows of 32 pages of 64 e4m3 tokens 67.6 -> 58.4 us, bf16 no difference); two, and two
+// waves, of the others.
+__host__ __device__ constexpr bool one_step(int kv, bool sparse) { return kv == MC_KV_E2M1 || sparse; }
+
 // SPARSE: a row's keys are those of its listed pages, one after the other; a row is any token of
 // a ragged batch (b.q_start null: the last of its sequence).
 template <int D, int KV, int MODE, bool SPARSE>
-__global__ void __launch_bounds__(kDecThreads, KV == MC_KV_E2M1 ? 3 : 2)
+__global__ void __launch_bounds__(kDecThreads, one_step(KV, SPARSE) ? 3 : 2)
     attn_decode_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                        int head_tiles, SparseArgs sparse) {
   using Step = DecodeStep<D, KV>;
@@ -169,7 +175,8 @@ __global__ void __launch_bounds__(kDecThreads, KV == MC_KV_E2M1 ? 3 : 2)
   // Values are read once and by whole lines: past the caches (64 sequences of 4096
   // e4m3 tokens, 537 MB: 109 -> 86 us; of 1024 bf16 tokens and 16 heads 100 -> 83).  A
   // load of keys takes half of each line that it touches, the next the other half: those
-  // stay ordinary loads (non-temporal ones: 58 us for 50 at 4 x 32768 e4m3 tokens).
+  // stay ordinary loads (non-temporal ones: 58 us for 50 at 4 x 32768 e4m3 tokens).  Listed pages are read by
+  // many rows of a chunk: ordinary loads for both (228 rows of 32 pages of 64 bf16 tokens 118 -> 77 us).
   auto load_keys = [&](Step& st, int i, int kp) {
     const int kb = min(step_blk(i) + kblk, last_blk);
     const int kpage = SPARSE ? s_page[(kb >> c.lb) - e0] : kv_page(c, kp);
@@ -189,7 +196,13 @@ __global__ void __launch_bounds__(kDecThreads, KV == MC_KV_E2M1 ? 3 : 2)
     const int vpage = SPARSE ? s_page[(vb >> c.lb) - e0] : kv_page(c, vp);
     const char* vp0 = c.v + kv_block_offset<kBlockBytes>(c, vpage, hk, vb) + voff;
 #pragma unroll
-    for (int t = 0; t < VT; ++t) st.v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp0 + 256 * t));
+    for (int t = 0; t < VT; ++t) {
+      const u32x4* from = reinterpret_cast<const u32x4*>(vp0 + 256 * t);
+      if constexpr (SPARSE)
+        st.v[t] = *from;
+      else
+        st.v[t] = __builtin_nontemporal_load(from);
+    }
     if constexpr (E2) {
       const char* vs = c.v + kv_scale_offset<D>(c, vpage, hk, vb);
 #pragma unroll
@@ -345,10 +358,8 @@ __global__ void __launch_bounds__(kDecThreads, KV == MC_KV_E2M1 ? 3 : 2)
     kp = page_of(blk + kblk);
     vp = page_of(blk + vblk);
   };
-  if constexpr (E2) {
-    // One step in registers: the next one's keys are loaded once this one's are used, its values
-    // likewise, and three waves a SIMD instead of two hide each other's starts (48 sequences of 300 to 8191
-    // tokens 54 -> 46 us, 4 of 50000 to 131071 77 -> 71; four waves spill: 70 and 97)
+  if constexpr (one_step(KV, SPARSE)) {
+    // the next step's keys are loaded once this one's are used, its values likewise
     if (it < i_end) {
       Step st;
       int kp = 0, vp = 0, kn = 0, vn = 0;
