@@ -406,7 +406,7 @@ mc_status mc_pmq_expert_error(const float *w_gate, const float *w_up, const floa
  *   k code   B*8*D + (i/32)*256 + (t%16)*16 + (i%32)/2, half i%2
  *   k scale  Z + B*D/2 + (i/32)*16 + 4*(t%4) + t%16/4: one byte, 2^(byte - 127), 255: NaN
  *   v code   B*8*D + (i/32)*256 + (i%16)*16 + 8*(i/16%2) + (t%16)/2, half t%2
- *   v scale  Z + B*D/2 + (i/64)*32 + 2*(t%16): bf16
+ *   v scale  Z + B*D/2 + (i/64)*32 + 2*(t%16): bf16 of at most 6 significant bits
  * so that 32 dimensions of a key and 64 of a value share a scale.  mc_kv_append takes of keys the
  * least power 2^e with max|y| <= 7 * 2^e, of values max|v| / 6 (in fp32, times the number
  * nearest to 1/6) rounded to 6 significant bits, and the nearest level (ties to the even code); every value is then a bf16 number.  Groups
@@ -546,7 +546,7 @@ mc_status mc_attn_prefill(const uint16_t *q, size_t q_stride, const mc_kv_batch 
 
 /* Keys and values of the batch's new tokens as the cache stands for them, as bf16 rows [T][Hkv*D]
  * with the given elements between them (multiples of 8); k or v may be NULL.  bf16 and e2m1 values
- * come exactly, e4m3's code * scale[h] is rounded once.  Rows of tokens that mc_kv_append would skip (but
+ * come exactly, e4m3's code * scale[h] is rounded to fp32 and then to bf16.  Rows of tokens that mc_kv_append would skip (but
  * for n_pos) and padding rows are left as they were.  Errors as mc_kv_append. */
 mc_status mc_kv_read(const mc_kv_batch* b, const mc_kv_cache* c, uint16_t* k, size_t k_stride, uint16_t* v,
                      size_t v_stride, void* stream);
@@ -555,7 +555,7 @@ mc_status mc_kv_read(const mc_kv_batch* b, const mc_kv_cache* c, uint16_t* k, si
  * release) needs no word from the host and can be captured into a graph.  Free pages are a stack:
  * free_list[0 .. n_free - 1], the top last. */
 typedef struct mc_kv_pool {
-  int n_pages;               /* entries of free_list */
+  int n_pages;               /* entries of free_list, at most 2^30 */
   int page;                  /* tokens a page: 16, 32, 64, 128 or 256 */
   int32_t *free_list;        /* device [n_pages] */
   const int32_t *n_free;     /* device [1]: the stack's height (taken within 0 .. n_pages) */
@@ -620,7 +620,7 @@ mc_status mc_kv_summarize(const mc_kv_batch *b, const mc_kv_cache *c, const mc_k
  * with the largest scores are taken, up to n_sel, equal scores by the lower page.  sel [rows][Hkv][n_sel]:
  * their places in the sequence (columns of page_table), ascending, -1 behind them; count [rows][Hkv].
  * Padding rows are left as they were.  a->prefix and a->slopes must be NULL; the cap does not change the
- * order.  1 <= keep_last, keep_first + keep_last <= n_sel <= MC_MAX_SELECT.
+ * order.  (Scores past fp32's range are taken in some order.)  1 <= keep_last, keep_first + keep_last <= n_sel <= MC_MAX_SELECT.
  * Limits: rows*Hkv, and the rows' heads over 16 times Hkv times max_pages over 256, below 2^24.
  * Workspace: mc_attn_select_workspace (at most some 256 MB, or one row's scores where they are more).
  * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */

@@ -954,6 +954,7 @@ static mc_status check_pool(const mc_kv_pool* p, const mc_kv_tables* t, const in
   if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1)))
     return fail(MC_EINVAL, "page=%d: 16, 32, 64, 128 or 256 tokens", p->page);
   if (p->n_pages < 1) return fail(MC_EINVAL, "n_pages=%d must be >= 1", p->n_pages);
+  if (p->n_pages > kMaxPositions) return fail(MC_EUNSUPPORTED, "n_pages=%d above 2^30", p->n_pages);
   if (!p->free_list || !p->n_free || !p->n_free_out) return fail(MC_EINVAL, "free_list, n_free or n_free_out is NULL");
   if (t->S < 1) return fail(MC_EINVAL, "S=%d must be >= 1", t->S);
   if (t->S > MC_MAX_TOKENS) return fail(MC_EUNSUPPORTED, "S=%d above %d", t->S, MC_MAX_TOKENS);

@@ -124,6 +124,7 @@ def test_read_refusals(b, batch, k, ks, v, vs, status):
 @pytest.mark.parametrize("p,tb,want,past,ws,n,status", [
     (dict(page=24), {}, P, P, P, 1 << 20, EINVAL), (dict(page=8), {}, P, P, P, 1 << 20, EINVAL),
     (dict(n_pages=0), {}, P, P, P, 1 << 20, EINVAL), (dict(free_list=None), {}, P, P, P, 1 << 20, EINVAL),
+    (dict(n_pages=(1 << 30) + 1), {}, P, P, P, 1 << 20, EUNSUPPORTED),
     (dict(n_free=None), {}, P, P, P, 1 << 20, EINVAL), (dict(n_free_out=None), {}, P, P, P, 1 << 20, EINVAL),
     ({}, dict(S=0), P, P, P, 1 << 20, EINVAL), ({}, dict(S=70000), P, P, P, 1 << 20, EUNSUPPORTED),
     ({}, dict(max_pages=0), P, P, P, 1 << 20, EINVAL),
@@ -220,3 +221,28 @@ def test_release_rules():
     assert o4.release([1, 0, 1], [17, 20, 16], free, 1, table, 16) == ([0, 20, 0], 4)
     assert free == [3, 7, 8, 5]
     assert o4.release([1, 1, 1], [32, 32, 32], free, 3, table, 16) == ([0, 0, 0], 4) and free == [3, 7, 8, 7]
+
+
+def test_binding_asserts(b):
+    """Tensors that are not on a GPU, of another type or shape."""
+    i = torch.zeros(4, dtype=torch.int32)
+    for args in ((16, i, i), (16, i.long(), i[:1]), (16, i, i[:1].float())):
+        with pytest.raises(AssertionError):
+            b.KVPool(*args)
+    with pytest.raises(AssertionError):
+        b.KVCache(2, 16, 1, 64, dtype=torch.float4_e2m1fn_x2, k=torch.zeros((2, 544), dtype=torch.uint8),
+                  v=torch.zeros((2, 544), dtype=torch.uint8))        # not on the GPU
+    with pytest.raises(AssertionError):
+        b.kv_page_bytes(16, 1, 64, torch.float16)
+    assert b.kv_page_bytes(16, 1, 64, torch.float4_e2m1fn_x2) == 544
+
+
+def test_many_rows_refused(b):
+    """Launches of 2^24 workgroups and more."""
+    lib = b.load()
+    bt, cc, sm = t.batch(b, S=65536, T=65536), cache4(b, Hkv=256), summary(b, bounds_bytes=1 << 30, scale_bytes=1 << 30)
+    at = t.attention(b, Hq=256)
+    r = ctypes.byref
+    assert lib.mc_kv_summarize(r(bt), r(cc), r(sm), None) == EUNSUPPORTED
+    assert lib.mc_attn_select(P, 1 << 14, r(bt), r(cc), r(sm), r(at), 4, 1, 1, P, P, P, 1 << 40, None) == EUNSUPPORTED
+    assert lib.mc_attn_sparse(P, 1 << 14, r(bt), r(cc), r(at), P, P, 4, P, 1 << 14, None, P, 1 << 40, None) == EUNSUPPORTED

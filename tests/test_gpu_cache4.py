@@ -72,6 +72,9 @@ def quiet_zeros(flat):
     (128, 12, 4, 16, "row", 16, True),
     (64, 0, 2, 16, "head", 48, False),       # keys and values alone
     (128, 40, 1, 32, "none", 128, True),
+    (128, 40, 8, 16, "row", 128, False),     # rows of more than a wave holds
+    (128, 96, 32, 32, "row", 64, True),
+    (64, 5, 256, 16, "head", 64, False),
 ])
 def test_append(mc, D, Hq, Hkv, page, norm, rot, pairs):
     new = [1, 0, 37, 16, 5, 32, 1, 8, 2]
@@ -171,7 +174,7 @@ def test_append_skips(mc):
 
 @pytest.mark.parametrize("dtype", [BF16, torch.float8_e4m3fn])
 def test_read_of_the_other_kinds(mc, dtype):
-    """bf16 as it is, e4m3 times its scale rounded once."""
+    """bf16 as it is, e4m3 times its scale."""
     lens, new = [40, 7, 100], [33, 0, 50]
     w = ta.World(mc, lens, Hkv=3, D=64, page=32, dtype=dtype, seed=3)
     T = sum(new)
@@ -182,7 +185,7 @@ def test_read_of_the_other_kinds(mc, dtype):
     for s, n in enumerate(new):
         for which, got in (("k", k), ("v", v)):
             for h in range(3):
-                # (the product of an 8-bit code and an fp32 scale is exact in 64 bits, so rounded to fp32 and then to bf16)
+                # (the product of a code and an fp32 scale is exact in 64 bits; it is rounded to fp32, then to bf16)
                 want = w.rows(which, s, h)[lens[s] - n:].float().to(BF16)
                 assert torch.equal(got[t0:t0 + n, h * 64:(h + 1) * 64].cpu(), want), (which, s, h)
         t0 += n
@@ -308,3 +311,80 @@ def test_shared_allocation(mc):
         mc.kv_append(None, k, k, None, batch, cache, None)
     assert torch.equal(both[:, 1, 0], plain.k) and torch.equal(both[:, 1, 1], plain.v)
     assert bool((both[:, 0] == 255).all())
+
+
+def test_far_pages(mc):
+    """Pages behind the first 4 GB: what near pages give, bit for bit."""
+    D, Hkv, page, n, Hq = 128, 8, 256, 700, 16
+    per = o4.page_bytes(page, Hkv, D)
+    n_pages = 2 ** 32 // per + 10
+    cache = mc.KVCache(n_pages, page, Hkv, D, dtype=E2M1)
+    sm = mc.KVSummary(cache)
+    g = torch.Generator().manual_seed(2)
+    k, v, q = (torch.randn((n, h * D), generator=g).to(BF16).cuda() for h in (Hkv, Hkv, Hq))
+    at = mc.Attention(Hq, D ** -0.5)
+    ws = torch.empty(max(mc.attn_workspace(n, Hq, Hkv, D), mc.attn_select_workspace(n, Hkv, 3)), dtype=torch.uint8,
+                     device="cuda")
+    outs = []
+    for table in ([2, 0, 1], [n_pages - 1, n_pages - 3, n_pages - 2]):
+        table = torch.tensor([table], dtype=torch.int32, device="cuda")
+        kv_len = torch.tensor([n], dtype=torch.int32, device="cuda")
+        batch = mc.KVBatch(kv_len, table, q_start=ta.starts([n]), T=n)
+        mc.kv_append(None, k, v, None, batch, cache, None)
+        mc.kv_summarize(batch, cache, sm)
+        back = [torch.empty((n, Hkv * D), dtype=BF16, device="cuda") for _ in range(2)]
+        mc.kv_read(batch, cache, *back)
+        o, o1, o2 = (torch.empty((n, Hq * D), dtype=BF16, device="cuda") for _ in range(3))
+        mc.attn_prefill(q, batch, cache, at, o, ws)
+        mc.attn_decode(q[:1], mc.KVBatch(kv_len, table), cache, at, o1[:1], ws)
+        sel = torch.empty((n, Hkv, 2), dtype=torch.int32, device="cuda")
+        count = torch.empty((n, Hkv), dtype=torch.int32, device="cuda")
+        mc.attn_select(q, batch, cache, sm, at, sel, count, ws)
+        mc.attn_sparse(q, batch, cache, at, sel, count, o2, ws)
+        pages = table[0].long()
+        outs.append([*back, o, o1[:1], o2, sel, count, cache.k[pages], cache.v[pages], sm.bounds[pages], sm.scale[pages]])
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    assert bool((cache.k[3:n_pages - 3] == 0).all()) and float(outs[0][2].float().abs().max()) > 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_before_the_first_position(mc, D):
+    """More rows than tokens: the first ones stand at negative positions, see nothing and are not read or
+    written; the others are what they are without them."""
+    Hkv, Hq, page = 2, 4, 16
+    w = World4(mc, [20], Hkv=Hkv, D=D, page=page, seed=D)
+    table = w.table.cuda()
+    kv_len = torch.tensor([20], dtype=torch.int32, device="cuda")
+    wide, exact = (mc.KVBatch(kv_len, table, q_start=ta.starts([n]), T=n) for n in (23, 20))
+    x = w.randn(23, Hkv * D).to(BF16).cuda()
+    q = w.randn(23, Hq * D).to(BF16).cuda()
+    other = mc.KVCache(w.n_pages, page, Hkv, D, dtype=E2M1, k=w.cache.k.clone(), v=w.cache.v.clone())
+    mc.kv_append(None, x, x, None, wide, w.cache, None)
+    mc.kv_append(None, x[3:], x[3:], None, exact, other, None)
+    assert torch.equal(w.cache.k, other.k) and torch.equal(w.cache.v, other.v)
+    at = mc.Attention(Hq, D ** -0.5)
+    sm = [mc.KVSummary(w.cache) for _ in range(2)]
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    got = []
+    for i, (batch, n) in enumerate(((wide, 23), (exact, 20))):
+        mc.kv_summarize(batch, w.cache, sm[i])
+        k = torch.full((n, Hkv * D), 7.0, dtype=BF16, device="cuda")
+        mc.kv_read(batch, w.cache, None, k)
+        sel = torch.full((n, Hkv, 1), 9, dtype=torch.int32, device="cuda")
+        count = torch.full((n, Hkv), 9, dtype=torch.int32, device="cuda")
+        mc.attn_select(q[-n:], batch, w.cache, sm[i], at, sel, count, ws, keep_first=0)
+        o, op = (torch.full((n, Hq * D), 7.0, dtype=BF16, device="cuda") for _ in range(2))
+        lse, lp = (torch.full((n, Hq), 7.0, device="cuda") for _ in range(2))
+        mc.attn_sparse(q[-n:], batch, w.cache, at, sel, count, o, ws, lse=lse)
+        mc.attn_prefill(q[-n:], batch, w.cache, at, op, ws, lse=lp)
+        got.append((k, sel, count, o, lse, op, lp))
+    k, sel, count, o, lse, op, lp = got[0]
+    assert bool((k[:3] == 7.0).all()) and bool((sel[:3] == -1).all()) and bool((count[:3] == 0).all())
+    for x in (o, op):
+        assert bool((x[:3] == 0.0).all())
+    for x in (lse, lp):
+        assert bool((x[:3] == float("-inf")).all())
+    for a, b in zip(*got):
+        assert torch.equal(a[3:], b)
+    assert torch.equal(sm[0].bounds, sm[1].bounds) and torch.equal(sm[0].scale, sm[1].scale)

@@ -172,3 +172,19 @@ def test_loop_against_the_oracle(mc, kind):
                     hq = h * g + i
                     ta.check(loop.o[t:t + 1, hq * D:(hq + 1) * D], o, to, "o t=%d hq=%d" % (t, hq))
                     ta.check(loop.lse[t:t + 1, hq], l, tl, "lse t=%d hq=%d" % (t, hq))
+
+
+def test_timing_names(mc):
+    """The step's launches are found under their names."""
+    loop = Loop(mc, E2M1)
+    want, done, qkv = next(inputs(1, 1))
+    loop.feed(want, done, qkv)
+    mc.timing_enable(True)
+    try:
+        loop.step()
+        for name, n in (("kv_tables", 2), ("kv_append", 1), ("kv_summary", 1), ("attn_select", 1), ("attn_sparse", 1),
+                        ("attn_prefill", 1), ("kv_read", 0)):
+            ms, launches = mc.timing_read(name)
+            assert launches == n and (ms > 0.0) == (n > 0), name
+    finally:
+        mc.timing_enable(False)

@@ -151,3 +151,50 @@ def test_pages_go_round(mc):  # noqa: F811
         assert pool.free_list.tolist()[:height] == ref_free[:height]
         held = [int(ref_table[s, j]) for s in range(S) for j in range(-(-ref_len[s] // page))]
         assert sorted(held + ref_free[:height]) == list(range(n_pages)) and torch.equal(table.cpu(), ref_table)
+
+
+@pytest.mark.parametrize("T", [100, 20000])
+def test_without_positions_or_slots(mc, T):  # noqa: F811
+    """Either array, or none; one workgroup and many."""
+    r = random.Random(T)
+    S, page = 30, 16
+    past, table, _ = state(r, S, page, 100, 0)
+    table = torch.cat((table, torch.full((S, 50), -1, dtype=torch.int32)), 1)
+    want, free = [r.randint(0, T // S) for _ in range(S)], list(range(4000))
+    ref = table.clone()
+    q, kl, pos, sl, left = o4.reserve(want, past, free, 4000, ref, page, T)
+    ws = torch.empty(mc.kv_tables_workspace(S), dtype=torch.uint8, device="cuda")
+    for p, s in ((True, False), (False, True), (False, False), (True, True)):
+        pool = mc.KVPool(page, i32(free), i32([4000]))
+        batch = mc.KVBatch(i32([0] * S), table.cuda(), q_start=i32([0] * (S + 1)), T=T)
+        positions = i32([7] * T) if p else None
+        slots = torch.full((T,), 7, dtype=torch.int64, device="cuda") if s else None
+        mc.kv_reserve(i32(want), i32(past), pool, batch, ws, positions=positions, slots=slots)
+        assert batch.q_start.tolist() == q and batch.kv_len.tolist() == kl and pool.n_free.item() == left
+        assert torch.equal(batch.page_table.cpu(), ref)
+        assert positions is None or positions.tolist() == pos
+        assert slots is None or slots.tolist() == sl
+
+
+def test_most_requests(mc):  # noqa: F811
+    """65536 requests, in place, then all of them released."""
+    S, page = 65536, 16
+    r = random.Random(1)
+    want = [int(r.random() < 0.7) for _ in range(S)]
+    past = [r.choice([0, 3, 15, 16, 31]) for _ in range(S)]
+    table = torch.arange(2 * S, dtype=torch.int32).view(S, 2)
+    n_pages = 3 * S
+    free = list(range(2 * S, 3 * S)) + [0] * (2 * S)
+    # (pages 2 s, 2 s + 1 count as held by s whether it does or not)
+    ref = table.clone()
+    q, kl, _, _, left = o4.reserve(want, past, free, S // 4, ref, page, S)
+    pool = mc.KVPool(page, i32(free), i32([S // 4]))
+    batch = mc.KVBatch(i32(past), table.cuda(), q_start=i32([0] * (S + 1)), T=S)
+    ws = torch.empty(mc.kv_tables_workspace(S), dtype=torch.uint8, device="cuda")
+    mc.kv_reserve(i32(want), batch.kv_len, pool, batch, ws)
+    assert batch.q_start.tolist() == q and batch.kv_len.tolist() == kl and pool.n_free.item() == left
+    assert torch.equal(batch.page_table.cpu(), ref)
+    lens, height = o4.release([1] * S, kl, free, left, ref, page)
+    mc.kv_release(torch.ones(S, dtype=torch.uint8, device="cuda"), batch.kv_len, pool, batch, ws)
+    assert batch.kv_len.tolist() == lens == [0] * S and pool.n_free.item() == height <= n_pages
+    assert pool.free_list.tolist() == free
