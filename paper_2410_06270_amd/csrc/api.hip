@@ -1066,7 +1066,7 @@ mc_status mc_attn_select(const uint16_t* q, size_t q_stride, const mc_kv_batch* 
   const int rows = b->q_start ? b->T : b->S;
   if (mc::select_workgroups(batch_args(b), kv_args(c), a->Hq / c->Hkv) >= 1 << 24 ||
       (long long)rows * c->Hkv >= 1 << 24)
-    return fail(MC_EUNSUPPORTED, "rows*Hkv, or with 256 pages a workgroup the launch, at or above 2^24");
+    return fail(MC_EUNSUPPORTED, "rows*Hkv, or the launch with 64 pages a workgroup, at or above 2^24");
   if (!workspace || misaligned(workspace, 4)) return fail(MC_EINVAL, "workspace is NULL or not 4-byte aligned");
   const size_t need = mc::attn_select_bytes(rows, c->Hkv, b->max_pages);
   if (ws_bytes < need) return fail(MC_ENOSPACE, "workspace %zu bytes, need %zu", ws_bytes, need);

@@ -619,12 +619,12 @@ size_t attn_workspace_bytes(int T, int Hq, int Hkv, int D) {
 
 template <int D, bool SPARSE>
 static void decode_launch(RowsIn q, int rows, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
-                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse,
+                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse, int keys,
                           hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)rows * c.Hkv * head_tiles * sp.nsplit));
   with_kv_kind(c, [&](auto kind) {
-    // (bound by memory: the relative form costs nothing; the older kinds keep what they had)
-    with_score_mode(a, SPARSE || decltype(kind)::value == MC_KV_E2M1, [&](auto mode) {
+    // (a cache of bf16 or e4m3 read whole keeps the form that it had)
+    with_score_mode(a, (SPARSE || decltype(kind)::value == MC_KV_E2M1) && keys <= kCapFew, [&](auto mode) {
       hipLaunchKernelGGL((attn_decode_kernel<D, decltype(kind)::value, decltype(mode)::value, SPARSE>), grid,
                          dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp, head_tiles, sparse);
     });
@@ -647,9 +647,9 @@ hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs&
   sp.ml = sp.o + (size_t)b.S * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnDecode);
   if (D == 64)
-    decode_launch<64, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
+    decode_launch<64, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, max_len, stream);
   else
-    decode_launch<128, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
+    decode_launch<128, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, max_len, stream);
   timing_end(stream, kSiteAttnDecode);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;
@@ -667,9 +667,9 @@ hipError_t launch_attn_sparse(RowsIn q, int D, const BatchArgs& b, const KvArgs&
   sp.ml = sp.o + (size_t)rows * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnSparse);
   if (D == 64)
-    decode_launch<64, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
+    decode_launch<64, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, keys, stream);
   else
-    decode_launch<128, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
+    decode_launch<128, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, keys, stream);
   timing_end(stream, kSiteAttnSparse);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;

@@ -171,15 +171,14 @@ __device__ __forceinline__ float rint_quotient(float x, float by, float r) {
   return n;
 }
 
-// Workspace: scores [row - row0][Hkv][pages], pages the row length of the tables.  A workgroup takes
-// 64 NT pages of a head, a wave NT times 16.  NT = 4 shares a row's quantization among more pages;
-// 1 is for calls that would not fill the chip (one row of 521 pages and 8 heads: 32 workgroups, 9.8
-// us with NT = 4, 7.4 with 1; 16 rows of some 1180 pages: 13.1 us with 4, 17.6 with 1).
-template <int D, int NT>
+// Workspace: scores [row - row0][Hkv][pages], pages the row length of the tables.  A workgroup takes 64 pages
+// of a head, 16 a wave.  (256, four tiles a wave at once: one row of 521 pages 3 us more, 16 rows of some 1180
+// pages 1 us less of 79, 228 rows of some 200 1 us more.)
+template <int D>
 __global__ void __launch_bounds__(kScoreThreads)
     page_score_kernel(RowsIn q, BatchArgs b, KvArgs c, SummaryArgs sm, SelectArgs a, int row0, int row1, int chunks,
                       float* __restrict__ scores) {
-  constexpr int NV = D / 64, kPages = 64 * NT, kQ = D + 16;       // (a row of queries, off the banks of the last)
+  constexpr int NV = D / 64, kPages = 64, kQ = D + 16;       // (a row of queries, off the banks of the last)
   __shared__ float s_part[kScoreWaves][16][kScoreCols + 1];
   __shared__ float s_most[kScoreWaves][kScoreCols], s_sq[kScoreCols];
   __shared__ __attribute__((aligned(16))) int8_t s_q[2][kScoreCols][kQ];
@@ -229,21 +228,15 @@ __global__ void __launch_bounds__(kScoreThreads)
 
   // the bounds of the wave's pages: lane (page n, quarter) holds dimensions 64 v + 16 quarter ..
   const int32_t* pages = b.page_table + (size_t)s * b.max_pages;
-  size_t at[NT];
-  i32x4 bl[NT][NV], bh[NT][NV];
-  float ps[NT];
+  const size_t at = (size_t)kv_page(c, pages[min(p0 + n, hi)]) * c.Hkv + hk;
+  const int8_t* from = sm.bounds + at * 2 * D + 16 * quarter;
+  i32x4 bl[NV], bh[NV];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) at[i] = (size_t)kv_page(c, pages[min(p0 + 64 * i + n, hi)]) * c.Hkv + hk;
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int8_t* from = sm.bounds + at[i] * 2 * D + 16 * quarter;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      bl[i][v] = *reinterpret_cast<const i32x4*>(from + 64 * v);
-      bh[i][v] = *reinterpret_cast<const i32x4*>(from + D + 64 * v);
-    }
-    ps[i] = sm.scale[at[i]];
+  for (int v = 0; v < NV; ++v) {
+    bl[v] = *reinterpret_cast<const i32x4*>(from + 64 * v);
+    bh[v] = *reinterpret_cast<const i32x4*>(from + D + 64 * v);
   }
+  const float ps = sm.scale[at];
 
   // The columns' queries as bytes, by way of LDS (each wave for itself: four times the instructions, which a
   // workgroup runs once and waits for), while the bounds are on their way: the barriers do not wait for them
@@ -284,35 +277,32 @@ __global__ void __launch_bounds__(kScoreThreads)
       neg[v] = *reinterpret_cast<const i32x4*>(&s_q[0][n][64 * v + 16 * quarter]);
       plus[v] = *reinterpret_cast<const i32x4*>(&s_q[1][n][64 * v + 16 * quarter]);
     }
+    if (p0 > hi) continue;                           // the same for the whole wave
+    i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      if (p0 + 64 * i > hi) break;                 // the same for the whole wave
-      i32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bl[i][v], neg[v], sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bh[i][v], plus[v], sum, 0, 0, 0);
-      }
-      // lane (column n, quarter): pages 4 quarter + r of the tile.  Heads are joined by way of LDS, whose
-      // accesses are in order (the places are the wave's own); there lane (n, quarter) has page n
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) s_part[wave][4 * quarter + r4][n] = (float)sum[r4];
-      asm volatile("" ::: "memory");
-      const int page = p0 + 64 * i + n;
-      for (int k = quarter; k < rows; k += 4) {
-        float m = kNegInf;
-        for (int j = 0; j < cols && cols * ht + j < a.g; ++j)
-          m = fmaxf(m, s_part[wave][n][k * cols + j] * (s_sq[k * cols + j] * ps[i]));
-        const int t = first + k;
-        if (page <= hi && t >= row0 && t < row1) {
-          float* out = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + page;
-          if (ht > 0) m = fmaxf(m, *out);
-          *out = m;
-        }
-      }
-      asm volatile("" ::: "memory");
+    for (int v = 0; v < NV; ++v) {
+      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bl[v], neg[v], sum, 0, 0, 0);
+      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(bh[v], plus[v], sum, 0, 0, 0);
     }
+    // lane (column n, quarter): pages 4 quarter + r of the tile.  Heads are joined by way of LDS, whose
+    // accesses are in order (the places are the wave's own); there lane (n, quarter) has page n
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_part[wave][4 * quarter + r][n] = (float)sum[r];
+    asm volatile("" ::: "memory");
+    const int page = p0 + n;
+    for (int k = quarter; k < rows; k += 4) {
+      float m = kNegInf;
+      for (int j = 0; j < cols && cols * ht + j < a.g; ++j)
+        m = fmaxf(m, s_part[wave][n][k * cols + j] * (s_sq[k * cols + j] * ps));
+      const int t = first + k;
+      if (page <= hi && t >= row0 && t < row1) {
+        float* out = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + page;
+        if (ht > 0) m = fmaxf(m, *out);
+        *out = m;
+      }
+    }
+    asm volatile("" ::: "memory");
   }
 }
 
@@ -462,7 +452,9 @@ __global__ void __launch_bounds__(kSelThreads)
   }
   const float* row = scores + ((size_t)(t - row0) * c.Hkv + hk) * b.max_pages + lo;
   if (pages <= 2 * kSelThreads)
-    select_pages<2, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
+    select_pages<2, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);      // (200 pages: 8 keys a thread 3 us more)
+  else if (pages <= 4 * kSelThreads)
+    select_pages<4, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
   else if (pages <= 8 * kSelThreads)
     select_pages<8, true>(a, row, lo, hi, out, s_hist, s_tmp, s_found);
   else
@@ -484,43 +476,30 @@ size_t attn_select_bytes(int rows, int Hkv, int max_pages) {
   return select_rows(rows, Hkv, max_pages) * Hkv * max_pages * sizeof(float);
 }
 
-// Chunks of 64 NT pages that cover any row's (the first begins at a multiple of 16 pages, below the
-// first page of the row).
-static int score_chunks(int max_pages, int nt) { return (max_pages + 64 * nt - 1) / (64 * nt) + 1; }
-
-// Pages a wave takes, in tiles: see page_score_kernel.
-static int score_tiles(const BatchArgs& b, const KvArgs& c, int g) {
-  return (long long)score_slots(b, g) * c.Hkv * score_chunks(b.max_pages, 4) < 512 ? 1 : 4;
-}
+// Chunks of 64 pages that cover any row's (the first begins at a multiple of 16 pages, below the first page of
+// the row).
+static int score_chunks(int max_pages) { return (max_pages + 63) / 64 + 1; }
 
 long long select_workgroups(const BatchArgs& b, const KvArgs& c, int g) {
-  return (long long)score_slots(b, g) * c.Hkv * score_chunks(b.max_pages, score_tiles(b, c, g));
-}
-
-template <int D, int NT>
-static void score_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm, const SelectArgs& a,
-                         int row0, int row1, float* scores, hipStream_t stream) {
-  const int chunks = score_chunks(b.max_pages, NT);
-  const dim3 grid((unsigned)((size_t)score_slots(b, a.g) * c.Hkv * chunks));
-  hipLaunchKernelGGL((page_score_kernel<D, NT>), grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1,
-                     chunks, scores);
+  return (long long)score_slots(b, g) * c.Hkv * score_chunks(b.max_pages);
 }
 
 hipError_t launch_attn_select(RowsIn q, int D, const BatchArgs& b, const KvArgs& c, const SummaryArgs& sm,
                               const SelectArgs& a, void* ws, hipStream_t stream) {
   const int rows = b.q_start ? b.T : b.S, each = (int)select_rows(rows, c.Hkv, b.max_pages);
-  const bool few = score_tiles(b, c, a.g) == 1;
+  const int chunks = score_chunks(b.max_pages);
+  const dim3 grid((unsigned)((size_t)score_slots(b, a.g) * c.Hkv * chunks));
   float* scores = static_cast<float*>(ws);
   hipError_t err = hipSuccess;
   for (int row0 = 0; row0 < rows && err == hipSuccess; row0 += each) {
     const int row1 = row0 + each < rows ? row0 + each : rows;
     timing_begin(stream, kSiteAttnSelect);
     if (D == 64)
-      few ? score_launch<64, 1>(q, b, c, sm, a, row0, row1, scores, stream)
-          : score_launch<64, 4>(q, b, c, sm, a, row0, row1, scores, stream);
+      hipLaunchKernelGGL(page_score_kernel<64>, grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1, chunks,
+                         scores);
     else
-      few ? score_launch<128, 1>(q, b, c, sm, a, row0, row1, scores, stream)
-          : score_launch<128, 4>(q, b, c, sm, a, row0, row1, scores, stream);
+      hipLaunchKernelGGL(page_score_kernel<128>, grid, dim3(kScoreThreads), 0, stream, q, b, c, sm, a, row0, row1, chunks,
+                         scores);
     hipLaunchKernelGGL(page_select_kernel, dim3((unsigned)((size_t)(row1 - row0) * c.Hkv)), dim3(kSelThreads), 0,
                        stream, b, c, a, row0, scores);
     timing_end(stream, kSiteAttnSelect);

@@ -15,8 +15,10 @@
 namespace mc {
 
 constexpr int kTabThreads = 1024;
-constexpr int kTabFused = 1024;          // requests of a call that one workgroup does alone
-constexpr int kTabRows = 8192, kTabPages = 65536;        // its rows; its table entries (release)
+// What one workgroup does alone: requests, rows (reserve), table entries (release).  A release and a
+// reservation: 64 requests, a token each 11.3 us and by two launches each 16.8; 256, 7700 rows 15.6 and 16.9;
+// 1024, 8700 rows 19.9 and 17.8; 64, 48000 rows 42 and 17.
+constexpr int kTabFused = 1024, kTabRows = 8192, kTabPages = 32768;
 constexpr int kTabHead = 4;              // workspace: the stack's height, pages moved, 2 unused; then S offsets
 
 size_t kv_tables_bytes(int S) { return ((size_t)S + kTabHead) * sizeof(int32_t); }
@@ -303,11 +305,11 @@ __global__ void __launch_bounds__(kTabFillThreads) tab_fill_kernel(TabArgs a, co
 }
 
 template <bool RESERVE>
-static hipError_t tab_launch(const TabArgs& a, bool fused, bool few, void* ws, hipStream_t stream) {
+static hipError_t tab_launch(const TabArgs& a, bool fused, void* ws, hipStream_t stream) {
   int32_t* w = static_cast<int32_t*>(ws);
   timing_begin(stream, kSiteKvTables);
   if (fused) {
-    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(few ? 256 : kTabThreads), 0, stream, a, w);
+    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(a.S <= 256 ? 256 : kTabThreads), 0, stream, a, w);
   } else {
     hipLaunchKernelGGL((tab_scan_kernel<RESERVE, false>), dim3(1), dim3(kTabThreads), 0, stream, a, w);
     hipLaunchKernelGGL(tab_fill_kernel<RESERVE>, dim3(256), dim3(kTabFillThreads), 0, stream, a, w);
@@ -320,14 +322,14 @@ hipError_t launch_kv_reserve(const int32_t* want, const int32_t* past, const Poo
                              int32_t* positions, int64_t* slots, void* ws, hipStream_t stream) {
   const TabArgs a = {want, past, nullptr, p.free_list, p.n_free, p.n_free_out, p.n_pages, p.page_log, b.q_start,
                      b.kv_len, b.page_table, b.S, b.T, b.max_pages, positions, slots};
-  return tab_launch<true>(a, b.S <= kTabFused && b.T <= kTabRows, b.S <= 256 && b.T <= 1024, ws, stream);
+  return tab_launch<true>(a, b.S <= kTabFused && b.T <= kTabRows, ws, stream);
 }
 
 hipError_t launch_kv_release(const uint8_t* done, const int32_t* past, const PoolArgs& p, const BatchOut& b, void* ws,
                              hipStream_t stream) {
   const TabArgs a = {nullptr, past, done, p.free_list, p.n_free, p.n_free_out, p.n_pages, p.page_log, nullptr,
                      b.kv_len, b.page_table, b.S, 0, b.max_pages, nullptr, nullptr};
-  return tab_launch<false>(a, b.S <= kTabFused && (long long)b.S * b.max_pages <= kTabPages, false, ws, stream);
+  return tab_launch<false>(a, b.S <= kTabFused && (long long)b.S * b.max_pages <= kTabPages, ws, stream);
 }
 
 }  // namespace mc
