@@ -19,6 +19,9 @@ constexpr int kTabThreads = 1024;
 // reservation: 64 requests, a token each 11.3 us and by two launches each 16.8; 256, 7700 rows 15.6 and 16.9;
 // 1024, 8700 rows 19.9 and 17.8; 64, 48000 rows 42 and 17.
 constexpr int kTabFused = 1024, kTabRows = 8192, kTabPages = 32768;
+// A reservation of few rows by 256 threads, whose barriers meet sooner (by 256 and by 1024, us: 64 requests of a row
+// 3.8, 5.6; 256 of a row 4.3, 6.1; 64 of some 15 rows 5.9, 5.6; 256 of some 30 28.5, 11.8; a release 4.7, 3.7).
+constexpr int kTabFew = 256, kTabFewRows = 512;
 constexpr int kTabHead = 4;              // workspace: the stack's height, pages moved, 2 unused; then S offsets
 
 size_t kv_tables_bytes(int S) { return ((size_t)S + kTabHead) * sizeof(int32_t); }
@@ -309,7 +312,8 @@ static hipError_t tab_launch(const TabArgs& a, bool fused, void* ws, hipStream_t
   int32_t* w = static_cast<int32_t*>(ws);
   timing_begin(stream, kSiteKvTables);
   if (fused) {
-    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(a.S <= 256 ? 256 : kTabThreads), 0, stream, a, w);
+    const bool few = RESERVE && a.S <= kTabFew && a.T <= kTabFewRows;
+    hipLaunchKernelGGL((tab_scan_kernel<RESERVE, true>), dim3(1), dim3(few ? kTabFew : kTabThreads), 0, stream, a, w);
   } else {
     hipLaunchKernelGGL((tab_scan_kernel<RESERVE, false>), dim3(1), dim3(kTabThreads), 0, stream, a, w);
     hipLaunchKernelGGL(tab_fill_kernel<RESERVE>, dim3(256), dim3(kTabFillThreads), 0, stream, a, w);
