@@ -391,7 +391,7 @@ __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float sl
 // Calls f(integral constant of the call's MODE).  relative: caps from kCapRelative on keep the error
 // relative.  That is for calls of few keys, up to kCapFew, whose lse is small and shows an error of 2^-23 cap (one
 // key, a cap of 50: 1.1e-6 of lse); over more it averages out, and the form costs a quarter of a long prompt's
-// time (two chunks of 2048 over 8192 e2m1 tokens 694 -> 864 us; decode of 48 sequences 48 -> 51).
+// time (two chunks of up to 2048 behind up to 8192 e2m1 tokens 694 -> 864 us; decode of 48 sequences 48 -> 51).
 constexpr float kCapRelative = 1.0f;
 constexpr int kCapFew = 256;
 

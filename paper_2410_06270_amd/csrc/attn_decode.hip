@@ -11,14 +11,19 @@
 // to 16 query heads as their columns; that most columns are empty costs nothing
 // that counts (5 % of the matrix rate at 8 TB/s).  48 sequences of 300 to 8191 tokens,
 // 813 MB of bf16: 141 us, 5.8 TB/s; 2 of 50000 to 131071, 380 MB of e4m3: 70 us, 5.4 TB/s.
-// One of 777: 8 us, two launches of three memory latencies each.
+// One of 777: 8 us, two launches of three memory latencies each.  e2m1: 4 of 50000 to 131071, 441 MB, 83 us
+// on data that no cache holds (72 on what was just read), the kernel's loads alone 69 of the 72; 48 of 300 to
+// 8191, 216 MB: 52 and 47, loads alone 42.  Listed pages: 64 pages of 64 bf16 tokens of 16 sequences, 268 MB,
+// 45 us, 6.0 TB/s; 228 rows of 32 pages of 64 e2m1 tokens 67 us, 28 thousand vector instructions a SIMD.
 //
-// A wave takes KS keys a step (32 of bf16, 64 of e4m3: 16 KB for D = 128), all
+// A wave takes KS keys a step (32 of bf16, 64 of the others: 16 KB for D = 128, 8.5 of e2m1), all
 // of it in registers straight from memory, the next step's loads issued before this
 // one's products.  Scores are keys x heads (S^T = K Q^T): lane (head n = lane % 16,
 // quarter q) holds 4 keys of each 16-key tile, and the tiles' rows are dealt so
 // that these are consecutive keys, the very ones that the lane supplies
 // to the product with the values (O^T = V^T P^T): nothing moves between lanes but the maximum.
+// e2m1 keys take their scale in the conversion to bf16 (one instruction for two codes), since a lane's piece of
+// a key has one; a lane's values have one scale a token, which goes to the token's weight.
 #include "attn.hpp"
 
 namespace mc {

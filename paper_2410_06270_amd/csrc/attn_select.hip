@@ -11,6 +11,11 @@
 // pages with 16 (row, head) columns are 2 D / 64 matrix instructions on bytes; negative parts of the
 // query go with lo, positive ones with hi.  page_select_kernel: one workgroup a row and head finds the
 // n-th largest score digit by digit and lists what is above it, and of its equals the first.
+//
+// Bounds are 2 D + 4 bytes a page and head (pages of 64 bf16 tokens: 1/126 of their keys and values), read
+// in pieces of 2 D bytes wherever the pages lie.  16 rows of some 1180 pages, 8 heads: scores 18 us (39 MB at
+// the least, 47 measured), selection 8.4, bounds of the last pages 5.8; one row of 521: 5.3, 5.9 and 4.9, each a chain
+// of memory latencies.  (Both in one launch of 1024 threads, the scores in LDS: 35 us for 25, and 21 for 13.)
 #include "attn.hpp"
 
 namespace mc {
@@ -210,7 +215,7 @@ __global__ void __launch_bounds__(kScoreThreads)
   if (pos < 0) return;
   page_range(a, pos, page_log, lo1, hi);
   page_range(a, pos0 < 0 ? 0 : pos0, page_log, lo, hi1);
-  const int p0 = lo / 16 * 16 + chunk * kPages + 16 * wave;       // the wave's: p0 + 64 i ..
+  const int p0 = lo / 16 * 16 + chunk * kPages + 16 * wave;       // the wave's: p0 .. p0 + 15
   if (lo / 16 * 16 + chunk * kPages > hi) return;
 
   // A head tile's queries: thread (wave, column n, quarter) takes dimensions 32 wave + 8 quarter ..
