@@ -567,7 +567,6 @@ class KVBatch:
         assert q_start is None or T is not None, "q_start comes with T, the number of rows"
         self.S, self.T, self.max_pages = S, S if T is None else int(T), max_pages
         self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
-        self.tables = None
         self.dev = _device_of(kv_len, page_table, q_start)
         self.desc = _KVBatch(S, self.T, max_pages, _bounded(max_len), None if q_start is None else q_start.data_ptr(),
                              kv_len.data_ptr(), page_table.data_ptr())
@@ -702,14 +701,11 @@ def kv_tables_workspace(S: int) -> int:
 
 
 def _tables(batch: KVBatch, positions=None, slots=None):
-    """The batch's arrays as the tables calls take them; the batch keeps the last descriptor made."""
-    at = (None if positions is None else positions.data_ptr(), None if slots is None else slots.data_ptr())
-    last = batch.tables
-    if last is None or last[0] != at:
-        last = batch.tables = (at, ctypes.byref(_KVTables(
-            batch.S, batch.T, batch.max_pages, None if batch.q_start is None else batch.q_start.data_ptr(),
-            batch.kv_len.data_ptr(), batch.page_table.data_ptr(), *at)))
-    return last[1]
+    """The batch's arrays as the tables calls take them."""
+    return ctypes.byref(_KVTables(
+        batch.S, batch.T, batch.max_pages, None if batch.q_start is None else batch.q_start.data_ptr(),
+        batch.kv_len.data_ptr(), batch.page_table.data_ptr(), None if positions is None else positions.data_ptr(),
+        None if slots is None else slots.data_ptr()))
 
 
 def kv_reserve(want, past, pool: KVPool, batch: KVBatch, workspace, positions=None, slots=None, stream=None):
