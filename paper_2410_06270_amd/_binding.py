@@ -557,7 +557,8 @@ class KVCache:
 class KVBatch:
     """Descriptor over a batch's device arrays (int32): kv_len [S], page_table
     [S][max_pages] and, for calls on several new tokens a sequence, q_start
-    [S + 1] with T rows.  max_len: a length that few sequences exceed."""
+    [S + 1] with T rows.  max_len: a length that few sequences exceed.  rows:
+    those that attn_select and attn_sparse take, T, or without q_start S."""
 
     def __init__(self, kv_len, page_table, q_start=None, T=None, max_len: int = 0):
         S, max_pages = page_table.shape
@@ -566,6 +567,7 @@ class KVBatch:
         assert kv_len.numel() == S and (q_start is None or q_start.numel() == S + 1)
         assert q_start is None or T is not None, "q_start comes with T, the number of rows"
         self.S, self.T, self.max_pages = S, S if T is None else int(T), max_pages
+        self.rows = S if q_start is None else self.T
         self.kv_len, self.page_table, self.q_start = kv_len, page_table, q_start
         self.dev = _device_of(kv_len, page_table, q_start)
         self.desc = _KVBatch(S, self.T, max_pages, _bounded(max_len), None if q_start is None else q_start.data_ptr(),
@@ -774,11 +776,11 @@ def _selection(sel, count, rows: int, Hkv: int) -> int:
 def attn_select(q, batch: KVBatch, cache: KVCache, summary: KVSummary, attn: Attention, sel, count, workspace,
                 keep_first: int = 1, keep_last: int = 1, stream=None):
     """q [rows][Hq*D] bf16; writes the selected pages sel (int32 [rows][Hkv][n_sel], places in the
-    sequence) and their number count (int32 [rows][Hkv]).  Rows: the batch's, T or, without q_start, S."""
+    sequence) and their number count (int32 [rows][Hkv]).  rows: batch.rows."""
     dev = _here(q, sel, count, workspace)
     _here_too(dev, cache, batch, summary, attn)
-    n_sel = _selection(sel, count, batch.T, cache.Hkv)
-    qp, qs = _row_matrix(q, batch.T, attn.Hq * cache.D)
+    n_sel = _selection(sel, count, batch.rows, cache.Hkv)
+    qp, qs = _row_matrix(q, batch.rows, attn.Hq * cache.D)
     _check(load().mc_attn_select(qp, qs, batch.ref, cache.ref, summary.ref, attn.ref, n_sel, _bounded(keep_first),
                                  _bounded(keep_last), sel.data_ptr(), count.data_ptr(), workspace.data_ptr(),
                                  workspace.nbytes, _stream_on(dev, stream)))
@@ -789,7 +791,7 @@ def attn_sparse(q, batch: KVBatch, cache: KVCache, attn: Attention, sel, count, 
     wider ones), lse [rows][Hq] float32.  Rows as for attn_select."""
     dev = _here(q, sel, count, o, lse, workspace)
     _here_too(dev, cache, batch, attn)
-    rows, width = batch.T, attn.Hq * cache.D
+    rows, width = batch.rows, attn.Hq * cache.D
     n_sel = _selection(sel, count, rows, cache.Hkv)
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * attn.Hq)
     qp, qs = _row_matrix(q, rows, width)
