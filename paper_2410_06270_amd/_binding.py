@@ -467,11 +467,13 @@ def kv_page_bytes(page: int, Hkv: int, D: int, dtype=torch.bfloat16) -> int:
     return b.value
 
 
-_KV_DTYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float4_e2m1fn_x2: 4}
+_KV_DTYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1}
+if hasattr(torch, "float4_e2m1fn_x2"):           # (all the rest works under a torch without it)
+    _KV_DTYPES[torch.float4_e2m1fn_x2] = 4
 
 
 def _kv_dtype(dtype) -> int:
-    assert dtype in _KV_DTYPES, "a cache holds bfloat16, float8_e4m3fn or float4_e2m1fn_x2"
+    assert dtype in _KV_DTYPES, "a cache holds bfloat16, float8_e4m3fn or float4_e2m1fn_x2 (where torch has it)"
     return _KV_DTYPES[dtype]
 
 
