@@ -621,7 +621,8 @@ mc_status mc_kv_summarize(const mc_kv_batch *b, const mc_kv_cache *c, const mc_k
  * their places in the sequence (columns of page_table), ascending, -1 behind them; count [rows][Hkv].
  * Padding rows are left as they were.  a->prefix and a->slopes must be NULL; the cap does not change the
  * order.  (Scores past fp32's range are taken in some order.)  1 <= keep_last, keep_first + keep_last <= n_sel <= MC_MAX_SELECT.
- * Limits: rows*Hkv, and (rows*min(g, 16)/16 + S)*Hkv*(max_pages/64 + 2) with g = Hq/Hkv, below 2^24.
+ * Limits: rows*Hkv, and tiles*Hkv*(ceil(max_pages/64) + 1), below 2^24; tiles of rows whose heads share a
+ * product: ceil(T/max(1, floor(16/g))) + S - 1 with g = Hq/Hkv, or without q_start S.
  * Workspace: mc_attn_select_workspace (at most some 256 MB, or one row's scores where they are more).
  * Errors: MC_EINVAL, MC_ENOSPACE, MC_EUNSUPPORTED, MC_EHIP. */
 #define MC_MAX_SELECT 4096
