@@ -615,7 +615,8 @@ mc_status mc_kv_summarize(const mc_kv_batch *b, const mc_kv_cache *c, const mc_k
  * for each query head (fp32; NaN and infinities of q count as 0; a negative a->scale turns q's signs), a page's
  * score is
  *   max over the group's heads of (sq * s) * sum_i q8_i * (q8_i > 0 ? hi_i : lo_i),
- * the sum of whole numbers being exact.  Of the pages 0 .. pos / page that a row at position pos sees (with a window,
+ * the sum of whole numbers being exact: at least the product of the rounded query with any finite key of the page, up to
+ * some 2^-22 of sum |q_i| max|k| (the rounding of s).  Of the pages 0 .. pos / page that a row at position pos sees (with a window,
  * those from (pos - window + 1) / page on) the first keep_first of the sequence, the last keep_last and then those
  * with the largest scores are taken, up to n_sel, equal scores by the lower page.  sel [rows][Hkv][n_sel]:
  * their places in the sequence (columns of page_table), ascending, -1 behind them; count [rows][Hkv].

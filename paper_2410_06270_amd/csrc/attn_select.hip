@@ -3,9 +3,10 @@
 //   bounds of a page and key-value head:  s = max |k| / 127 (times the fp32 number nearest to 1/127),
 //   hi = ceil(max_t k / s),  lo = floor(min_t k / s)
 //   score of a page for a row:  max over the group's heads of (sq s) sum_i (q8_i > 0 ? q8_i hi_i : q8_i lo_i)
-// with q8 = rint(q / sq), sq = max |q| / 127: no key of the page has a larger product with the
-// rounded query.  All sums are of whole numbers below 2^24 and so exact in any order; what is rounded
-// is one product, the same in any implementation, and so is the selection.
+// with q8 = rint(q / sq), sq = max |q| / 127.  It bounds the products of the page's finite keys with the rounded
+// query from above, up to 2^-22 of sum |q_i| max |k|: s is rounded, and where 127 s lies below max |k| the quotient's
+// ceiling, 128, is cut to 127.  All sums are of whole numbers below 2^24 and so exact in any order; what is
+// rounded is one product, the same in any implementation, and so is the selection.
 //
 // kv_summary_kernel: one workgroup a touched page and head.  page_score_kernel: the products of 16
 // pages with 16 (row, head) columns are 2 D / 64 matrix instructions on bytes; negative parts of the
