@@ -505,7 +505,9 @@ typedef struct mc_attention {
                                 k_scale[h] times it) */
   float softcap;             /* 0: none; else positive, up to 2^126.  Capped scores are
                                 off by some 2^-22 softcap at most up to 64, above that by
-                                some 2^-19 of themselves */
+                                some 2^-19 of themselves; in mc_attn_decode and
+                                mc_attn_sparse by the latter too, for any softcap, where a
+                                row sees fewer than 32 keys */
   int window;                /* 0: none; else positive (2^30 and more: none) */
   const float *slopes;       /* device [Hq] or NULL */
   const int32_t *prefix;     /* device [S] or NULL */

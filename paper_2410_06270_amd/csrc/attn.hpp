@@ -346,8 +346,8 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // A score in the log2 domain from the plain product q.k.  cap tanh(x / cap) =
 // cap - 2 cap u with u = 1 / (1 + exp(2 x / cap)), off by some 2^-23 cap whatever the
-// score: up to kCapPlain 2^-17, a weight's rounding to bf16 is 2^-8.  Larger caps keep
-// the error relative, the tanh being x / cap (1 - z/3 + 2 z^2/15 - 17 z^3/315 + 62 z^4/2835), z =
+// score: up to kCapPlain 2^-17, a weight's rounding to bf16 is 2^-8.  Larger caps, and decode's
+// rows of few keys, keep the error relative, the tanh being x / cap (1 - z/3 + 2 z^2/15 - 17 z^3/315 + 62 z^4/2835), z =
 // (x / cap)^2, up to x = cap / 4 (the next term, below 2^-26), and cap (1 - 2 u) from there
 // (prefill of 8192 tokens, 32 heads over 8: 803 us, by the first form 651).
 constexpr float kCapPlain = 64.0f;
@@ -369,8 +369,8 @@ __device__ __forceinline__ float cap_unit(float qk, const ScoreConsts& c) {
   return __builtin_amdgcn_rcpf(1.0f + exp2_fast(qk * c.cap_in));
 }
 
-// MODE: bit 0 capped, bit 1 slopes, bit 2 (with 0) a cap above kCapPlain; dist = j - i, a
-// whole number (callers add small ones to one conversion: exact below 2^24).
+// MODE: bit 0 capped, bit 1 slopes, bit 2 (with 0) a relative error (caps above kCapPlain, and edge_mode); dist =
+// j - i, a whole number (callers add small ones to one conversion: exact below 2^24).
 template <int MODE>
 __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float slope2, float dist) {
   float s;
@@ -388,16 +388,24 @@ __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float sl
   return MODE & 2 ? __builtin_fmaf(slope2, dist, s) : s;
 }
 
-// Calls f(integral constant of the call's MODE).  relative: caps from kCapRelative on keep the error
-// relative.  That is for calls of few keys, up to kCapFew, whose lse is small and shows an error of 2^-23 cap (one
-// key, a cap of 50: 1.1e-6 of lse); over more it averages out, and the form costs a quarter of a long prompt's
-// time (two chunks of up to 2048 behind up to 8192 e2m1 tokens 694 -> 864 us; decode of 48 sequences 48 -> 51).
-constexpr float kCapRelative = 1.0f;
-constexpr int kCapFew = 256;
+// Decode: the MODE of a step of keys that the row does not see whole.  A row of few keys has no others, and it is there
+// that an error of the cap's size shows, in an lse as small as the scores (one key, a cap of 50: 1.1e-6): capped
+// scores of such steps keep the error relative, at no cost in time.  (For all steps the form takes 50 us for 47, 48
+// sequences over e2m1 pages; in prefill a quarter of a long prompt's time, and in its masked tiles alone registers:
+// 4096 tokens of 32 heads of 64, 128 -> 148.  There, as in the importance that takes its lse, the cap alone decides.)
+constexpr int edge_mode(int mode) { return mode & 1 ? mode | 4 : mode; }
 
+// x, in a way that work on it is not taken for work on x: what two forms of a score have in common would else be held
+// for all scores at once, beside the scores (registers spilled).
+__device__ __forceinline__ float apart(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Calls f(integral constant of the call's MODE).
 template <class F>
-void with_score_mode(const ScoreArgs& a, bool relative, F&& f) {
-  if (a.softcap > kCapPlain || (relative && a.softcap >= kCapRelative))
+void with_score_mode(const ScoreArgs& a, F&& f) {
+  if (a.softcap > kCapPlain)
     a.slopes ? f(std::integral_constant<int, 7>{}) : f(std::integral_constant<int, 5>{});
   else if (a.softcap > 0.0f)
     a.slopes ? f(std::integral_constant<int, 3>{}) : f(std::integral_constant<int, 1>{});

@@ -268,6 +268,12 @@ __global__ void __launch_bounds__(kDecThreads, one_step(KV, SPARSE) ? 3 : 2)
     const bool whole = SPARSE ? __all(lane_key >= wstart && lane_key + 4 * KT <= len)
                               : (key0 >= wstart && key0 + KS <= len) || key0 + KS <= pre;
     if (!whole) {
+      if constexpr (MODE != edge_mode(MODE)) {     // (again: chosen before the loop above, registers spilled)
+        const float far = apart(dist);
+#pragma unroll
+        for (int e = 0; e < 4 * KT; ++e)
+          x[e] = score2<edge_mode(MODE)>(apart(sv[e / 4][e % 4]), sc, slope2, far + (float)e);
+      }
       // keys out of sight: weight 0, and values 0 whatever the cache holds there
       uint32_t seen = 0;
 #pragma unroll
@@ -624,12 +630,10 @@ size_t attn_workspace_bytes(int T, int Hq, int Hkv, int D) {
 
 template <int D, bool SPARSE>
 static void decode_launch(RowsIn q, int rows, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
-                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse, int keys,
-                          hipStream_t stream) {
+                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)rows * c.Hkv * head_tiles * sp.nsplit));
   with_kv_kind(c, [&](auto kind) {
-    // (a cache of bf16 or e4m3 read whole keeps the form that it had)
-    with_score_mode(a, (SPARSE || decltype(kind)::value == MC_KV_E2M1) && keys <= kCapFew, [&](auto mode) {
+    with_score_mode(a, [&](auto mode) {
       hipLaunchKernelGGL((attn_decode_kernel<D, decltype(kind)::value, decltype(mode)::value, SPARSE>), grid,
                          dim3(kDecThreads), 0, stream, q, b, c, a, o, lse, sp, head_tiles, sparse);
     });
@@ -652,9 +656,9 @@ hipError_t launch_attn_decode(RowsIn q, int D, const BatchArgs& b, const KvArgs&
   sp.ml = sp.o + (size_t)b.S * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnDecode);
   if (D == 64)
-    decode_launch<64, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, max_len, stream);
+    decode_launch<64, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
   else
-    decode_launch<128, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, max_len, stream);
+    decode_launch<128, false>(q, b.S, b, c, a, o, lse, sp, head_tiles, {}, stream);
   timing_end(stream, kSiteAttnDecode);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;
@@ -672,9 +676,9 @@ hipError_t launch_attn_sparse(RowsIn q, int D, const BatchArgs& b, const KvArgs&
   sp.ml = sp.o + (size_t)rows * a.Hq * sp.nsplit * D;
   timing_begin(stream, kSiteAttnSparse);
   if (D == 64)
-    decode_launch<64, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, keys, stream);
+    decode_launch<64, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
   else
-    decode_launch<128, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, keys, stream);
+    decode_launch<128, true>(q, rows, b, c, a, o, lse, sp, head_tiles, {sel, count, n_sel}, stream);
   timing_end(stream, kSiteAttnSparse);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit == 1) return err;

@@ -321,7 +321,7 @@ template <int D, int KV>
 static void colsum_launch(RowsIn q, const float* lse, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, int L,
                           int slices, float* partial, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)col_tiles(L) * slices * c.Hkv));
-  with_score_mode(a, false, [&](auto mode) {
+  with_score_mode(a, [&](auto mode) {
     hipLaunchKernelGGL((attn_colsum_kernel<D, KV, decltype(mode)::value>), grid, dim3(kColThreads), 0, stream, q,
                        lse, b, c, a, L, slices, partial);
   });

@@ -629,7 +629,7 @@ template <int D, int KV>
 static void prefill_launch(RowsIn q, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o, float* lse,
                            const SplitArgs& sp, int slots, int max_len, hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)slots * c.Hkv * sp.nsplit));
-  with_score_mode(a, KV == MC_KV_E2M1 && max_len <= kCapFew, [&](auto mode) {
+  with_score_mode(a, [&](auto mode) {
     constexpr int MODE = decltype(mode)::value;
     if constexpr (D == 64) {
       if (prefill_two_teams(slots, c.Hkv, sp.nsplit, max_len)) {
