@@ -523,7 +523,8 @@ mc_status mc_attn_workspace(int T, int Hq, int Hkv, int D, size_t *bytes);
  * (b->T is ignored), after its key and value are in the cache.
  *   o = sum_j exp(s_j - lse) v_j,   lse = ln sum_j exp(s_j)   over visible j
  * Scores, sums and statistics in fp32; the weights exp(s - max) are rounded to
- * bf16 for the product with the values.  The products are summed in fp32 before they are
+ * bf16 for the product with the values (over e2m1, here and in mc_attn_sparse, the
+ * weights times the values' scales, for the product with the codes).  The products are summed in fp32 before they are
  * divided, with weights up to 2^8 in mc_attn_prefill: the visible |v| (of e4m3, the
  * codes') have to sum to less than 2^120.  A row that sees no key (kv_len 0), or
  * only scores of -infinity, gets o = 0 and lse = -infinity.  What the cache
