@@ -505,9 +505,9 @@ typedef struct mc_attention {
                                 k_scale[h] times it) */
   float softcap;             /* 0: none; else positive, up to 2^126.  Capped scores are
                                 off by some 2^-22 softcap at most up to 64, above that by
-                                some 2^-19 of themselves; in mc_attn_decode and
-                                mc_attn_sparse by the latter too, for any softcap, where a
-                                row sees fewer than 32 keys */
+                                some 2^-19 of themselves, and so for any softcap where a
+                                row sees fewer than 32 keys (in mc_attn_prefill: at
+                                positions 0 to 6, with a prefix below 8) */
   int window;                /* 0: none; else positive (2^30 and more: none) */
   const float *slopes;       /* device [Hq] or NULL */
   const int32_t *prefix;     /* device [S] or NULL */
@@ -618,8 +618,9 @@ mc_status mc_kv_summarize(const mc_kv_batch *b, const mc_kv_cache *c, const mc_k
  * for each query head (fp32; NaN and infinities of q count as 0; a negative a->scale turns q's signs), a page's
  * score is
  *   max over the group's heads of (sq * s) * sum_i q8_i * (q8_i > 0 ? hi_i : lo_i),
- * the sum of whole numbers being exact: at least the product of the rounded query with any finite key of the page, up to
- * some 2^-22 of sum |q_i| max|k| (the rounding of s).  Of the pages 0 .. pos / page that a row at position pos sees (with a window,
+ * the sum of whole numbers being exact: at least the product of the rounded query with any finite key of the
+ * page, up to some 2^-22 of sum |q_i| max|k| (the rounding of s).
+ * Of the pages 0 .. pos / page that a row at position pos sees (with a window,
  * those from (pos - window + 1) / page on) the first keep_first of the sequence, the last keep_last and then those
  * with the largest scores are taken, up to n_sel, equal scores by the lower page.  sel [rows][Hkv][n_sel]:
  * their places in the sequence (columns of page_table), ascending, -1 behind them; count [rows][Hkv].

@@ -346,9 +346,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // A score in the log2 domain from the plain product q.k.  cap tanh(x / cap) =
 // cap - 2 cap u with u = 1 / (1 + exp(2 x / cap)), off by some 2^-23 cap whatever the
-// score: up to kCapPlain 2^-17, a weight's rounding to bf16 is 2^-8.  Larger caps, and decode's
-// rows of few keys, keep the error relative, the tanh being x / cap (1 - z/3 + 2 z^2/15 - 17 z^3/315 + 62 z^4/2835), z =
-// (x / cap)^2, up to x = cap / 4 (the next term, below 2^-26), and cap (1 - 2 u) from there
+// score: up to kCapPlain 2^-17, a weight's rounding to bf16 is 2^-8.  Larger caps, and rows of few keys
+// (edge_mode), keep the error relative, the tanh being x / cap (1 - z/3 + 2 z^2/15 - 17 z^3/315 + 62 z^4/2835), z
+// = (x / cap)^2, up to x = cap / 4 (the next term, below 2^-26), and cap (1 - 2 u) from there
 // (prefill of 8192 tokens, 32 heads over 8: 803 us, by the first form 651).
 constexpr float kCapPlain = 64.0f;
 // Larger caps and scales are refused: theirs are finite in the log2 domain.
@@ -388,15 +388,14 @@ __device__ __forceinline__ float score2(float qk, const ScoreConsts& c, float sl
   return MODE & 2 ? __builtin_fmaf(slope2, dist, s) : s;
 }
 
-// Decode: the MODE of a step of keys that the row does not see whole.  A row of few keys has no others, and it is there
-// that an error of the cap's size shows, in an lse as small as the scores (one key, a cap of 50: 1.1e-6): capped
-// scores of such steps keep the error relative, at no cost in time.  (For all steps the form takes 50 us for 47, 48
-// sequences over e2m1 pages; in prefill a quarter of a long prompt's time, and in its masked tiles alone registers:
-// 4096 tokens of 32 heads of 64, 128 -> 148.  There, as in the importance that takes its lse, the cap alone decides.)
+// The MODE of capped scores whose error is relative: in decode those of a step of keys that the row does not see
+// whole (a row of few keys has no others), in prefill those of rows of few keys.  There an error of the cap's size
+// shows, in an lse as small as the scores (one key, a cap of 50: 1.1e-6).  For all steps the form takes 50 us for 47
+// (48 sequences over e2m1 pages), and a quarter more of a long prompt's time.
 constexpr int edge_mode(int mode) { return mode & 1 ? mode | 4 : mode; }
 
-// x, in a way that work on it is not taken for work on x: what two forms of a score have in common would else be held
-// for all scores at once, beside the scores (registers spilled).
+// x, in a way that work on it is not taken for work on x: what two forms of a score have in common would else be
+// held for all scores at once, beside the scores (registers spilled).
 __device__ __forceinline__ float apart(float x) {
   asm volatile("" : "+v"(x));
   return x;

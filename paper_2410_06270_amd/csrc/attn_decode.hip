@@ -630,7 +630,8 @@ size_t attn_workspace_bytes(int T, int Hq, int Hkv, int D) {
 
 template <int D, bool SPARSE>
 static void decode_launch(RowsIn q, int rows, const BatchArgs& b, const KvArgs& c, const ScoreArgs& a, RowsOut o,
-                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse, hipStream_t stream) {
+                          float* lse, const SplitArgs& sp, int head_tiles, const SparseArgs& sparse,
+                          hipStream_t stream) {
   const dim3 grid((unsigned)((size_t)rows * c.Hkv * head_tiles * sp.nsplit));
   with_kv_kind(c, [&](auto kind) {
     with_score_mode(a, [&](auto mode) {

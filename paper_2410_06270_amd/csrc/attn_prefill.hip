@@ -110,6 +110,13 @@ __device__ __forceinline__ bool clean_values(char* vt, int n) {
   return odd != 0;
 }
 
+// Rows that see fewer keys than this from the first on (those at the first positions, with no longer prefix) have
+// their capped scores formed once more after the loop, in the form whose error is relative: that of the cap, up to
+// kCapPlain, would show in an lse as small as the scores (one key, a cap of 50: 1.1e-6).  In the loop that form costs
+// time or registers wherever it is chosen (masked tiles: 1 to 6 %, 4096 tokens of 32 heads of 64 128 -> 148 us; a
+// second copy of the loop: e2m1 chunks 698 -> 732).
+constexpr int kPreFew = 8;
+
 // The order of a round's instructions: LDS reads some matrix instructions before their
 // use, and the vector work (some 135 instructions) spread over the spaces between all of
 // them: the first products with the values need only the first weights.  Heads of 128, 32
@@ -128,9 +135,14 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
+// Waves a SIMD: three where the loop's registers are at what those may have (168).
+constexpr int pre_waves(int D, int kv, int mode, int G) {
+  return D == 64 && G == 1 && kv == MC_KV_E4M3 && mode == 1 ? 3 : 2;
+}
+
 // MODE: as score2 (attn.hpp).
 template <int D, int KV, int MODE, int G>
-__global__ void __launch_bounds__(G * kPreThreads, 2)
+__global__ void __launch_bounds__(G * kPreThreads, pre_waves(D, KV, MODE, G))
     attn_prefill_kernel(RowsIn q, BatchArgs b, KvArgs c, ScoreArgs a, RowsOut o, float* __restrict__ lse, SplitArgs sp,
                         int slots) {
   constexpr int DT = D / 32, DK = D / 16;      // value tiles; score steps
@@ -559,6 +571,57 @@ __global__ void __launch_bounds__(G * kPreThreads, 2)
             acc[d][r] += in && is_odd ? (E4 ? __builtin_nanf("") : bf16_bits_to_float(w)) : 0.0f;
           }
       }
+    }
+  }
+
+  if constexpr (MODE != edge_mode(MODE)) {
+    if (wave_live && t_begin == 0 && t_end > 0 && pre < kPreFew && wpos_first < kPreFew - 1) {
+      // the first block of keys holds all that these rows see: lane (key n % 16, half) supplies the dimensions
+      // 16 i + 8 half .. that it holds of its query.  (Lane numbers and constants are found anew: held through the
+      // loop, they cost heads of 64 a wave a SIMD)
+      const int id = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), t16 = id & 15, half = id >> 5;
+      const ScoreConsts sc = score_consts(fabsf(apart(a.scale)) * (E4 ? c.k_scale[hk] : 1.0f), a.softcap);
+      const int page = kv_page(c, pages[0]);
+      const char* kp = c.k + kv_block_offset<kBlockBytes>(c, page, hk, 0) + t16 * 16;
+      f32x16 sv;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sv[r] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DK; ++i) {
+        bf16x8 kf;
+        if constexpr (E2) {
+          const uint8_t* ks = reinterpret_cast<const uint8_t*>(c.k + kv_scale_offset<D>(c, page, hk, 0));
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(kp + 256 * (i / 2) + 8 * (i & 1) + 4 * half);
+          const uint32_t byte = ks[16 * (i / 2) + 4 * (t16 & 3) + (t16 >> 2)];
+          kf = as_bf16x8(e2m1_to_bf16(w, __uint_as_float(byte << 23)));
+        } else if constexpr (E4) {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(kp + 256 * i + 8 * half);
+          kf = as_bf16x8(e4m3_to_bf16(w[0], w[1]));
+        } else {
+          kf = as_bf16x8(*reinterpret_cast<const u32x4*>(kp + 256 * (2 * i + half)));
+        }
+        sv = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], sv, 0, 0, 0);
+      }
+      // keys 4 half + r of the row
+      float x[4], mx = kNegInf, sum = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = 4 * half + r;
+        const float y = score2<edge_mode(MODE)>(sv[r], sc, slope2, (float)(j - pos));
+        x[r] = visible(Mask{pos, rlow, rpre}, j) ? y : kNegInf;
+        mx = fmaxf(mx, x[r]);
+      }
+      mx = halves_max(mx);
+      const bool few = (unsigned)pos < (unsigned)(kPreFew - 1) && mx > kNegInf;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += exp2_fast(x[r] - (few ? mx : 0.0f));
+      const float alpha = few ? exp2_fast(m - mx) : 1.0f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] *= alpha;
+      m = few ? mx : m;
+      l = few ? sum : l;
     }
   }
 
